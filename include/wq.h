@@ -352,6 +352,68 @@ wq_status_t wq_direct_forward(const wq_direct_plan_t *plan, void *stream, const 
                               const void *weight_blob_dev, size_t blob_bytes, void *workspace_dev,
                               size_t workspace_bytes, float *y_dev);
 
+/* ---------------------------------------------------------------------------
+ * What stands around a quantized linear layer in a transformer block, for plans of
+ * wq_linear_plan_create / wq_linear_plan_create_bits (any other plan -> UNSUPPORTED), in the formats of
+ * the layer itself: the workspace's xq and sx and the weight blob above.  fp32, bf16 or fp16 tensors
+ * [rows][columns] with a row stride in elements (columns adjacent, rows not overlapping, base aligned
+ * to an element; the stride of a single row is not looked at) and `rows` of the plan's R rows, so that
+ * one plan, one workspace and one blob serve calls of any length up to R: a call touches rows
+ * 0..rows-1 alone, rows = 0 launches nothing (tensor pointers may then be NULL).  Calls on one workspace that
+ * overlap in time race (two streams, two captured graphs); with a workspace each they do not.  Everything
+ * is enqueued on `stream`, may be captured into a graph, and is checked on the host first: a NULL
+ * pointer, rows or a stride out of range, a misaligned tensor, an unknown type or activation ->
+ * INVALID_ARG; a buffer smaller than the layout says -> WORKSPACE. */
+typedef enum { WQ_FP32 = 0, WQ_BF16 = 1, WQ_FP16 = 2 } wq_type_t;
+
+/* z; max(z, 0); z / (1 + e^-z); z (1 + erf(z / sqrt 2)) / 2; z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+typedef enum {
+    WQ_ACT_NONE = 0,
+    WQ_ACT_RELU = 1,
+    WQ_ACT_SILU = 2,
+    WQ_ACT_GELU = 3,
+    WQ_ACT_GELU_TANH = 4
+} wq_activation_t;
+
+/* Root-mean-square norm with the residual's addition, quantized:
+ *   h = x + residual (residual_dev NULL: h = x), in fp32;
+ *   rho = 1 / sqrt(sum of h^2 / Cin + eps), the sum and rho in fp64, rounded once to fp32;
+ *   v = (h rho) gamma, two rounded fp32 products (gamma_dev [Cin] fp32; NULL: v = h rho);
+ *   xq, sx of the workspace: the dynamic group quantizer's codes and scales of v, as wq_direct_quantize
+ *   leaves them of its x.
+ * sum_dev (NULL: not wanted) gets h rounded to the type, while the norm goes on from the unrounded h; it may
+ * be x_dev or residual_dev itself with the same stride (the residual stream updated in place), any other
+ * overlap of the tensors is the caller's error.  All of x, residual and sum are of `type`.  Codes and scales
+ * depend neither on `rows` nor on the launch.  eps: at least 2^-126 and finite, else INVALID_ARG. */
+wq_status_t wq_rms_norm_quantize(const wq_direct_plan_t *plan, void *stream, int rows, int type,
+                                 const void *x_dev, int64_t x_stride, const void *residual_dev,
+                                 int64_t residual_stride, const float *gamma_dev, double eps, void *sum_dev,
+                                 int64_t sum_stride, void *workspace_dev, size_t workspace_bytes);
+
+/* wq_direct_quantize for rows of any type: the codes and scales of x (converted to fp32, which is exact). */
+wq_status_t wq_linear_quantize(const wq_direct_plan_t *plan, void *stream, int rows, int type,
+                               const void *x_dev, int64_t x_stride, void *workspace_dev, size_t workspace_bytes);
+
+/* The product with its epilogue, of the codes that one of the two calls above left in the workspace:
+ *   z = bias + the group-wise product of wq_direct_conv;
+ *   gated 0:  y = act(z) + residual                                  y, residual [rows][Cout]
+ *   gated 1:  y[o] = act(z[o]) z[Cout/2 + o] + residual[o]           y, residual [rows][Cout/2]
+ * (a gated feed-forward layer: the first half of the weight rows is the gate's; Cout has to be a multiple of 32
+ * then, else UNSUPPORTED).  Computed in fp32, rounded once to `type`, which y and residual (NULL: none) share;
+ * y_dev may be residual_dev itself with the same stride.  NOT_PREPARED before wq_direct_weight_prepare.  The sums over groups
+ * are fp32; their order, and with it the last bits of y, may depend on `rows`. */
+wq_status_t wq_linear_matmul(const wq_direct_plan_t *plan, void *stream, int rows, const void *workspace_dev,
+                             size_t workspace_bytes, const void *weight_blob_dev, size_t blob_bytes,
+                             int activation, int gated, int type, const void *residual_dev,
+                             int64_t residual_stride, void *y_dev, int64_t y_stride);
+
+/* wq_linear_quantize followed by wq_linear_matmul; x, residual and y of one type.  What the workspace holds
+ * afterwards is unspecified. */
+wq_status_t wq_linear_forward(const wq_direct_plan_t *plan, void *stream, int rows, int type, const void *x_dev,
+                              int64_t x_stride, const void *weight_blob_dev, size_t blob_bytes,
+                              void *workspace_dev, size_t workspace_bytes, int activation, int gated,
+                              const void *residual_dev, int64_t residual_stride, void *y_dev, int64_t y_stride);
+
 /* Issue-rate microbenchmark of the contraction's inner loop, without memory traffic: every
  * wave repeats, `iters` times (even), the int8 MFMAs of one quantization group on
  * `blocks_per_wave` (2 or 4) 16x16 blocks followed by the per-group dequantization the second

@@ -1,0 +1,345 @@
+// What stands around a quantized linear layer in a transformer block, in the formats of the layer itself:
+//   k_rms_norm_quantize   h = x + residual, v = h rho gamma with rho = 1 / sqrt(mean(h^2) + eps), group-wise
+//                         int8 codes and scales of v
+//   k_quantize_rows       the same codes of rows of any float type
+//   k_linear              y = act(x W^T + bias) (or, gated, act(gate) * up) + residual
+// Activations lie in the workspace as the standard convolution keeps them (planes of one K-quarter of one MFMA
+// K-step, rows in order inside a plane), weights in the blob in MFMA operand order.
+#include <float.h>
+#include <math.h>
+
+#include "wq_device.h"
+#include "wq_direct_plan.h"
+
+namespace {
+
+// ------------------------------------------------------------ element types
+template <int TYPE>
+struct Elem;
+template <>
+struct Elem<WQ_FP32> {
+    using type = float;
+};
+template <>
+struct Elem<WQ_BF16> {
+    using type = __bf16;
+};
+template <>
+struct Elem<WQ_FP16> {
+    using type = _Float16;
+};
+
+int type_size(int type) { return type == WQ_FP32 ? 4 : 2; }
+
+// ------------------------------------------------------------ norm, quantization
+struct QArgs {
+    const void *x, *res;   // rows of the type, res may be null
+    void *sum;             // h, may be null; may be x or res itself
+    const float *gamma;    // may be null
+    int8_t *xq;
+    float *sx;
+    long xs, rs, hs;       // row strides in elements
+    int rows, P, Cin, g;   // P: rows of the workspace's planes
+    double eps;
+};
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
+    return v;
+}
+
+// The norm's factor.  The squares of fp32 numbers are exact in 64 bits and their sum is off by some 1e-16, so
+// that the factor, rounded once to fp32, does not depend on the order of the sum, nor do the codes behind it.
+__device__ __forceinline__ float norm_factor(double squares, int Cin, double eps) {
+    return (float)(1.0 / sqrt(squares / Cin + eps));
+}
+
+template <int TYPE, bool NORM>
+__global__ __launch_bounds__(256) void k_quantize_row(const QArgs a) {
+    using T = typename Elem<TYPE>::type;
+    __shared__ double part[4];
+    const int p = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const T *x = (const T *)a.x + (size_t)p * a.xs, *res = a.res ? (const T *)a.res + (size_t)p * a.rs : nullptr;
+    T *sum = a.sum ? (T *)a.sum + (size_t)p * a.hs : nullptr;
+    auto load = [&](int c) { return res ? (float)x[c] + (float)res[c] : (float)x[c]; };
+    float rho = 1.0f;
+    if constexpr (NORM) {
+        double q = 0.0;
+        for (int c = tid; c < a.Cin; c += 256) {
+            const double h = (double)load(c);
+            q += h * h;
+        }
+        q = wave_sum(q);
+        if (lane == 0) part[w] = q;
+        __syncthreads();
+        rho = norm_factor(part[0] + part[1] + part[2] + part[3], a.Cin, a.eps);
+    }
+    const int KB = a.g == 32 ? 8 : 16;
+    for (int gi = w; gi < a.Cin / a.g; gi += 4) {
+        float v[8];
+        float top = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int j = lane + 64 * k, c = gi * a.g + j;
+            v[k] = 0.0f;
+            if (j >= a.g) continue;
+            const float h = load(c);
+            if (NORM && sum) sum[c] = (T)h;
+            v[k] = NORM ? (a.gamma ? h * rho * a.gamma[c] : h * rho) : h;
+            top = fmaxf(top, fabsf(v[k]));
+        }
+#pragma unroll
+        for (int m = 32; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+        float s = 0.0f, r = 0.0f;
+        if (top >= 127.0f * FLT_MIN) {
+            s = top / 127.0f;   // correctly rounded
+            r = 127.0f / top;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int j = lane + 64 * k, c = gi * a.g + j;
+            if (j < a.g) a.xq[((size_t)(c / KB) * a.P + p) * KB + c % KB] = (int8_t)quant_code(v[k], r);
+        }
+        if (lane == 0) a.sx[(size_t)gi * a.P + p] = s;
+    }
+}
+
+// ------------------------------------------------------------ product
+struct LArgs {
+    const int8_t *xq, *Wq;
+    const float *sx, *sW, *bias;
+    const void *res;   // may be null; may be y itself
+    void *y;
+    long rs, ys;       // row strides in elements
+    int rows, P, Cin, Cout_pad, log2g;
+    int outs;          // columns of y: Cout, or Cout / 2 with a gate
+    int type, act;
+};
+
+__device__ __forceinline__ float activate(float z, int act) {
+    switch (act) {
+        case WQ_ACT_RELU: return fmaxf(z, 0.0f);
+        case WQ_ACT_SILU: return z / (1.0f + expf(-z));
+        case WQ_ACT_GELU: return 0.5f * z * erfcf(z * -0.70710678f);
+        // z (1 + tanh u) / 2 = z / (1 + e^-2u)
+        case WQ_ACT_GELU_TANH: return z / (1.0f + expf(-1.5957691f * (z + 0.044715f * z * z * z)));
+        default: return z;
+    }
+}
+
+__device__ __forceinline__ float load_elem(const void *p, long i, int type) {
+    if (type == WQ_FP32) return ((const float *)p)[i];
+    if (type == WQ_BF16) return (float)((const __bf16 *)p)[i];
+    return (float)((const _Float16 *)p)[i];
+}
+
+__device__ __forceinline__ void store_elem(void *p, long i, int type, float v) {
+    if (type == WQ_FP32) ((float *)p)[i] = v;
+    else if (type == WQ_BF16) ((__bf16 *)p)[i] = (__bf16)v;
+    else ((_Float16 *)p)[i] = (_Float16)v;
+}
+
+// A wave owns 16 channels (gated: two blocks of 16, of the gate and of what it multiplies) x 16 rows.
+template <bool K64, bool W4, bool GATED>
+__global__ __launch_bounds__(256) void k_linear(const LArgs a) {
+    constexpr int KSTEP = K64 ? 64 : 32, KB = KSTEP / 4, BLK = 16 * KSTEP, NE = GATED ? 2 : 1;
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, q = lane >> 4;
+    const int nO = (a.outs + 15) / 16, id = (int)blockIdx.x * 4 + (tid >> 6);
+    const int ob = id % nO, p0 = id / nO * 16, p = p0 + l16;
+    if (p0 >= a.rows) return;
+    const int groups = a.Cin >> a.log2g, cpg = (1 << a.log2g) / KSTEP;
+    float M[NE][4] = {};
+    for (int gi = 0; gi < groups; ++gi) {
+        v4i acc[NE];
+#pragma unroll
+        for (int e = 0; e < NE; ++e) acc[e] = v4i{0, 0, 0, 0};
+        for (int k = 0; k < cpg; ++k) {
+            const int ks = gi * cpg + k;
+            v4i b = {0, 0, 0, 0};
+            if (p < a.rows) {
+                const int8_t *src = a.xq + ((size_t)(ks * 4 + q) * a.P + p) * KB;
+                if constexpr (K64) b = *(const v4i *)src;
+                else b.x = ((const int *)src)[0], b.y = ((const int *)src)[1];
+            }
+#pragma unroll
+            for (int e = 0; e < NE; ++e) {
+                const size_t off = (size_t)(ob + e * nO) * 16 * a.Cin + (size_t)ks * BLK + lane * KB;
+                v4i wv = {0, 0, 0, 0};
+                if constexpr (W4) {
+                    const unsigned *src = (const unsigned *)(a.Wq + off / 2);
+                    const unsigned a0 = src[0], a1 = K64 ? src[1] : 0u;
+                    wv = v4i{(int)((a0 << 4) & 0xf0f0f0f0u), (int)(a0 & 0xf0f0f0f0u), (int)((a1 << 4) & 0xf0f0f0f0u),
+                             (int)(a1 & 0xf0f0f0f0u)};
+                } else if constexpr (K64) {
+                    wv = *(const v4i *)(a.Wq + off);
+                } else {
+                    const int *src = (const int *)(a.Wq + off);
+                    wv.x = src[0], wv.y = src[1];
+                }
+                if constexpr (K64)
+                    acc[e] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv, b, acc[e], 0, 0, 0);
+                else
+                    acc[e] = __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, v2i{wv.x, wv.y}),
+                                                                   __builtin_bit_cast(long, v2i{b.x, b.y}), acc[e], 0, 0, 0);
+            }
+        }
+        const float sx = p < a.rows ? a.sx[(size_t)gi * a.P + p] : 0.0f;
+#pragma unroll
+        for (int e = 0; e < NE; ++e)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float sw = a.sW[(size_t)gi * a.Cout_pad + (ob + e * nO) * 16 + 4 * q + r] * (W4 ? 0.0625f : 1.0f);
+                M[e][r] = __builtin_fmaf((float)acc[e][r], sw * sx, M[e][r]);
+            }
+    }
+    if (p >= a.rows) return;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int o = ob * 16 + 4 * q + r;
+        if (o >= a.outs) continue;
+        float z = activate(M[0][r] + a.bias[o], a.act);
+        if constexpr (GATED) z *= M[1][r] + a.bias[a.outs + o];
+        if (a.res) z += load_elem(a.res, p * a.rs + o, a.type);
+        store_elem(a.y, p * a.ys + o, a.type, z);
+    }
+}
+
+bool good_type(int type) { return type == WQ_FP32 || type == WQ_BF16 || type == WQ_FP16; }
+
+// A tensor [rows][cols] of the type with a row stride: aligned to its elements, rows that do not overlap.
+bool good_rows(const void *t, int64_t stride, int rows, int cols, int type) {
+    return ((uintptr_t)t % type_size(type)) == 0 && (rows <= 1 || (stride >= cols && stride <= INT64_MAX / 16 / rows));
+}
+
+template <int TYPE>
+void launch_quantize(const QArgs &a, bool norm, hipStream_t s) {
+    const dim3 grid((unsigned)a.rows), block(256);
+    if (norm) hipLaunchKernelGGL((k_quantize_row<TYPE, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_quantize_row<TYPE, false>), grid, block, 0, s, a);
+}
+
+wq_status_t run_quantize(const wq_direct_plan *plan, hipStream_t s, int type, QArgs &a, bool norm, void *workspace) {
+    char *ws = (char *)workspace;
+    a.xq = (int8_t *)(ws + plan->lay.ws_xq_off);
+    a.sx = (float *)(ws + plan->lay.ws_sx_off);
+    a.P = plan->P; a.Cin = plan->Cin; a.g = plan->g;
+    if (a.rows == 0) return WQ_OK;
+    if (type == WQ_FP32) launch_quantize<WQ_FP32>(a, norm, s);
+    else if (type == WQ_BF16) launch_quantize<WQ_BF16>(a, norm, s);
+    else launch_quantize<WQ_FP16>(a, norm, s);
+    return hipGetLastError() == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;
+}
+
+template <bool K64, bool W4>
+void launch_linear(const LArgs &a, bool gated, hipStream_t s) {
+    const long waves = (long)((a.outs + 15) / 16) * ((a.rows + 15) / 16);
+    const dim3 grid((unsigned)((waves + 3) / 4)), block(256);
+    if (gated) hipLaunchKernelGGL((k_linear<K64, W4, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_linear<K64, W4, false>), grid, block, 0, s, a);
+}
+
+int ilog2(int v) {
+    int l = 0;
+    while ((1 << l) < v) ++l;
+    return l;
+}
+
+// What wq_linear_matmul and wq_linear_forward check about the product.
+wq_status_t check_product(const wq_direct_plan_t *plan, int rows, const void *workspace, size_t workspace_bytes,
+                          const void *blob, size_t blob_bytes, int activation, int gated, int type, const void *res,
+                          int64_t res_stride, const void *y, int64_t y_stride) {
+    if (!plan || !workspace || !blob || (rows != 0 && !y)) return WQ_ERR_INVALID_ARG;
+    if (plan->taps != 1) return WQ_ERR_UNSUPPORTED;
+    if (rows < 0 || rows > plan->P || !good_type(type) || activation < WQ_ACT_NONE || activation > WQ_ACT_GELU_TANH ||
+        (gated != 0 && gated != 1))
+        return WQ_ERR_INVALID_ARG;
+    if (gated && plan->Cout % 32 != 0) return WQ_ERR_UNSUPPORTED;
+    const int outs = gated ? plan->Cout / 2 : plan->Cout;
+    if (!good_rows(y, y_stride, rows, outs, type) || (res && !good_rows(res, res_stride, rows, outs, type)))
+        return WQ_ERR_INVALID_ARG;
+    if (workspace_bytes < plan->lay.ws_bytes || blob_bytes < plan->lay.blob_bytes) return WQ_ERR_WORKSPACE;
+    if (!plan->prepared.load()) return WQ_ERR_NOT_PREPARED;
+    return WQ_OK;
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------ C ABI
+extern "C" {
+
+wq_status_t wq_rms_norm_quantize(const wq_direct_plan_t *plan, void *stream, int rows, int type, const void *x_dev,
+                                 int64_t x_stride, const void *residual_dev, int64_t residual_stride,
+                                 const float *gamma_dev, double eps, void *sum_dev, int64_t sum_stride,
+                                 void *workspace_dev, size_t workspace_bytes) {
+    if (!plan || (rows != 0 && !x_dev) || !workspace_dev) return WQ_ERR_INVALID_ARG;
+    if (plan->taps != 1) return WQ_ERR_UNSUPPORTED;
+    if (rows < 0 || rows > plan->P || !good_type(type) || !(eps >= FLT_MIN && eps <= DBL_MAX))
+        return WQ_ERR_INVALID_ARG;
+    if (!good_rows(x_dev, x_stride, rows, plan->Cin, type) ||
+        (residual_dev && !good_rows(residual_dev, residual_stride, rows, plan->Cin, type)) ||
+        (sum_dev && !good_rows(sum_dev, sum_stride, rows, plan->Cin, type)) || ((uintptr_t)gamma_dev & 3))
+        return WQ_ERR_INVALID_ARG;
+    if (workspace_bytes < plan->lay.ws_bytes) return WQ_ERR_WORKSPACE;
+    QArgs a = {};
+    a.x = x_dev; a.res = residual_dev; a.sum = sum_dev; a.gamma = gamma_dev;
+    a.xs = x_stride; a.rs = residual_stride; a.hs = sum_stride;
+    a.rows = rows; a.eps = eps;
+    return run_quantize(plan, (hipStream_t)stream, type, a, true, workspace_dev);
+}
+
+wq_status_t wq_linear_quantize(const wq_direct_plan_t *plan, void *stream, int rows, int type, const void *x_dev,
+                               int64_t x_stride, void *workspace_dev, size_t workspace_bytes) {
+    if (!plan || (rows != 0 && !x_dev) || !workspace_dev) return WQ_ERR_INVALID_ARG;
+    if (plan->taps != 1) return WQ_ERR_UNSUPPORTED;
+    if (rows < 0 || rows > plan->P || !good_type(type) || !good_rows(x_dev, x_stride, rows, plan->Cin, type))
+        return WQ_ERR_INVALID_ARG;
+    if (workspace_bytes < plan->lay.ws_bytes) return WQ_ERR_WORKSPACE;
+    QArgs a = {};
+    a.x = x_dev; a.xs = x_stride; a.rows = rows;
+    return run_quantize(plan, (hipStream_t)stream, type, a, false, workspace_dev);
+}
+
+wq_status_t wq_linear_matmul(const wq_direct_plan_t *plan, void *stream, int rows, const void *workspace_dev,
+                             size_t workspace_bytes, const void *weight_blob_dev, size_t blob_bytes, int activation,
+                             int gated, int type, const void *residual_dev, int64_t residual_stride, void *y_dev,
+                             int64_t y_stride) {
+    const wq_status_t st = check_product(plan, rows, workspace_dev, workspace_bytes, weight_blob_dev, blob_bytes,
+                                         activation, gated, type, residual_dev, residual_stride, y_dev, y_stride);
+    if (st != WQ_OK || rows == 0) return st;
+    const char *ws = (const char *)workspace_dev, *b = (const char *)weight_blob_dev;
+    LArgs a = {};
+    a.xq = (const int8_t *)(ws + plan->lay.ws_xq_off);
+    a.sx = (const float *)(ws + plan->lay.ws_sx_off);
+    a.Wq = (const int8_t *)(b + plan->lay.blob_Wq_off);
+    a.sW = (const float *)(b + plan->lay.blob_sW_off);
+    a.bias = (const float *)(b + plan->lay.blob_bias_off);
+    a.res = residual_dev; a.y = y_dev; a.rs = residual_stride; a.ys = y_stride;
+    a.rows = rows; a.P = plan->P; a.Cin = plan->Cin; a.Cout_pad = plan->Cout_pad; a.log2g = ilog2(plan->g);
+    a.outs = gated ? plan->Cout / 2 : plan->Cout;
+    a.type = type; a.act = activation;
+    hipStream_t s = (hipStream_t)stream;
+    if (plan->wbits == 4) {
+        if (plan->kstep == 32) launch_linear<false, true>(a, gated, s);
+        else launch_linear<true, true>(a, gated, s);
+    } else {
+        if (plan->kstep == 32) launch_linear<false, false>(a, gated, s);
+        else launch_linear<true, false>(a, gated, s);
+    }
+    return hipGetLastError() == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;
+}
+
+wq_status_t wq_linear_forward(const wq_direct_plan_t *plan, void *stream, int rows, int type, const void *x_dev,
+                              int64_t x_stride, const void *weight_blob_dev, size_t blob_bytes, void *workspace_dev,
+                              size_t workspace_bytes, int activation, int gated, const void *residual_dev,
+                              int64_t residual_stride, void *y_dev, int64_t y_stride) {
+    const wq_status_t st = check_product(plan, rows, workspace_dev, workspace_bytes, weight_blob_dev, blob_bytes,
+                                         activation, gated, type, residual_dev, residual_stride, y_dev, y_stride);
+    if (st != WQ_OK) return st;
+    const wq_status_t sq = wq_linear_quantize(plan, stream, rows, type, x_dev, x_stride, workspace_dev, workspace_bytes);
+    if (sq != WQ_OK) return sq;
+    return wq_linear_matmul(plan, stream, rows, workspace_dev, workspace_bytes, weight_blob_dev, blob_bytes, activation,
+                            gated, type, residual_dev, residual_stride, y_dev, y_stride);
+}
+
+}  // extern "C"

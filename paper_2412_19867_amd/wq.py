@@ -28,6 +28,7 @@ EXPORTS = ["wq_standard_transforms", "wq_scaled_transforms", "wq_plan_create", "
            "wq_direct_plan_create", "wq_linear_plan_create", "wq_direct_plan_create_bits",
            "wq_linear_plan_create_bits", "wq_direct_plan_destroy", "wq_direct_plan_layout",
            "wq_direct_weight_prepare", "wq_direct_quantize", "wq_direct_conv", "wq_direct_forward",
+           "wq_rms_norm_quantize", "wq_linear_quantize", "wq_linear_matmul", "wq_linear_forward",
            "wq_conv_forward_debug", "wq_status_string"]
 
 
@@ -55,6 +56,8 @@ K2_VARIANTS = {"auto": -1, "fused_16x16": 0, "fused_ksplit": 1, "fused_32x16": 2
                "gemm_64x64": 10, "gemm_32x128": 11, "gemm_128x128": 12,
                "lds_full_64x64": 20, "lds_full_32x64": 21, "lds_full_32x32": 22, "lds_row_64x64": 30, "lds_row_32x64": 31,
                "lds_tap_64x64": 40, "lds_tap_128x128": 41}
+# wq_activation_t
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 K2_VARIANT_NAMES = {v: k for k, v in K2_VARIANTS.items()}
 
 
@@ -105,6 +108,11 @@ def lib() -> ctypes.CDLL:
         L.wq_direct_quantize.argtypes = [vp, vp, vp, vp, sz]
         L.wq_direct_conv.argtypes = [vp, vp, vp, sz, vp, sz, vp]
         L.wq_direct_forward.argtypes = [vp, vp, vp, vp, sz, vp, sz, vp]
+        ll = ctypes.c_int64
+        L.wq_rms_norm_quantize.argtypes = [vp, vp, ip, ip, vp, ll, vp, ll, vp, ctypes.c_double, vp, ll, vp, sz]
+        L.wq_linear_quantize.argtypes = [vp, vp, ip, ip, vp, ll, vp, sz]
+        L.wq_linear_matmul.argtypes = [vp, vp, ip, vp, sz, vp, sz, ip, ip, ip, vp, ll, vp, ll]
+        L.wq_linear_forward.argtypes = [vp, vp, ip, ip, vp, ll, vp, sz, vp, sz, ip, ip, vp, ll, vp, ll]
         L.wq_status_string.argtypes = [ip]
         L.wq_status_string.restype = ctypes.c_char_p
         for name in EXPORTS:
@@ -495,3 +503,105 @@ class DirectPlan:
                                        _dev_ptr(ws, torch.uint8, "workspace"), ws.numel(),
                                        _dev_ptr(y, torch.float32, "y", L.P * L.Cout)),
                "wq_direct_forward")
+
+
+class LinearPlan(DirectPlan):
+    """A group-wise quantized linear layer of up to `rows` rows, with what a transformer block puts
+    around it: the root-mean-square norm with the residual's addition in front of it, bias, activation,
+    gate and residual behind it.  x, residual and outputs are [n][columns] tensors of one float type
+    (fp32, bf16, fp16) with adjacent columns and any row stride, n <= rows; blob and workspace are
+    DirectPlan's.  All tensors are on the device of the stream, which is the current one."""
+
+    def __init__(self, rows, Cin, Cout, group_size, weight_bits: int = 8):
+        super().__init__(rows, 1, 1, Cin, Cout, group_size, linear=True, weight_bits=weight_bits)
+        L = self.layout
+        self._rows, self._cin, self._cout = L.P, L.Cin, L.Cout
+        self._blob_bytes, self._ws_bytes = L.blob_bytes, L.ws_bytes
+
+    def _buffer(self, t, need, what):
+        """Address of a workspace or blob on the current device."""
+        import torch
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous():
+            raise TypeError(f"{what}: expected a contiguous uint8 device tensor")
+        if t.get_device() != torch.cuda.current_device():
+            raise ValueError(f"{what}: expected a tensor on the current device")
+        return t.data_ptr()
+
+    @staticmethod
+    def _tensor(t, like, cols, what):
+        """(address, row stride) of a [n][cols] tensor; `like`: the call's first tensor, whose type, device and rows it shares."""
+        import torch
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{what}: expected a device tensor")
+        if t.dtype != like.dtype:
+            raise TypeError(f"{what}: expected {like.dtype}")
+        if t.dim() != 2 or t.shape[1] != cols or t.shape[0] != like.shape[0]:
+            raise ValueError(f"{what}: expected shape [{like.shape[0]}][{cols}], got {tuple(t.shape)}")
+        if t.stride(1) != 1:
+            raise ValueError(f"{what}: expected adjacent columns")
+        if t.get_device() != like.get_device():
+            raise ValueError(f"{what}: expected a tensor on the same device")
+        return t.data_ptr(), t.stride(0)
+
+    def _first(self, t, cols, ws, what):
+        """(rows, type, address, row stride) of a call's first tensor."""
+        import torch
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{what}: expected a device tensor")
+        code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t.dtype)
+        if code is None:
+            raise TypeError(f"{what}: expected fp32, bf16 or fp16")
+        if t.dim() != 2 or t.shape[1] != cols or t.shape[0] > self._rows:
+            raise ValueError(f"{what}: expected shape [up to {self._rows}][{cols}], got {tuple(t.shape)}")
+        if t.stride(1) != 1:
+            raise ValueError(f"{what}: expected adjacent columns")
+        if t.get_device() != ws.get_device():
+            raise ValueError(f"{what}: expected a tensor on the workspace's device")
+        return t.shape[0], code, t.data_ptr(), t.stride(0)
+
+    def _epilogue(self, activation, gated):
+        act = ACTIVATIONS.get(activation)
+        if act is None:
+            raise ValueError(f"activation: expected one of {', '.join(ACTIVATIONS)}")
+        return act, self._cout // 2 if gated else self._cout
+
+    def rms_norm_quantize(self, x, ws, residual=None, gamma=None, eps=1e-6, out=None, stream=None):
+        """Codes and scales of (x + residual) / rms(x + residual) * gamma into the workspace; `out` (may be
+        x or residual itself) gets x + residual.  gamma: fp32 [Cin]."""
+        import torch
+        wp = self._buffer(ws, self._ws_bytes, "workspace")
+        n, code, xp, xs = self._first(x, self._cin, ws, "x")
+        rp, rs = (None, 0) if residual is None else self._tensor(residual, x, self._cin, "residual")
+        op, os_ = (None, 0) if out is None else self._tensor(out, x, self._cin, "out")
+        gp = None if gamma is None else _dev_ptr(gamma, torch.float32, "gamma", self._cin)
+        if gamma is not None and gamma.get_device() != ws.get_device():
+            raise ValueError("gamma: expected a tensor on the workspace's device")
+        _check(lib().wq_rms_norm_quantize(self._h, _stream_handle(stream), n, code, xp, xs, rp, rs, gp, float(eps), op,
+                                          os_, wp, ws.numel()), "wq_rms_norm_quantize")
+
+    def quantize_rows(self, x, ws, stream=None):
+        """Codes and scales of x into the workspace."""
+        wp = self._buffer(ws, self._ws_bytes, "workspace")
+        n, code, xp, xs = self._first(x, self._cin, ws, "x")
+        _check(lib().wq_linear_quantize(self._h, _stream_handle(stream), n, code, xp, xs, wp, ws.numel()),
+               "wq_linear_quantize")
+
+    def matmul(self, ws, blob, y, activation="none", gated=False, residual=None, stream=None):
+        """y = act(z) + residual, or act(gate) * up + residual, z the product of the workspace's first
+        len(y) rows with the weights, plus bias."""
+        act, outs = self._epilogue(activation, gated)
+        wp, bp = self._buffer(ws, self._ws_bytes, "workspace"), self._buffer(blob, self._blob_bytes, "blob")
+        n, code, yp, ys = self._first(y, outs, ws, "y")
+        rp, rs = (None, 0) if residual is None else self._tensor(residual, y, outs, "residual")
+        _check(lib().wq_linear_matmul(self._h, _stream_handle(stream), n, wp, ws.numel(), bp, blob.numel(), act,
+                                      1 if gated else 0, code, rp, rs, yp, ys), "wq_linear_matmul")
+
+    def linear(self, x, blob, ws, y, activation="none", gated=False, residual=None, stream=None):
+        """quantize_rows followed by matmul."""
+        act, outs = self._epilogue(activation, gated)
+        wp, bp = self._buffer(ws, self._ws_bytes, "workspace"), self._buffer(blob, self._blob_bytes, "blob")
+        n, code, xp, xs = self._first(x, self._cin, ws, "x")
+        yp, ys = self._tensor(y, x, outs, "y")
+        rp, rs = (None, 0) if residual is None else self._tensor(residual, x, outs, "residual")
+        _check(lib().wq_linear_forward(self._h, _stream_handle(stream), n, code, xp, xs, bp, blob.numel(), wp, ws.numel(),
+                                       act, 1 if gated else 0, rp, rs, yp, ys), "wq_linear_forward")
