@@ -6,10 +6,8 @@
 // Activations lie in the workspace as the standard convolution keeps them (planes of one K-quarter of one MFMA
 // K-step, rows in order inside a plane), weights in the blob in MFMA operand order.
 #include <float.h>
-#include <math.h>
 
-#include "wq_device.h"
-#include "wq_direct_plan.h"
+#include "wq_linear_args.h"
 
 namespace {
 
@@ -106,105 +104,6 @@ __global__ __launch_bounds__(256) void k_quantize_row(const QArgs a) {
 }
 
 // ------------------------------------------------------------ product
-struct LArgs {
-    const int8_t *xq, *Wq;
-    const float *sx, *sW, *bias;
-    const void *res;   // may be null; may be y itself
-    void *y;
-    long rs, ys;       // row strides in elements
-    int rows, P, Cin, Cout_pad, log2g;
-    int outs;          // columns of y: Cout, or Cout / 2 with a gate
-    int type, act;
-};
-
-__device__ __forceinline__ float activate(float z, int act) {
-    switch (act) {
-        case WQ_ACT_RELU: return fmaxf(z, 0.0f);
-        case WQ_ACT_SILU: return z / (1.0f + expf(-z));
-        case WQ_ACT_GELU: return 0.5f * z * erfcf(z * -0.70710678f);
-        // z (1 + tanh u) / 2 = z / (1 + e^-2u)
-        case WQ_ACT_GELU_TANH: return z / (1.0f + expf(-1.5957691f * (z + 0.044715f * z * z * z)));
-        default: return z;
-    }
-}
-
-__device__ __forceinline__ float load_elem(const void *p, long i, int type) {
-    if (type == WQ_FP32) return ((const float *)p)[i];
-    if (type == WQ_BF16) return (float)((const __bf16 *)p)[i];
-    return (float)((const _Float16 *)p)[i];
-}
-
-__device__ __forceinline__ void store_elem(void *p, long i, int type, float v) {
-    if (type == WQ_FP32) ((float *)p)[i] = v;
-    else if (type == WQ_BF16) ((__bf16 *)p)[i] = (__bf16)v;
-    else ((_Float16 *)p)[i] = (_Float16)v;
-}
-
-// A wave owns 16 channels (gated: two blocks of 16, of the gate and of what it multiplies) x 16 rows.
-template <bool K64, bool W4, bool GATED>
-__global__ __launch_bounds__(256) void k_linear(const LArgs a) {
-    constexpr int KSTEP = K64 ? 64 : 32, KB = KSTEP / 4, BLK = 16 * KSTEP, NE = GATED ? 2 : 1;
-    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, q = lane >> 4;
-    const int nO = (a.outs + 15) / 16, id = (int)blockIdx.x * 4 + (tid >> 6);
-    const int ob = id % nO, p0 = id / nO * 16, p = p0 + l16;
-    if (p0 >= a.rows) return;
-    const int groups = a.Cin >> a.log2g, cpg = (1 << a.log2g) / KSTEP;
-    float M[NE][4] = {};
-    for (int gi = 0; gi < groups; ++gi) {
-        v4i acc[NE];
-#pragma unroll
-        for (int e = 0; e < NE; ++e) acc[e] = v4i{0, 0, 0, 0};
-        for (int k = 0; k < cpg; ++k) {
-            const int ks = gi * cpg + k;
-            v4i b = {0, 0, 0, 0};
-            if (p < a.rows) {
-                const int8_t *src = a.xq + ((size_t)(ks * 4 + q) * a.P + p) * KB;
-                if constexpr (K64) b = *(const v4i *)src;
-                else b.x = ((const int *)src)[0], b.y = ((const int *)src)[1];
-            }
-#pragma unroll
-            for (int e = 0; e < NE; ++e) {
-                const size_t off = (size_t)(ob + e * nO) * 16 * a.Cin + (size_t)ks * BLK + lane * KB;
-                v4i wv = {0, 0, 0, 0};
-                if constexpr (W4) {
-                    const unsigned *src = (const unsigned *)(a.Wq + off / 2);
-                    const unsigned a0 = src[0], a1 = K64 ? src[1] : 0u;
-                    wv = v4i{(int)((a0 << 4) & 0xf0f0f0f0u), (int)(a0 & 0xf0f0f0f0u), (int)((a1 << 4) & 0xf0f0f0f0u),
-                             (int)(a1 & 0xf0f0f0f0u)};
-                } else if constexpr (K64) {
-                    wv = *(const v4i *)(a.Wq + off);
-                } else {
-                    const int *src = (const int *)(a.Wq + off);
-                    wv.x = src[0], wv.y = src[1];
-                }
-                if constexpr (K64)
-                    acc[e] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv, b, acc[e], 0, 0, 0);
-                else
-                    acc[e] = __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, v2i{wv.x, wv.y}),
-                                                                   __builtin_bit_cast(long, v2i{b.x, b.y}), acc[e], 0, 0, 0);
-            }
-        }
-        const float sx = p < a.rows ? a.sx[(size_t)gi * a.P + p] : 0.0f;
-#pragma unroll
-        for (int e = 0; e < NE; ++e)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float sw = a.sW[(size_t)gi * a.Cout_pad + (ob + e * nO) * 16 + 4 * q + r] * (W4 ? 0.0625f : 1.0f);
-                M[e][r] = __builtin_fmaf((float)acc[e][r], sw * sx, M[e][r]);
-            }
-    }
-    if (p >= a.rows) return;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const int o = ob * 16 + 4 * q + r;
-        if (o >= a.outs) continue;
-        float z = activate(M[0][r] + a.bias[o], a.act);
-        if constexpr (GATED) z *= M[1][r] + a.bias[a.outs + o];
-        if (a.res) z += load_elem(a.res, p * a.rs + o, a.type);
-        store_elem(a.y, p * a.ys + o, a.type, z);
-    }
-}
-
 bool good_type(int type) { return type == WQ_FP32 || type == WQ_BF16 || type == WQ_FP16; }
 
 // A tensor [rows][cols] of the type with a row stride: aligned to its elements, rows that do not overlap.
@@ -229,14 +128,6 @@ wq_status_t run_quantize(const wq_direct_plan *plan, hipStream_t s, int type, QA
     else if (type == WQ_BF16) launch_quantize<WQ_BF16>(a, norm, s);
     else launch_quantize<WQ_FP16>(a, norm, s);
     return hipGetLastError() == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;
-}
-
-template <bool K64, bool W4>
-void launch_linear(const LArgs &a, bool gated, hipStream_t s) {
-    const long waves = (long)((a.outs + 15) / 16) * ((a.rows + 15) / 16);
-    const dim3 grid((unsigned)((waves + 3) / 4)), block(256);
-    if (gated) hipLaunchKernelGGL((k_linear<K64, W4, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((k_linear<K64, W4, false>), grid, block, 0, s, a);
 }
 
 int ilog2(int v) {
@@ -308,7 +199,7 @@ wq_status_t wq_linear_matmul(const wq_direct_plan_t *plan, void *stream, int row
                                          activation, gated, type, residual_dev, residual_stride, y_dev, y_stride);
     if (st != WQ_OK || rows == 0) return st;
     const char *ws = (const char *)workspace_dev, *b = (const char *)weight_blob_dev;
-    LArgs a = {};
+    wq_linear_args a = {};
     a.xq = (const int8_t *)(ws + plan->lay.ws_xq_off);
     a.sx = (const float *)(ws + plan->lay.ws_sx_off);
     a.Wq = (const int8_t *)(b + plan->lay.blob_Wq_off);
@@ -317,16 +208,14 @@ wq_status_t wq_linear_matmul(const wq_direct_plan_t *plan, void *stream, int row
     a.res = residual_dev; a.y = y_dev; a.rs = residual_stride; a.ys = y_stride;
     a.rows = rows; a.P = plan->P; a.Cin = plan->Cin; a.Cout_pad = plan->Cout_pad; a.log2g = ilog2(plan->g);
     a.outs = gated ? plan->Cout / 2 : plan->Cout;
-    a.type = type; a.act = activation;
+    a.type = type; a.act = activation; a.gated = gated;
+    const int64_t piece = 4 * type_size(type);
+    auto whole = [&](const void *t, int64_t stride) { return (uintptr_t)t % piece == 0 && (rows == 1 || stride % 4 == 0); };
+    a.wide = whole(y_dev, y_stride) && (!residual_dev || whole(residual_dev, residual_stride));
     hipStream_t s = (hipStream_t)stream;
-    if (plan->wbits == 4) {
-        if (plan->kstep == 32) launch_linear<false, true>(a, gated, s);
-        else launch_linear<true, true>(a, gated, s);
-    } else {
-        if (plan->kstep == 32) launch_linear<false, false>(a, gated, s);
-        else launch_linear<true, false>(a, gated, s);
-    }
-    return hipGetLastError() == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;
+    const int n = rows > 256 ? 4 : 2;
+    const hipError_t e = plan->wbits == 4 ? wq_launch_linear_tile4(a, plan->g, n, n, s) : wq_launch_linear_tile8(a, plan->g, n, n, s);
+    return e == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;
 }
 
 wq_status_t wq_linear_forward(const wq_direct_plan_t *plan, void *stream, int rows, int type, const void *x_dev,
