@@ -53,6 +53,128 @@ __device__ __forceinline__ float norm_factor(double squares, int Cin, double eps
     return (float)(1.0 / sqrt(squares / Cin + eps));
 }
 
+// The group quantizer's scale and reciprocal of a group with this largest magnitude.
+__device__ __forceinline__ void group_scale(float top, float &s, float &r) {
+    const bool live = top >= 127.0f * FLT_MIN;
+    s = live ? top / 127.0f : 0.0f;   // correctly rounded
+    r = live ? 127.0f / top : 0.0f;
+}
+
+// Eight adjacent elements (aligned to 16 bytes) as fp32, and back.
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, float (&v)[8]) {
+    typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+        const vec t = ((const vec *)p)[k];
+#pragma unroll
+        for (int j = 0; j < 16 / (int)sizeof(T); ++j) v[k * 16 / sizeof(T) + j] = (float)t[j];
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T *p, const float (&v)[8]) {
+    typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+        vec t;
+#pragma unroll
+        for (int j = 0; j < 16 / (int)sizeof(T); ++j) t[j] = (T)v[k * 16 / sizeof(T) + j];
+        ((vec *)p)[k] = t;
+    }
+}
+
+// Rows in pieces of eight elements a lane, held in registers: one pass over the data.  A group of g elements is g / 8 adjacent
+// lanes of one wave.  NORM: `wpr` waves share a row of up to 512 V wpr elements; otherwise a wave takes 512 V elements of
+// a row (the rows one after the other, then the next elements of each), wpr = 1.
+template <int TYPE, bool NORM, int V>
+__global__ __launch_bounds__(512) void k_quantize_pieces(const QArgs a, int wpr, int per_xcd) {
+    using T = typename Elem<TYPE>::type;
+    __shared__ double part[8];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rpw = (int)(blockDim.x >> 6) / wpr;   // rows of a workgroup
+    // neighbouring rows' codes share lines: an XCD takes a contiguous share of the rows, whose lines its L2 puts together
+    const long unit = ((long)(blockIdx.x & 7u) * per_xcd + (blockIdx.x >> 3)) * rpw + w / wpr;
+    const int p = NORM ? (int)unit : (int)(unit % a.rows);
+    const int c0 = NORM ? (w % wpr) * 512 + lane * 8 : (int)(unit / a.rows) * (512 * V) + lane * 8, step = 512 * wpr;
+    const bool row = NORM ? unit < a.rows : true;
+    const T *x = (const T *)a.x + (size_t)p * a.xs;
+    float v[V][8];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int c = c0 + k * step;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[k][j] = 0.0f;
+        if (row && c < a.Cin) load8<T>(x + c, v[k]);
+    }
+    if constexpr (NORM) {
+        if (a.res) {
+            const T *res = (const T *)a.res + (size_t)p * a.rs;
+            float t[V][8];
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) t[k][j] = 0.0f;
+                if (row && c0 + k * step < a.Cin) load8<T>(res + c0 + k * step, t[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[k][j] += t[k][j];
+        }
+        double squares = 0.0;
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) squares = __builtin_fma((double)v[k][j], (double)v[k][j], squares);
+        squares = wave_sum(squares);
+        if (wpr > 1) {
+            if (lane == 0) part[w] = squares;
+            __syncthreads();
+            squares = 0.0;
+            for (int k = 0; k < wpr; ++k) squares += part[w / wpr * wpr + k];
+        }
+        if (a.sum) {   // (all of the row has been read: it may be x or the residual itself)
+            T *sum = (T *)a.sum + (size_t)p * a.hs;
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (row && c0 + k * step < a.Cin) store8<T>(sum + c0 + k * step, v[k]);
+        }
+        const float rho = norm_factor(squares, a.Cin, a.eps);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            float gm[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+            if (a.gamma && c0 + k * step < a.Cin) load8<float>(a.gamma + c0 + k * step, gm);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[k][j] = v[k][j] * rho * gm[j];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int c = c0 + k * step;
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[k][j]) & 0x7fffffffu);
+        top = dpp_max<0xB1>(top);   // quad_perm [1,0,3,2]
+        top = dpp_max<0x4E>(top);   // quad_perm [2,3,0,1]: the 4 lanes of 32 elements
+        if (a.g > 32) top = dpp_max<0x141>(top);   // row_half_mirror: 8 lanes
+        if (a.g > 64) top = dpp_max<0x140>(top);   // row_mirror: 16 lanes
+        if (a.g > 128) top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+        if (a.g > 256) top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+        float s, r;
+        group_scale(__uint_as_float(top), s, r);
+        const uint32_t lo = quant_code(v[k][0], r) | (quant_code(v[k][1], r) << 8) | (quant_code(v[k][2], r) << 16) |
+                            (quant_code(v[k][3], r) << 24);
+        const uint32_t hi = quant_code(v[k][4], r) | (quant_code(v[k][5], r) << 8) | (quant_code(v[k][6], r) << 16) |
+                            (quant_code(v[k][7], r) << 24);
+        if (!row || c >= a.Cin) continue;
+        // planes of 8 bytes a row with groups of 32, else of 16, of which this is a half
+        const size_t at = a.g == 32 ? ((size_t)(c >> 3) * a.P + p) * 8 : ((size_t)(c >> 4) * a.P + p) * 16 + (c & 8);
+        *(uint2 *)(a.xq + at) = make_uint2(lo, hi);
+        if ((c & (a.g - 1)) == 0) a.sx[(size_t)(c / a.g) * a.P + p] = s;
+    }
+}
+
+// Rows of any alignment and any length, read twice: a workgroup to a row, a wave to a group at a time.
 template <int TYPE, bool NORM>
 __global__ __launch_bounds__(256) void k_quantize_row(const QArgs a) {
     using T = typename Elem<TYPE>::type;
@@ -89,11 +211,8 @@ __global__ __launch_bounds__(256) void k_quantize_row(const QArgs a) {
         }
 #pragma unroll
         for (int m = 32; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
-        float s = 0.0f, r = 0.0f;
-        if (top >= 127.0f * FLT_MIN) {
-            s = top / 127.0f;   // correctly rounded
-            r = 127.0f / top;
-        }
+        float s, r;
+        group_scale(top, s, r);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const int j = lane + 64 * k, c = gi * a.g + j;
@@ -111,11 +230,45 @@ bool good_rows(const void *t, int64_t stride, int rows, int cols, int type) {
     return ((uintptr_t)t % type_size(type)) == 0 && (rows <= 1 || (stride >= cols && stride <= INT64_MAX / 16 / rows));
 }
 
+template <int TYPE, bool NORM>
+void launch_quantize(const QArgs &a, hipStream_t s) {
+    // whole pieces of 16 bytes: bases and strides
+    const int64_t e = type_size(TYPE);
+    auto whole = [&](const void *t, int64_t stride) { return !t || ((uintptr_t)t % 16 == 0 && (a.rows == 1 || stride * e % 16 == 0)); };
+    const bool pieces = whole(a.x, a.xs) && whole(a.res, a.rs) && whole(a.sum, a.hs) && ((uintptr_t)a.gamma % 16 == 0);
+    if (!pieces || (NORM && a.Cin > 32768)) {
+        hipLaunchKernelGGL((k_quantize_row<TYPE, NORM>), dim3((unsigned)a.rows), dim3(256), 0, s, a);
+        return;
+    }
+    const int chunks = (a.Cin + 511) / 512;   // of a wave's 512 elements
+    int wpr = 1, V = 1;
+    long units;
+    if (NORM) {
+        // as few waves to a row as hold it in 64 registers each, more while they would leave CUs without work
+        while (8 * wpr < chunks) wpr *= 2;
+        while (wpr < chunks && wpr < 8 && (long)a.rows * wpr < 4096) wpr *= 2;
+        while (V * wpr < chunks) V *= 2;
+        units = a.rows;
+    } else {
+        V = (long)a.rows * chunks >= 16384 && chunks >= 4 ? 4 : 1;
+        units = (long)a.rows * ((chunks + V - 1) / V);
+    }
+    const int waves = wpr < 4 ? 4 : wpr, rpw = waves / wpr;
+    const long blocks = (units + rpw - 1) / rpw, per_xcd = (blocks + 7) / 8;
+    const dim3 grid((unsigned)(blocks < 8 ? blocks : per_xcd * 8)), block(64 * waves);
+    const int share = blocks < 8 ? 1 : (int)per_xcd;
+    if (V == 1) hipLaunchKernelGGL((k_quantize_pieces<TYPE, NORM, 1>), grid, block, 0, s, a, wpr, share);
+    if (V == 4) hipLaunchKernelGGL((k_quantize_pieces<TYPE, NORM, 4>), grid, block, 0, s, a, wpr, share);
+    if constexpr (NORM) {
+        if (V == 2) hipLaunchKernelGGL((k_quantize_pieces<TYPE, NORM, 2>), grid, block, 0, s, a, wpr, share);
+        if (V == 8) hipLaunchKernelGGL((k_quantize_pieces<TYPE, NORM, 8>), grid, block, 0, s, a, wpr, share);
+    }
+}
+
 template <int TYPE>
-void launch_quantize(const QArgs &a, bool norm, hipStream_t s) {
-    const dim3 grid((unsigned)a.rows), block(256);
-    if (norm) hipLaunchKernelGGL((k_quantize_row<TYPE, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((k_quantize_row<TYPE, false>), grid, block, 0, s, a);
+void launch_quantize_type(const QArgs &a, bool norm, hipStream_t s) {
+    if (norm) launch_quantize<TYPE, true>(a, s);
+    else launch_quantize<TYPE, false>(a, s);
 }
 
 wq_status_t run_quantize(const wq_direct_plan *plan, hipStream_t s, int type, QArgs &a, bool norm, void *workspace) {
@@ -124,9 +277,9 @@ wq_status_t run_quantize(const wq_direct_plan *plan, hipStream_t s, int type, QA
     a.sx = (float *)(ws + plan->lay.ws_sx_off);
     a.P = plan->P; a.Cin = plan->Cin; a.g = plan->g;
     if (a.rows == 0) return WQ_OK;
-    if (type == WQ_FP32) launch_quantize<WQ_FP32>(a, norm, s);
-    else if (type == WQ_BF16) launch_quantize<WQ_BF16>(a, norm, s);
-    else launch_quantize<WQ_FP16>(a, norm, s);
+    if (type == WQ_FP32) launch_quantize_type<WQ_FP32>(a, norm, s);
+    else if (type == WQ_BF16) launch_quantize_type<WQ_BF16>(a, norm, s);
+    else launch_quantize_type<WQ_FP16>(a, norm, s);
     return hipGetLastError() == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;
 }
 
