@@ -8,24 +8,9 @@
 #include <float.h>
 
 #include "wq_linear_args.h"
+#include "wq_quantize_piece.h"
 
 namespace {
-
-// ------------------------------------------------------------ element types
-template <int TYPE>
-struct Elem;
-template <>
-struct Elem<WQ_FP32> {
-    using type = float;
-};
-template <>
-struct Elem<WQ_BF16> {
-    using type = __bf16;
-};
-template <>
-struct Elem<WQ_FP16> {
-    using type = _Float16;
-};
 
 int type_size(int type) { return type == WQ_FP32 ? 4 : 2; }
 
@@ -51,36 +36,6 @@ __device__ __forceinline__ double wave_sum(double v) {
 // that the factor, rounded once to fp32, does not depend on the order of the sum, nor do the codes behind it.
 __device__ __forceinline__ float norm_factor(double squares, int Cin, double eps) {
     return (float)(1.0 / sqrt(squares / Cin + eps));
-}
-
-// The group quantizer's scale and reciprocal of a group with this largest magnitude.
-__device__ __forceinline__ void group_scale(float top, float &s, float &r) {
-    const bool live = top >= 127.0f * FLT_MIN;
-    s = live ? top / 127.0f : 0.0f;   // correctly rounded
-    r = live ? 127.0f / top : 0.0f;
-}
-
-// Eight adjacent elements (aligned to 16 bytes) as fp32, and back.
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, float (&v)[8]) {
-    typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
-#pragma unroll
-    for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
-        const vec t = ((const vec *)p)[k];
-#pragma unroll
-        for (int j = 0; j < 16 / (int)sizeof(T); ++j) v[k * 16 / sizeof(T) + j] = (float)t[j];
-    }
-}
-template <typename T>
-__device__ __forceinline__ void store8(T *p, const float (&v)[8]) {
-    typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
-#pragma unroll
-    for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
-        vec t;
-#pragma unroll
-        for (int j = 0; j < 16 / (int)sizeof(T); ++j) t[j] = (T)v[k * 16 / sizeof(T) + j];
-        ((vec *)p)[k] = t;
-    }
 }
 
 // Rows in pieces of eight elements a lane, held in registers: one pass over the data.  A group of g elements is g / 8 adjacent
@@ -151,25 +106,12 @@ __global__ __launch_bounds__(512) void k_quantize_pieces(const QArgs a, int wpr,
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         const int c = c0 + k * step;
-        uint32_t top = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[k][j]) & 0x7fffffffu);
-        top = dpp_max<0xB1>(top);   // quad_perm [1,0,3,2]
-        top = dpp_max<0x4E>(top);   // quad_perm [2,3,0,1]: the 4 lanes of 32 elements
-        if (a.g > 32) top = dpp_max<0x141>(top);   // row_half_mirror: 8 lanes
-        if (a.g > 64) top = dpp_max<0x140>(top);   // row_mirror: 16 lanes
-        if (a.g > 128) top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-        if (a.g > 256) top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        float s, r;
-        group_scale(__uint_as_float(top), s, r);
-        const uint32_t lo = quant_code(v[k][0], r) | (quant_code(v[k][1], r) << 8) | (quant_code(v[k][2], r) << 16) |
-                            (quant_code(v[k][3], r) << 24);
-        const uint32_t hi = quant_code(v[k][4], r) | (quant_code(v[k][5], r) << 8) | (quant_code(v[k][6], r) << 16) |
-                            (quant_code(v[k][7], r) << 24);
+        float s;
+        const uint2 codes = quantize_piece(v[k], a.g, s);
         if (!row || c >= a.Cin) continue;
         // planes of 8 bytes a row with groups of 32, else of 16, of which this is a half
         const size_t at = a.g == 32 ? ((size_t)(c >> 3) * a.P + p) * 8 : ((size_t)(c >> 4) * a.P + p) * 16 + (c & 8);
-        *(uint2 *)(a.xq + at) = make_uint2(lo, hi);
+        *(uint2 *)(a.xq + at) = codes;
         if ((c & (a.g - 1)) == 0) a.sx[(size_t)(c / a.g) * a.P + p] = s;
     }
 }
@@ -307,6 +249,64 @@ wq_status_t check_product(const wq_direct_plan_t *plan, int rows, const void *wo
     return WQ_OK;
 }
 
+wq_linear_args product_args(const wq_direct_plan_t *plan, int rows, const void *workspace, const void *blob, int activation,
+                            int gated, int type, const void *res, int64_t res_stride, void *y, int64_t y_stride) {
+    const char *ws = (const char *)workspace, *b = (const char *)blob;
+    wq_linear_args a = {};
+    a.xq = (const int8_t *)(ws + plan->lay.ws_xq_off);
+    a.sx = (const float *)(ws + plan->lay.ws_sx_off);
+    a.Wq = (const int8_t *)(b + plan->lay.blob_Wq_off);
+    a.sW = (const float *)(b + plan->lay.blob_sW_off);
+    a.bias = (const float *)(b + plan->lay.blob_bias_off);
+    a.res = res; a.y = y; a.rs = res_stride; a.ys = y_stride;
+    a.rows = rows; a.P = plan->P; a.Cin = plan->Cin; a.Cout_pad = plan->Cout_pad; a.log2g = ilog2(plan->g);
+    a.outs = gated ? plan->Cout / 2 : plan->Cout;
+    a.type = type; a.act = activation; a.gated = gated;
+    const int64_t piece = 4 * type_size(type);
+    auto whole = [&](const void *t, int64_t stride) { return (uintptr_t)t % piece == 0 && (rows == 1 || stride % 4 == 0); };
+    a.wide = whole(y, y_stride) && (!res || whole(res, res_stride));
+    return a;
+}
+
+// Whether the product takes the rows of x as they are: a few thousand elements, in aligned pieces, and apart from y (which
+// some workgroups write while others still read x).  Every workgroup quantizes all of x then, which costs less than a
+// launch as long as that is two pieces a wave (us, 4-bit weights, g 128, both launches and one: 1x4096->4096 7.0, 5.5;
+// 1x8192->4096 9.4, 8.3; 2x4096->4096 7.1, 6.1; 4x4096->4096 7.1, 7.5; 8x4096->4096 7.1, 10.2).
+bool quantizes_itself(const wq_linear_args &a, const void *x, int64_t xs) {
+    const int64_t e = type_size(a.type);
+    if (a.rows > 16 || a.rows * a.Cin > 8192 || (uintptr_t)x % 16 != 0 || (a.rows > 1 && xs * e % 16 != 0)) return false;
+    const char *x0 = (const char *)x, *x1 = x0 + ((a.rows - 1) * xs + a.Cin) * e;
+    const char *y0 = (const char *)a.y, *y1 = y0 + ((a.rows - 1) * a.ys + a.outs) * e;
+    return x1 <= y0 || y1 <= x0;
+}
+
+// Which kernel multiplies: over 279 drawn layers of 4 to 4096 rows, 320 to 8192 input and 32 to 16384 output channels the rules
+// below are 1.5 % (geometric mean) from the best of the forms.  With n64 and n128 the numbers of tiles of 64 (128) weight
+// rows x 64 (128) rows of x; us of the forms on either side of each line:
+//   rows: one 16-row block a workgroup up to 16 rows, else for up to 256 blocks of 16 columns x 16 rows
+//     (57x1920->1440 g 128, 360 blocks: one 6.7, two 5.5; 55x3328->800 g 32, 200: 7.7, 8.8), two beyond
+//   tiles from 33 rows and 150 tiles of 64 (75x1792->2x3808 g 256, 238: rows 10.5, tiles 8.9; 188x4928->1952 g 64, 93: 16.2, 17.3)
+//   tiles of 64: four teams share a reduction below 256 tiles (128x8192->4096 g 128: four 19.2, two 23.4, one 35.3), two
+//     below 512 (1001x2048->2040 g 256: 16.5, 13.6, 15.6), else one (1024x4096->4096 g 64: 52.5, 44.8, 42.8): CUs with
+//     eight to sixteen waves
+//   tiles of 128: long reductions from 640 of them (4096x4096->2x8192 g 128: 64 427, 128 336), where their prologue and
+//     epilogue weigh less (1740x896->10144 g 128: 47, 55); groups of up to 64 from 768, whose shorter stages
+//     leave room for more workgroups on a CU (4096x1280->2x5120 g 64: 130, 107)
+wq_status_t run_product(const wq_direct_plan *plan, const wq_linear_args &a, hipStream_t s) {
+    const int Cout = a.gated ? 2 * a.outs : a.outs;
+    auto tiles = [&](int n) { return (long)((Cout + n - 1) / n) * ((a.rows + n - 1) / n); };
+    const long n64 = tiles(64), n128 = tiles(128);
+    hipError_t e;
+    if (a.rows <= 32 || n64 <= 150) {
+        const bool one = a.rows <= 16 || (long)((a.outs + 15) / 16) * ((a.rows + 15) / 16) <= 256;
+        e = wq_launch_linear_rows(a, plan->g, plan->wbits, one ? 1 : 2, s);
+    } else {
+        const bool large = plan->g <= 64 ? n128 >= 768 : n128 >= 640 && a.Cin >= 2048;
+        e = (plan->wbits == 4 ? wq_launch_linear_tile4 : wq_launch_linear_tile8)(a, plan->g, large, n64 < 256 ? 4 : n64 < 512 ? 2 : 1, s);
+    }
+    return e == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;
+}
+
 }  // namespace
 
 // ------------------------------------------------------------------ C ABI
@@ -351,37 +351,29 @@ wq_status_t wq_linear_matmul(const wq_direct_plan_t *plan, void *stream, int row
     const wq_status_t st = check_product(plan, rows, workspace_dev, workspace_bytes, weight_blob_dev, blob_bytes,
                                          activation, gated, type, residual_dev, residual_stride, y_dev, y_stride);
     if (st != WQ_OK || rows == 0) return st;
-    const char *ws = (const char *)workspace_dev, *b = (const char *)weight_blob_dev;
-    wq_linear_args a = {};
-    a.xq = (const int8_t *)(ws + plan->lay.ws_xq_off);
-    a.sx = (const float *)(ws + plan->lay.ws_sx_off);
-    a.Wq = (const int8_t *)(b + plan->lay.blob_Wq_off);
-    a.sW = (const float *)(b + plan->lay.blob_sW_off);
-    a.bias = (const float *)(b + plan->lay.blob_bias_off);
-    a.res = residual_dev; a.y = y_dev; a.rs = residual_stride; a.ys = y_stride;
-    a.rows = rows; a.P = plan->P; a.Cin = plan->Cin; a.Cout_pad = plan->Cout_pad; a.log2g = ilog2(plan->g);
-    a.outs = gated ? plan->Cout / 2 : plan->Cout;
-    a.type = type; a.act = activation; a.gated = gated;
-    const int64_t piece = 4 * type_size(type);
-    auto whole = [&](const void *t, int64_t stride) { return (uintptr_t)t % piece == 0 && (rows == 1 || stride % 4 == 0); };
-    a.wide = whole(y_dev, y_stride) && (!residual_dev || whole(residual_dev, residual_stride));
-    hipStream_t s = (hipStream_t)stream;
-    const int n = rows > 256 ? 4 : 2;
-    const hipError_t e = plan->wbits == 4 ? wq_launch_linear_tile4(a, plan->g, n, n, s) : wq_launch_linear_tile8(a, plan->g, n, n, s);
-    return e == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;
+    wq_linear_args a = product_args(plan, rows, workspace_dev, weight_blob_dev, activation, gated, type, residual_dev,
+                                    residual_stride, y_dev, y_stride);
+    return run_product(plan, a, (hipStream_t)stream);
 }
 
 wq_status_t wq_linear_forward(const wq_direct_plan_t *plan, void *stream, int rows, int type, const void *x_dev,
                               int64_t x_stride, const void *weight_blob_dev, size_t blob_bytes, void *workspace_dev,
                               size_t workspace_bytes, int activation, int gated, const void *residual_dev,
                               int64_t residual_stride, void *y_dev, int64_t y_stride) {
-    const wq_status_t st = check_product(plan, rows, workspace_dev, workspace_bytes, weight_blob_dev, blob_bytes,
-                                         activation, gated, type, residual_dev, residual_stride, y_dev, y_stride);
+    wq_status_t st = check_product(plan, rows, workspace_dev, workspace_bytes, weight_blob_dev, blob_bytes, activation,
+                                   gated, type, residual_dev, residual_stride, y_dev, y_stride);
     if (st != WQ_OK) return st;
-    const wq_status_t sq = wq_linear_quantize(plan, stream, rows, type, x_dev, x_stride, workspace_dev, workspace_bytes);
-    if (sq != WQ_OK) return sq;
-    return wq_linear_matmul(plan, stream, rows, workspace_dev, workspace_bytes, weight_blob_dev, blob_bytes, activation,
-                            gated, type, residual_dev, residual_stride, y_dev, y_stride);
+    if ((rows != 0 && !x_dev) || !good_rows(x_dev, x_stride, rows, plan->Cin, type)) return WQ_ERR_INVALID_ARG;
+    if (rows == 0) return WQ_OK;
+    wq_linear_args a = product_args(plan, rows, workspace_dev, weight_blob_dev, activation, gated, type, residual_dev,
+                                    residual_stride, y_dev, y_stride);
+    if (quantizes_itself(a, x_dev, x_stride)) {
+        a.x = x_dev; a.xs = x_stride;
+    } else {
+        st = wq_linear_quantize(plan, stream, rows, type, x_dev, x_stride, workspace_dev, workspace_bytes);
+        if (st != WQ_OK) return st;
+    }
+    return run_product(plan, a, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -2,6 +2,8 @@
 // group scales, in workgroup tiles whose operands are staged in LDS.
 #pragma once
 
+#include <type_traits>
+
 #include "wq_linear_args.h"
 
 namespace {
@@ -10,25 +12,34 @@ __device__ __forceinline__ void lds_load4(__amdgpu_buffer_rsrc_t r, char *lds, u
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, WQ_LDS_PTR(lds), 4, voff, soff, 0, 0);
 }
 
+// Until at most VM of the wave's loads are outstanding (they complete in order) and its LDS reads are done, then the
+// workgroup's barrier.
+template <int VM>
+__device__ __forceinline__ void wait_and_barrier() {
+    static_assert(VM >= 0 && VM < 64, "vmcnt is a 6-bit counter");
+    asm volatile("s_waitcnt %0\n\ts_barrier" ::"n"(0x0070 | (VM & 0xf) | ((VM >> 4) << 14)) : "memory");
+}
+
 struct wq_tile_grid {
     int nO, nP, total, per_xcd;   // workgroup tiles along weight rows and rows of x, their number, the share of each XCD
 };
 
 // GS: the group size, 256 standing for 256 and 512.  Four waves, 2 along weight rows x 2 along rows of x, each with NO x NB
-// 16 x 16 blocks.  A stage is 128 bytes of K: the operand blocks, in the MFMA's order in memory already, go straight
-// into LDS with the scales of the groups that the stage meets; two stages take turns.
-template <int GS, bool W4, int NO, int NB>
-__global__ __launch_bounds__(256, 2) void k_linear_tile(const wq_linear_args a, const wq_tile_grid t) {
+// 16 x 16 blocks; KS such teams share a tile's reduction, each a contiguous part of K.  A stage is SK bytes of K: the
+// operand blocks, in the MFMA's order in memory already, go straight into LDS with the scales of the groups that the
+// stage meets, into a ring of NST stages per team, NST - 1 of them in flight.
+template <int GS, bool W4, int NO, int NB, int SK, int NST, int KS>
+__global__ __launch_bounds__(256 * KS, 2) void k_linear_tile(const wq_linear_args a, const wq_tile_grid t) {
     constexpr bool K64 = GS != 32;
-    constexpr int KSTEP = K64 ? 64 : 32, NK = 128 / KSTEP;
-    constexpr int WB = W4 ? 1024 : 2048, XB = 2048;       // bytes of a 16-row block in a stage
+    constexpr int KSTEP = K64 ? 64 : 32, NK = SK / KSTEP;
+    constexpr int WB = 16 * SK / (W4 ? 2 : 1), XB = 16 * SK;   // bytes of a 16-row block in a stage
     constexpr int OB = 2 * NO, PB = 2 * NB;               // blocks of the workgroup tile
-    constexpr int NGS = GS >= 128 ? 1 : 128 / GS;         // groups that a stage meets
+    constexpr int NGS = GS >= SK ? 1 : SK / GS;           // groups that a stage meets
     constexpr int WOFF = 0, XOFF = OB * WB, SWOFF = XOFF + PB * XB, SXOFF = SWOFF + NGS * OB * 64, STAGE = SXOFF + NGS * PB * 64;
-    __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
+    __shared__ __attribute__((aligned(16))) char lds[KS * NST * STAGE];
 
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, q = lane >> 4;
-    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wo = w & 1, wp = w >> 1;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), w = wave & 3, team = wave >> 2, wo = w & 1, wp = w >> 1;
     // workgroup ids go round-robin over the XCDs: each takes a contiguous share of the tile order, in which 8 tiles
     // of rows share their weights' tile before the next follows
     const int logical = (int)(blockIdx.x & 7u) * t.per_xcd + (int)(blockIdx.x >> 3);
@@ -36,7 +47,10 @@ __global__ __launch_bounds__(256, 2) void k_linear_tile(const wq_linear_args a, 
     const int band = logical / (8 * t.nO), in_band = logical - band * 8 * t.nO, high = min(8, t.nP - band * 8);
     const int po = in_band / high, pp = band * 8 + in_band % high;
     const int p0 = pp * PB * 16, last_row = a.rows - 1;
-    const int groups = a.Cin >> a.log2g, NS = (a.Cin + 127) / 128;
+    const int groups = a.Cin >> a.log2g;
+    // the team's stages: whole groups
+    const int spu = GS > SK ? (1 << a.log2g) / SK : 1, units = (a.Cin + SK - 1) / SK / spu;
+    const int s_beg = team * units / KS * spu, s_end = (team + 1) * units / KS * spu, rounds = (units + KS - 1) / KS * spu;
 
     // the weight block of block j of the tile.  Gated: the first half of a wave's blocks are the gate's, the second the
     // same channels of what it multiplies
@@ -62,20 +76,21 @@ __global__ __launch_bounds__(256, 2) void k_linear_tile(const wq_linear_args a, 
     // Rows and channels past the end read the last one again (not stored).  K past the end (half of a last stage, groups of
     // 32 and 64) brings codes of whatever lies there, or nothing behind a tensor's end: finite sums, whose scales are taken
     // as zero.  Scalar offsets never pass a tensor's size, which the range check subtracts them from.
-    constexpr int LW = OB * (WB / 1024) / 4, LX = PB * 2 / 4;   // 1 KiB loads of a wave and stage
-    static_assert(LW * 4 == OB * (WB / 1024) && LX * 4 == PB * 2, "four waves share the loads evenly");
+    constexpr int LW = OB * WB / 4096, LX = PB * XB / 4096;   // 1 KiB loads of a wave and stage
+    static_assert(LW * 4096 == OB * WB && LX * 4096 == PB * XB, "four waves share the loads evenly");
+    constexpr int SPAN = 1024 / (16 * KSTEP);                 // K-steps that a load of x brings
+    const unsigned run = (16u * (unsigned)a.Cin) >> (W4 ? 1 : 0);   // bytes of a weight block: all of K
     unsigned vW[LW], vX[LX];
-    int kW[LW], kX[LX];   // which K-steps of the stage a load brings
+    int kX[LX];   // which K-steps of the stage a load brings
 #pragma unroll
     for (int u = 0; u < LW; ++u) {
-        const int i = w * LW + u;
-        kW[u] = W4 ? 0 : i % 2 * (NK / 2);
-        vW[u] = (unsigned)lane * 16u + (((unsigned)block_of(W4 ? i : i / 2) * 16u * (unsigned)a.Cin) >> (W4 ? 1 : 0));
+        const int byte = (w * LW + u) * 1024 + lane * 16;
+        vW[u] = (unsigned)block_of(byte / WB) * run + (unsigned)(byte % WB);
     }
 #pragma unroll
     for (int u = 0; u < LX; ++u) {
-        const int i = w * LX + u, row0 = p0 + i / 2 * 16;
-        kX[u] = i % 2 * (NK / 2);
+        const int i = w * LX + u, row0 = p0 + i * 1024 / XB * 16;
+        kX[u] = i * 1024 % XB / 1024 * SPAN;
         if constexpr (K64) {
             vX[u] = ((unsigned)q * (unsigned)a.P + (unsigned)min(row0 + l16, last_row)) * 16u;
         } else {   // lanes 0-31 and 32-63: a K-step each, its quarters of 16 rows in pairs
@@ -89,19 +104,17 @@ __global__ __launch_bounds__(256, 2) void k_linear_tile(const wq_linear_args a, 
     unsigned vS[LS];
 #pragma unroll
     for (int u = 0; u < LS; ++u) {
-        const int i = w + u * 4, k = i % (QW + QX);
+        const int i = (w + u * 4) % NL, k = i % (QW + QX);
         vS[u] = k < QW ? (unsigned)block_of(k * 4 + q) * 64u + (unsigned)l16 * 4u
                        : (unsigned)min(p0 + (k - QW) * 64 + lane, last_row) * 4u;
     }
     const int steps = a.Cin / KSTEP;
     const unsigned stepX = 4u * (unsigned)a.P * (KSTEP / 4);
-    auto issue = [&](int s, int buf) {
-        char *base = lds + buf * STAGE;
+    auto issue = [&](int s, int slot) {
+        char *base = lds + (team * NST + slot) * STAGE;
 #pragma unroll
-        for (int u = 0; u < LW; ++u) {
-            const int k = min(s * NK + kW[u], steps);
-            lds_load16(rW, base + WOFF + (w * LW + u) * 1024, vW[u], ((unsigned)k * 16u * KSTEP) >> (W4 ? 1 : 0));
-        }
+        for (int u = 0; u < LW; ++u)
+            lds_load16(rW, base + WOFF + (w * LW + u) * 1024, vW[u], min((unsigned)s * WB, run));
 #pragma unroll
         for (int u = 0; u < LX; ++u) {
             const int k = min(s * NK + kX[u], steps);
@@ -109,9 +122,8 @@ __global__ __launch_bounds__(256, 2) void k_linear_tile(const wq_linear_args a, 
         }
 #pragma unroll
         for (int u = 0; u < LS; ++u) {
-            const int i = w + u * 4, k = i % (QW + QX), gl = i / (QW + QX);
-            if (NL % 4 != 0 && i >= NL) break;
-            const int gi = min(GS >= 256 ? (s * 128) >> a.log2g : s * NGS + gl, groups - 1);
+            const int i = (w + u * 4) % NL, k = i % (QW + QX), gl = i / (QW + QX);   // (a wave without one of its own repeats another's)
+            const int gi = min(GS > SK ? (s * SK) >> a.log2g : s * NGS + gl, groups - 1);
             if (k < QW)
                 lds_load4(rSW, base + SWOFF + gl * OB * 64 + k * 256, vS[u], (unsigned)gi * (unsigned)a.Cout_pad * 4u);
             else
@@ -131,64 +143,76 @@ __global__ __launch_bounds__(256, 2) void k_linear_tile(const wq_linear_args a, 
     constexpr bool MAGIC = GS < 256;
     constexpr int start = W4 ? kMagic16 : kMagic;
 
-    auto compute = [&](int s, int buf) {
-        const char *base = lds + buf * STAGE;
-        v4i bv[NK][NB];
+    // A stage's operands of x and their scales, in registers; the weights' are read as their turn comes.
+    struct Operands {
+        v4i x[NK][NB];
         float sx[NGS][NB];
+    };
+    auto piece = [&](const char *p, auto bytes) {
+        v4i v = {0, 0, 0, 0};
+        if constexpr (bytes == 16) v = *(const v4i *)p;
+        else if constexpr (bytes == 8) {
+            const v2i b = *(const v2i *)p;
+            v.x = b.x; v.y = b.y;
+        } else {
+            v.x = *(const int *)p;
+        }
+        return v;
+    };
+    constexpr int KB = KSTEP / 4, WKB = W4 ? KB / 2 : KB;   // bytes a lane holds of a K-step
+    auto read_w = [&](const char *base, int e, int k) {
+        return piece(base + WOFF + (wo * NO + e) * WB + (k * 64 + lane) * WKB, std::integral_constant<int, WKB>{});
+    };
+    auto read_sw = [&](const char *base, int e, int k) { return *(const v4f *)(base + SWOFF + k * OB * 64 + (wo * NO + e) * 64 + q * 16); };
+    auto read = [&](int s, int slot, Operands &op) {
+        const char *base = lds + (team * NST + slot) * STAGE;
 #pragma unroll
         for (int k = 0; k < NK; ++k)
 #pragma unroll
-            for (int f = 0; f < NB; ++f) {
-                const char *p = base + XOFF + (wp * NB + f) * XB + (k * 64 + lane) * (KSTEP / 4);
-                if constexpr (K64) bv[k][f] = *(const v4i *)p;
-                else {
-                    const v2i b = *(const v2i *)p;
-                    bv[k][f] = v4i{b.x, b.y, 0, 0};
-                }
-            }
-        const bool done = GS < 256 || ((s + 1) * 128 & ((1 << a.log2g) - 1)) == 0;   // a group ends with this stage
+            for (int f = 0; f < NB; ++f)
+                op.x[k][f] = piece(base + XOFF + (wp * NB + f) * XB + (k * 64 + lane) * KB, std::integral_constant<int, KB>{});
 #pragma unroll
         for (int k = 0; k < NGS; ++k)
 #pragma unroll
             for (int f = 0; f < NB; ++f) {
                 const float v = *(const float *)(base + SXOFF + k * PB * 64 + (wp * NB + f) * 64 + l16 * 4);
-                sx[k][f] = GS >= 128 || s * NGS + k < groups ? v : 0.f;
+                op.sx[k][f] = GS >= SK || s * NGS + k < groups ? v : 0.f;
             }
+    };
+
+    auto compute = [&](int s, int slot, const Operands &op) {
+        const char *base = lds + (team * NST + slot) * STAGE;
+        const bool done = GS <= SK || ((s + 1) * SK & ((1 << a.log2g) - 1)) == 0;   // a group ends with this stage
 #pragma unroll
         for (int e = 0; e < NO; ++e) {
             v4i av[NK];
 #pragma unroll
             for (int k = 0; k < NK; ++k) {
-                const char *p = base + WOFF + (wo * NO + e) * WB + ((k * 64 + lane) * (KSTEP / 4) >> (W4 ? 1 : 0));
-                if constexpr (!W4) {
-                    if constexpr (K64) av[k] = *(const v4i *)p;
-                    else {
-                        const v2i b = *(const v2i *)p;
-                        av[k] = v4i{b.x, b.y, 0, 0};
-                    }
-                } else {
-                    const unsigned a0 = ((const unsigned *)p)[0], a1 = K64 ? ((const unsigned *)p)[1] : 0u;
+                av[k] = read_w(base, e, k);
+                if constexpr (W4) {
+                    const unsigned a0 = (unsigned)av[k].x, a1 = (unsigned)av[k].y;
                     av[k] = v4i{(int)((a0 << 4) & 0xf0f0f0f0u), (int)(a0 & 0xf0f0f0f0u), (int)((a1 << 4) & 0xf0f0f0f0u),
                                 (int)(a1 & 0xf0f0f0f0u)};
                 }
             }
             auto mfma = [&](int k, int f, v4i c) {
-                if constexpr (K64) return __builtin_amdgcn_mfma_i32_16x16x64_i8(av[k], bv[k][f], c, 0, 0, 0);
+                const v4i b = op.x[k][f];
+                if constexpr (K64) return __builtin_amdgcn_mfma_i32_16x16x64_i8(av[k], b, c, 0, 0, 0);
                 else
                     return __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, v2i{av[k].x, av[k].y}),
-                                                                 __builtin_bit_cast(long, v2i{bv[k][f].x, bv[k][f].y}), c, 0, 0, 0);
+                                                                 __builtin_bit_cast(long, v2i{b.x, b.y}), c, 0, 0, 0);
             };
             auto dequant = [&](int k, v4i (&P)[NB]) {
-                v4f sw = *(const v4f *)(base + SWOFF + k * OB * 64 + (wo * NO + e) * 64 + q * 16);
+                v4f sw = read_sw(base, e, k);
                 if constexpr (W4 && !MAGIC) sw *= 0.0625f;
 #pragma unroll
                 for (int f = 0; f < NB; ++f)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        M[e][f][r] = __builtin_fmaf(group_sum<MAGIC, W4>(P[f][r]), sw[r] * sx[k][f], M[e][f][r]);
+                        M[e][f][r] = __builtin_fmaf(group_sum<MAGIC, W4>(P[f][r]), sw[r] * op.sx[k][f], M[e][f][r]);
             };
             const v4i magic = {start, start, start, start};
-            if constexpr (GS <= 64) {
+            if constexpr (GS == KSTEP) {
 #pragma unroll
                 for (int k = 0; k < NK; ++k) {
                     v4i P[NB];
@@ -217,41 +241,73 @@ __global__ __launch_bounds__(256, 2) void k_linear_tile(const wq_linear_args a, 
         }
     };
 
-    issue(0, 0);
-    for (int s = 0; s < NS; ++s) {
-        // the stage's loads have landed, every wave's, and the other buffer has been read by all
-        wait_loads<0>();
-        __syncthreads();
-        if (s + 1 < NS) issue(s + 1, (s + 1) & 1);
-        compute(s, s & 1);
+    constexpr int LPS = LW + LX + LS;   // a wave's loads of a stage
+#pragma unroll
+    for (int d = 0; d < NST - 1; ++d)
+        if (s_beg + d < s_end) issue(s_beg + d, d);
+    int slot = 0;
+    for (int n = 0; n < rounds; ++n) {
+        const int s = s_beg + n;
+        // the stage's loads have landed, every wave's, and the slot of the stage before has been read by all
+        if (NST > 2 && s + NST - 1 <= s_end) wait_and_barrier<(NST - 2) * LPS>();
+        else wait_and_barrier<0>();
+        if (s + NST - 1 < s_end) issue(s + NST - 1, slot == 0 ? NST - 1 : slot - 1);
+        if (s < s_end) {
+            Operands op;
+            read(s, slot, op);
+            compute(s, slot, op);
+        }
+        slot = slot == NST - 1 ? 0 : slot + 1;
     }
 
     // ---- epilogue ----
     // Through LDS, FB row blocks of a wave at a time: its 64 lanes then hold whole runs of columns of a row, and the code of the
     // activations is there once, not once per register of M.
-    constexpr int RS = 16 * NO + 4, FB = NB % 2 == 0 && 4 * 32 * RS * 4 <= 2 * STAGE ? 2 : 1;
-    static_assert(4 * FB * 16 * RS * 4 <= 2 * STAGE, "the waves' rows fit the stages' memory");
-    float *mine = (float *)lds + w * (FB * 16 * RS);
+    constexpr int RS = 16 * NO + 4, FB = NB % 2 == 0 && 4 * 32 * RS * 4 <= NST * STAGE ? 2 : 1, PART = FB * 16 * RS;
+    static_assert(4 * PART * 4 <= NST * STAGE, "the waves' rows fit the stages' memory");
+    float *mine = (float *)lds + wave * PART;
+    // a lane keeps its four columns from row to row: their bias is in registers, the next row's residual under way
     const int quads = a.gated ? 2 * NO : 4 * NO, shift = a.gated ? __builtin_ctz(2 * NO) : __builtin_ctz(4 * NO);
-    const int col0 = (po * 2 + wo) * quads * 4;
+    const int c = (lane & (quads - 1)) * 4, o = (po * 2 + wo) * quads * 4 + c;
+    const int items = o < a.outs ? FB * 16 << shift : 0, row_step = (64 * KS) >> shift;
+    v4f bias = {}, bias_up = {};
+    if (o < a.outs) {   // (the bias is padded as the weights are)
+        bias = *(const v4f *)(a.bias + o);
+        if (a.gated) bias_up = *(const v4f *)(a.bias + a.outs + o);
+    }
     __syncthreads();   // the last stage has been read by all
 #pragma unroll
     for (int f0 = 0; f0 < NB; f0 += FB) {
+        if (KS > 1 && f0) __syncthreads();   // the rows before have been read by all teams
 #pragma unroll
         for (int f = 0; f < FB; ++f)
 #pragma unroll
             for (int e = 0; e < NO; ++e) *(v4f *)&mine[(16 * f + l16) * RS + 16 * e + 4 * q] = M[e][f0 + f];
-        __builtin_amdgcn_wave_barrier();
+        if (KS > 1) __syncthreads();
+        else __builtin_amdgcn_wave_barrier();
+        int row = (team * 64 + lane) >> shift, p = p0 + (wp * NB + f0) * 16 + row;   // (the teams share the rows)
+        v4f res = items && p < a.rows ? residual_of(a, p, o) : v4f{};
 #pragma unroll 1
-        for (int i = lane; i < FB * 16 << shift; i += 64) {
-            const int row = i >> shift, c = (i & (quads - 1)) * 4;
-            finish_columns(a, p0 + (wp * NB + f0) * 16 + row, col0 + c, &mine[row * RS + c], 8 * NO);
+        for (int i = team * 64 + lane; i < items; i += 64 * KS) {
+            if (p >= a.rows) break;
+            const v4f next = i + 64 * KS < items && p + row_step < a.rows ? residual_of(a, p + row_step, o) : v4f{};
+            const float *sums = (const float *)lds + w * PART + row * RS + c;
+            v4f z = bias + *(const v4f *)sums, up = a.gated ? bias_up + *(const v4f *)(sums + 8 * NO) : v4f{};
+#pragma unroll
+            for (int k = 1; k < KS; ++k) {
+                z += *(const v4f *)(sums + 4 * k * PART);
+                if (a.gated) up += *(const v4f *)(sums + 4 * k * PART + 8 * NO);
+            }
+            finish_columns(a, p, o, z, up, res);
+            res = next;
+            row += row_step;
+            p += row_step;
         }
         __builtin_amdgcn_wave_barrier();
     }
 }
 
-template <int GS, bool W4, int NO, int NB>
+template <int GS, bool W4, int NO, int NB, int SK, int NST, int KS>
 hipError_t launch_tile(const wq_linear_args &a, hipStream_t s) {
     wq_tile_grid t;
     const int cols = a.gated ? 16 * NO : 32 * NO;   // columns of y in a tile
@@ -259,8 +315,17 @@ hipError_t launch_tile(const wq_linear_args &a, hipStream_t s) {
     t.nP = (a.rows + 32 * NB - 1) / (32 * NB);
     t.total = t.nO * t.nP;
     t.per_xcd = (t.total + 7) / 8;
-    hipLaunchKernelGGL((k_linear_tile<GS, W4, NO, NB>), dim3((unsigned)t.per_xcd * 8u), dim3(256), 0, s, a, t);
+    hipLaunchKernelGGL((k_linear_tile<GS, W4, NO, NB, SK, NST, KS>), dim3((unsigned)t.per_xcd * 8u), dim3(256 * KS), 0, s, a, t);
     return hipGetLastError();
+}
+
+// Tiles of 128 x 128.  Groups of up to 64 take stages of one group of 64 (two of 32): fewer registers and less LDS, so that
+// three or four workgroups share a CU where two would (4096x1280->2x5120 g 64, 8-bit: 107 us, 124 with stages of 128;
+// 4-bit, whose stages are small enough for a third of them: 101.5, in two 107.8).
+template <int GS, bool W4>
+hipError_t launch_large(const wq_linear_args &a, hipStream_t s) {
+    if constexpr (GS <= 64) return launch_tile<GS, W4, 4, 4, 64, W4 ? 3 : 2, 1>(a, s);
+    else return launch_tile<GS, W4, 4, 4, 128, 2, 1>(a, s);
 }
 
 }  // namespace
