@@ -286,12 +286,12 @@ bool quantizes_itself(const wq_linear_args &a, const void *x, int64_t xs) {
 //   rows: one 16-row block a workgroup up to 16 rows, else for up to 256 blocks of 16 columns x 16 rows
 //     (57x1920->1440 g 128, 360 blocks: one 6.7, two 5.5; 55x3328->800 g 32, 200: 7.7, 8.8), two beyond
 //   tiles from 33 rows and 150 tiles of 64 (75x1792->2x3808 g 256, 238: rows 10.5, tiles 8.9; 188x4928->1952 g 64, 93: 16.2, 17.3)
-//   tiles of 64: four teams share a reduction below 256 tiles (128x8192->4096 g 128: four 19.2, two 23.4, one 35.3), two
-//     below 512 (1001x2048->2040 g 256: 16.5, 13.6, 15.6), else one (1024x4096->4096 g 64: 52.5, 44.8, 42.8): CUs with
+//   tiles of 64: four teams share a reduction up to 256 tiles (128x8192->4096 g 128: four 19.2, two 23.4, one 35.3), two
+//     up to 512 (1001x2048->2040 g 256: 16.5, 13.6, 15.6), else one (1024x4096->4096 g 64: 52.5, 44.8, 42.8): CUs with
 //     eight to sixteen waves
-//   tiles of 128: long reductions from 640 of them (4096x4096->2x8192 g 128: 64 427, 128 336), where their prologue and
-//     epilogue weigh less (1740x896->10144 g 128: 47, 55); groups of up to 64 from 768, whose shorter stages
-//     leave room for more workgroups on a CU (4096x1280->2x5120 g 64: 130, 107)
+//   tiles of 128: long reductions from 400 of them (4096x4096->2x8192 g 128: 64 427, 128 336; 512x4096->2x8192: 59.7, 51.3), where
+//     their prologue and epilogue weigh less (1740x896->10144 g 128: 47, 55); groups of up to 64 from 640, whose
+//     shorter stages leave room for more workgroups on a CU (4096x1280->2x5120 g 64: 130, 107)
 wq_status_t run_product(const wq_direct_plan *plan, const wq_linear_args &a, hipStream_t s) {
     const int Cout = a.gated ? 2 * a.outs : a.outs;
     auto tiles = [&](int n) { return (long)((Cout + n - 1) / n) * ((a.rows + n - 1) / n); };
@@ -301,8 +301,8 @@ wq_status_t run_product(const wq_direct_plan *plan, const wq_linear_args &a, hip
         const bool one = a.rows <= 16 || (long)((a.outs + 15) / 16) * ((a.rows + 15) / 16) <= 256;
         e = wq_launch_linear_rows(a, plan->g, plan->wbits, one ? 1 : 2, s);
     } else {
-        const bool large = plan->g <= 64 ? n128 >= 768 : n128 >= 640 && a.Cin >= 2048;
-        e = (plan->wbits == 4 ? wq_launch_linear_tile4 : wq_launch_linear_tile8)(a, plan->g, large, n64 < 256 ? 4 : n64 < 512 ? 2 : 1, s);
+        const bool large = plan->g <= 64 ? n128 >= 640 : n128 >= 400 && a.Cin >= 2048;
+        e = (plan->wbits == 4 ? wq_launch_linear_tile4 : wq_launch_linear_tile8)(a, plan->g, large, n64 <= 256 ? 4 : n64 <= 512 ? 2 : 1, s);
     }
     return e == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;
 }

@@ -510,54 +510,67 @@ class LinearPlan(DirectPlan):
     around it: the root-mean-square norm with the residual's addition in front of it, bias, activation,
     gate and residual behind it.  x, residual and outputs are [n][columns] tensors of one float type
     (fp32, bf16, fp16) with adjacent columns and any row stride, n <= rows; blob and workspace are
-    DirectPlan's.  All tensors are on the device of the stream, which is the current one."""
+    DirectPlan's.  All tensors are on the current device, which is the stream's."""
 
     def __init__(self, rows, Cin, Cout, group_size, weight_bits: int = 8):
+        import torch
         super().__init__(rows, 1, 1, Cin, Cout, group_size, linear=True, weight_bits=weight_bits)
-        L = self.layout
-        self._rows, self._cin, self._cout = L.P, L.Cin, L.Cout
-        self._blob_bytes, self._ws_bytes = L.blob_bytes, L.ws_bytes
+        self._rows, self._cin, self._cout = self.layout.P, self.layout.Cin, self.layout.Cout
+        # a decoding step makes hundreds of these calls: what they look up is looked up once
+        self._tensor_type, self._uint8, self._cuda = torch.Tensor, torch.uint8, torch.cuda
+        self._types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._lib = lib()
 
-    def _buffer(self, t, need, what):
-        """Address of a workspace or blob on the current device."""
-        import torch
-        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous():
+    def _stream(self, stream, device):
+        """The stream's handle; the call's tensors have to be on the current device."""
+        if device != self._cuda.current_device():
+            raise ValueError("expected tensors on the current device")
+        if stream is None and self._raw_stream is not None:
+            return self._raw_stream(device)
+        return _stream_handle(stream)
+
+    def _buffer(self, t, device, what):
+        """Address and size of a workspace or blob."""
+        if not isinstance(t, self._tensor_type) or not t.is_cuda or t.dtype != self._uint8 or not t.is_contiguous():
             raise TypeError(f"{what}: expected a contiguous uint8 device tensor")
-        if t.get_device() != torch.cuda.current_device():
-            raise ValueError(f"{what}: expected a tensor on the current device")
-        return t.data_ptr()
+        if t.get_device() != device:
+            raise ValueError(f"{what}: expected a tensor on the device of the others")
+        return t.data_ptr(), t.numel()
 
-    @staticmethod
-    def _tensor(t, like, cols, what):
-        """(address, row stride) of a [n][cols] tensor; `like`: the call's first tensor, whose type, device and rows it shares."""
-        import torch
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    def _first(self, t, cols, what):
+        """(rows, dtype, its code, device, address, row stride) of a call's first tensor."""
+        if not isinstance(t, self._tensor_type) or not t.is_cuda:
             raise TypeError(f"{what}: expected a device tensor")
-        if t.dtype != like.dtype:
-            raise TypeError(f"{what}: expected {like.dtype}")
-        if t.dim() != 2 or t.shape[1] != cols or t.shape[0] != like.shape[0]:
-            raise ValueError(f"{what}: expected shape [{like.shape[0]}][{cols}], got {tuple(t.shape)}")
-        if t.stride(1) != 1:
-            raise ValueError(f"{what}: expected adjacent columns")
-        if t.get_device() != like.get_device():
-            raise ValueError(f"{what}: expected a tensor on the same device")
-        return t.data_ptr(), t.stride(0)
-
-    def _first(self, t, cols, ws, what):
-        """(rows, type, address, row stride) of a call's first tensor."""
-        import torch
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise TypeError(f"{what}: expected a device tensor")
-        code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t.dtype)
+        dtype = t.dtype
+        code = self._types.get(dtype)
         if code is None:
             raise TypeError(f"{what}: expected fp32, bf16 or fp16")
-        if t.dim() != 2 or t.shape[1] != cols or t.shape[0] > self._rows:
-            raise ValueError(f"{what}: expected shape [up to {self._rows}][{cols}], got {tuple(t.shape)}")
-        if t.stride(1) != 1:
+        shape = t.shape
+        if len(shape) != 2 or shape[1] != cols or shape[0] > self._rows:
+            raise ValueError(f"{what}: expected shape [up to {self._rows}][{cols}], got {tuple(shape)}")
+        stride = t.stride()
+        if stride[1] != 1 and cols > 1:
             raise ValueError(f"{what}: expected adjacent columns")
-        if t.get_device() != ws.get_device():
-            raise ValueError(f"{what}: expected a tensor on the workspace's device")
-        return t.shape[0], code, t.data_ptr(), t.stride(0)
+        return shape[0], dtype, code, t.get_device(), t.data_ptr(), stride[0]
+
+    def _other(self, t, rows, cols, dtype, device, what):
+        """(address, row stride) of a [rows][cols] tensor like the first one; (None, 0) of None."""
+        if t is None:
+            return None, 0
+        if not isinstance(t, self._tensor_type) or not t.is_cuda:
+            raise TypeError(f"{what}: expected a device tensor")
+        if t.dtype != dtype:
+            raise TypeError(f"{what}: expected {dtype}")
+        shape = t.shape
+        if len(shape) != 2 or shape[0] != rows or shape[1] != cols:
+            raise ValueError(f"{what}: expected shape [{rows}][{cols}], got {tuple(shape)}")
+        stride = t.stride()
+        if stride[1] != 1 and cols > 1:
+            raise ValueError(f"{what}: expected adjacent columns")
+        if t.get_device() != device:
+            raise ValueError(f"{what}: expected a tensor on the device of the others")
+        return t.data_ptr(), stride[0]
 
     def _epilogue(self, activation, gated):
         act = ACTIVATIONS.get(activation)
@@ -568,40 +581,46 @@ class LinearPlan(DirectPlan):
     def rms_norm_quantize(self, x, ws, residual=None, gamma=None, eps=1e-6, out=None, stream=None):
         """Codes and scales of (x + residual) / rms(x + residual) * gamma into the workspace; `out` (may be
         x or residual itself) gets x + residual.  gamma: fp32 [Cin]."""
-        import torch
-        wp = self._buffer(ws, self._ws_bytes, "workspace")
-        n, code, xp, xs = self._first(x, self._cin, ws, "x")
-        rp, rs = (None, 0) if residual is None else self._tensor(residual, x, self._cin, "residual")
-        op, os_ = (None, 0) if out is None else self._tensor(out, x, self._cin, "out")
-        gp = None if gamma is None else _dev_ptr(gamma, torch.float32, "gamma", self._cin)
-        if gamma is not None and gamma.get_device() != ws.get_device():
-            raise ValueError("gamma: expected a tensor on the workspace's device")
-        _check(lib().wq_rms_norm_quantize(self._h, _stream_handle(stream), n, code, xp, xs, rp, rs, gp, float(eps), op,
-                                          os_, wp, ws.numel()), "wq_rms_norm_quantize")
+        cin = self._cin
+        n, dtype, code, dev, xp, xs = self._first(x, cin, "x")
+        rp, rs = self._other(residual, n, cin, dtype, dev, "residual")
+        op, os_ = self._other(out, n, cin, dtype, dev, "out")
+        wp, wn = self._buffer(ws, dev, "workspace")
+        gp = None
+        if gamma is not None:
+            import torch
+            gp = _dev_ptr(gamma, torch.float32, "gamma", cin)
+            if gamma.get_device() != dev:
+                raise ValueError("gamma: expected a tensor on the device of the others")
+        _check(self._lib.wq_rms_norm_quantize(self._h, self._stream(stream, dev), n, code, xp, xs, rp, rs, gp, eps, op, os_, wp,
+                                              wn), "wq_rms_norm_quantize")
 
     def quantize_rows(self, x, ws, stream=None):
         """Codes and scales of x into the workspace."""
-        wp = self._buffer(ws, self._ws_bytes, "workspace")
-        n, code, xp, xs = self._first(x, self._cin, ws, "x")
-        _check(lib().wq_linear_quantize(self._h, _stream_handle(stream), n, code, xp, xs, wp, ws.numel()),
-               "wq_linear_quantize")
+        n, _, code, dev, xp, xs = self._first(x, self._cin, "x")
+        wp, wn = self._buffer(ws, dev, "workspace")
+        _check(self._lib.wq_linear_quantize(self._h, self._stream(stream, dev), n, code, xp, xs, wp, wn), "wq_linear_quantize")
 
     def matmul(self, ws, blob, y, activation="none", gated=False, residual=None, stream=None):
         """y = act(z) + residual, or act(gate) * up + residual, z the product of the workspace's first
         len(y) rows with the weights, plus bias."""
         act, outs = self._epilogue(activation, gated)
-        wp, bp = self._buffer(ws, self._ws_bytes, "workspace"), self._buffer(blob, self._blob_bytes, "blob")
-        n, code, yp, ys = self._first(y, outs, ws, "y")
-        rp, rs = (None, 0) if residual is None else self._tensor(residual, y, outs, "residual")
-        _check(lib().wq_linear_matmul(self._h, _stream_handle(stream), n, wp, ws.numel(), bp, blob.numel(), act,
-                                      1 if gated else 0, code, rp, rs, yp, ys), "wq_linear_matmul")
+        n, dtype, code, dev, yp, ys = self._first(y, outs, "y")
+        rp, rs = self._other(residual, n, outs, dtype, dev, "residual")
+        wp, wn = self._buffer(ws, dev, "workspace")
+        bp, bn = self._buffer(blob, dev, "blob")
+        _check(self._lib.wq_linear_matmul(self._h, self._stream(stream, dev), n, wp, wn, bp, bn, act, 1 if gated else 0, code, rp,
+                                          rs, yp, ys), "wq_linear_matmul")
 
     def linear(self, x, blob, ws, y, activation="none", gated=False, residual=None, stream=None):
-        """quantize_rows followed by matmul."""
+        """quantize_rows followed by matmul; what the workspace holds afterwards is unspecified."""
         act, outs = self._epilogue(activation, gated)
-        wp, bp = self._buffer(ws, self._ws_bytes, "workspace"), self._buffer(blob, self._blob_bytes, "blob")
-        n, code, xp, xs = self._first(x, self._cin, ws, "x")
-        yp, ys = self._tensor(y, x, outs, "y")
-        rp, rs = (None, 0) if residual is None else self._tensor(residual, x, outs, "residual")
-        _check(lib().wq_linear_forward(self._h, _stream_handle(stream), n, code, xp, xs, bp, blob.numel(), wp, ws.numel(),
-                                       act, 1 if gated else 0, rp, rs, yp, ys), "wq_linear_forward")
+        n, dtype, code, dev, xp, xs = self._first(x, self._cin, "x")
+        if y is None:
+            raise TypeError("y: expected a device tensor")
+        yp, ys = self._other(y, n, outs, dtype, dev, "y")
+        rp, rs = self._other(residual, n, outs, dtype, dev, "residual")
+        wp, wn = self._buffer(ws, dev, "workspace")
+        bp, bn = self._buffer(blob, dev, "blob")
+        _check(self._lib.wq_linear_forward(self._h, self._stream(stream, dev), n, code, xp, xs, bp, bn, wp, wn, act,
+                                           1 if gated else 0, rp, rs, yp, ys), "wq_linear_forward")
