@@ -29,7 +29,7 @@ struct wq_tile_grid {
 // operand blocks, in the MFMA's order in memory already, go straight into LDS with the scales of the groups that the
 // stage meets, into a ring of NST stages per team, NST - 1 of them in flight.
 template <int GS, bool W4, int NO, int NB, int SK, int NST, int KS>
-__global__ __launch_bounds__(256 * KS, 2) void k_linear_tile(const wq_linear_args a, const wq_tile_grid t) {
+__global__ __launch_bounds__(256 * KS, NO == 4 && SK == 64 ? (W4 ? 3 : 4) : 2) void k_linear_tile(const wq_linear_args a, const wq_tile_grid t) {
     constexpr bool K64 = GS != 32;
     constexpr int KSTEP = K64 ? 64 : 32, NK = SK / KSTEP;
     constexpr int WB = 16 * SK / (W4 ? 2 : 1), XB = 16 * SK;   // bytes of a 16-row block in a stage
@@ -67,10 +67,6 @@ __global__ __launch_bounds__(256 * KS, 2) void k_linear_tile(const wq_linear_arg
     // in the workspace still)
     const __amdgpu_buffer_rsrc_t rX = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<int8_t *>(a.xq), 0, (int)((unsigned)a.P * (unsigned)a.Cin + (K64 ? 0u : 8u)), kBufFlags);
-    const __amdgpu_buffer_rsrc_t rSW = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<float *>(a.sW), 0, (int)((unsigned)groups * (unsigned)a.Cout_pad * 4u), kBufFlags);
-    const __amdgpu_buffer_rsrc_t rSX = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<float *>(a.sx), 0, (int)((unsigned)groups * (unsigned)a.P * 4u), kBufFlags);
 
     // ---- the loader ----
     // Rows and channels past the end read the last one again (not stored).  K past the end (half of a last stage, groups of
@@ -80,8 +76,8 @@ __global__ __launch_bounds__(256 * KS, 2) void k_linear_tile(const wq_linear_arg
     static_assert(LW * 4096 == OB * WB && LX * 4096 == PB * XB, "four waves share the loads evenly");
     constexpr int SPAN = 1024 / (16 * KSTEP);                 // K-steps that a load of x brings
     const unsigned run = (16u * (unsigned)a.Cin) >> (W4 ? 1 : 0);   // bytes of a weight block: all of K
+    const unsigned stepX = 4u * (unsigned)a.P * (KSTEP / 4);  // bytes of a K-step of x
     unsigned vW[LW], vX[LX];
-    int kX[LX];   // which K-steps of the stage a load brings
 #pragma unroll
     for (int u = 0; u < LW; ++u) {
         const int byte = (w * LW + u) * 1024 + lane * 16;
@@ -90,45 +86,45 @@ __global__ __launch_bounds__(256 * KS, 2) void k_linear_tile(const wq_linear_arg
 #pragma unroll
     for (int u = 0; u < LX; ++u) {
         const int i = w * LX + u, row0 = p0 + i * 1024 / XB * 16;
-        kX[u] = i * 1024 % XB / 1024 * SPAN;
+        const unsigned k = (unsigned)(i * 1024 % XB / 1024 * SPAN) * stepX;   // which K-steps of the stage
         if constexpr (K64) {
-            vX[u] = ((unsigned)q * (unsigned)a.P + (unsigned)min(row0 + l16, last_row)) * 16u;
+            vX[u] = k + ((unsigned)q * (unsigned)a.P + (unsigned)min(row0 + l16, last_row)) * 16u;
         } else {   // lanes 0-31 and 32-63: a K-step each, its quarters of 16 rows in pairs
             const int row = min(row0 + (lane & 7) * 2, last_row & ~1);
-            vX[u] = ((unsigned)((lane >> 3) & 7) * (unsigned)a.P + (unsigned)row) * 8u;
+            vX[u] = k + ((unsigned)((lane >> 3) & 7) * (unsigned)a.P + (unsigned)row) * 8u;
         }
     }
     // scales, a word a lane: weight rows first, then rows of x, 64 of one group to a load
     constexpr int QW = OB / 4, QX = PB / 4, NL = NGS * (QW + QX), LS = (NL + 3) / 4;
     static_assert(OB % 4 == 0 && PB % 4 == 0, "a load brings the scales of four blocks");
-    unsigned vS[LS];
+    static_assert(OB == PB, "both kinds of scales lie alike in LDS");
+    const int kind = w % (QW + QX);   // what the wave's loads bring, of every group: its quarter of the weight rows or of x's
+    const bool of_w = kind < QW;
+    const unsigned vS = of_w ? (unsigned)block_of(kind * 4 + q) * 64u + (unsigned)l16 * 4u
+                             : (unsigned)min(p0 + (kind - QW) * 64 + lane, last_row) * 4u;
+    const unsigned stepS = (unsigned)(of_w ? a.Cout_pad : a.P) * 4u;
+    const __amdgpu_buffer_rsrc_t rS = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<float *>(of_w ? a.sW : a.sx), 0, (int)((unsigned)groups * stepS), kBufFlags);
+    char *const stages = lds + team * NST * STAGE;
+    char *const toW = stages + WOFF + w * LW * 1024, *const toX = stages + XOFF + w * LX * 1024,
+               *const toS = stages + (of_w ? SWOFF + kind * 256 : SXOFF + (kind - QW) * 256);
+    unsigned oW = (unsigned)s_beg * WB, oX = (unsigned)s_beg * NK * stepX;
+    int s_next = s_beg;   // stages are asked for in turn
+    auto issue = [&](int slot) {
 #pragma unroll
-    for (int u = 0; u < LS; ++u) {
-        const int i = (w + u * 4) % NL, k = i % (QW + QX);
-        vS[u] = k < QW ? (unsigned)block_of(k * 4 + q) * 64u + (unsigned)l16 * 4u
-                       : (unsigned)min(p0 + (k - QW) * 64 + lane, last_row) * 4u;
-    }
-    const int steps = a.Cin / KSTEP;
-    const unsigned stepX = 4u * (unsigned)a.P * (KSTEP / 4);
-    auto issue = [&](int s, int slot) {
-        char *base = lds + (team * NST + slot) * STAGE;
+        for (int u = 0; u < LW; ++u) lds_load16(rW, toW + slot * STAGE + u * 1024, vW[u], oW);
 #pragma unroll
-        for (int u = 0; u < LW; ++u)
-            lds_load16(rW, base + WOFF + (w * LW + u) * 1024, vW[u], min((unsigned)s * WB, run));
-#pragma unroll
-        for (int u = 0; u < LX; ++u) {
-            const int k = min(s * NK + kX[u], steps);
-            lds_load16(rX, base + XOFF + (w * LX + u) * 1024, vX[u], (unsigned)k * stepX);
-        }
+        for (int u = 0; u < LX; ++u) lds_load16(rX, toX + slot * STAGE + u * 1024, vX[u], oX);
 #pragma unroll
         for (int u = 0; u < LS; ++u) {
-            const int i = (w + u * 4) % NL, k = i % (QW + QX), gl = i / (QW + QX);   // (a wave without one of its own repeats another's)
-            const int gi = min(GS > SK ? (s * SK) >> a.log2g : s * NGS + gl, groups - 1);
-            if (k < QW)
-                lds_load4(rSW, base + SWOFF + gl * OB * 64 + k * 256, vS[u], (unsigned)gi * (unsigned)a.Cout_pad * 4u);
-            else
-                lds_load4(rSX, base + SXOFF + gl * PB * 64 + (k - QW) * 256, vS[u], (unsigned)gi * (unsigned)a.P * 4u);
+            const int gl = (w + u * 4) % NL / (QW + QX);   // (a wave without a load of its own repeats another's)
+            int gi = GS > SK ? (s_next * SK) >> a.log2g : s_next * NGS + gl;
+            if (GS < SK) gi = min(gi, groups - 1);
+            lds_load4(rS, toS + slot * STAGE + gl * OB * 64, vS, (unsigned)gi * stepS);
         }
+        oW += WB;
+        oX += NK * stepX;
+        ++s_next;
     };
 
     v4f M[NO][NB];
@@ -160,35 +156,36 @@ __global__ __launch_bounds__(256 * KS, 2) void k_linear_tile(const wq_linear_arg
         return v;
     };
     constexpr int KB = KSTEP / 4, WKB = W4 ? KB / 2 : KB;   // bytes a lane holds of a K-step
-    auto read_w = [&](const char *base, int e, int k) {
-        return piece(base + WOFF + (wo * NO + e) * WB + (k * 64 + lane) * WKB, std::integral_constant<int, WKB>{});
+    // (the lane's parts of the addresses once: all else is constants)
+    const char *const atW = stages + WOFF + wo * NO * WB + lane * WKB, *const atX = stages + XOFF + wp * NB * XB + lane * KB,
+               *const atSW = stages + SWOFF + wo * NO * 64 + q * 16, *const atSX = stages + SXOFF + wp * NB * 64 + l16 * 4;
+    auto read_w = [&](int slot, int e, int k) {
+        return piece(atW + slot * STAGE + e * WB + k * 64 * WKB, std::integral_constant<int, WKB>{});
     };
-    auto read_sw = [&](const char *base, int e, int k) { return *(const v4f *)(base + SWOFF + k * OB * 64 + (wo * NO + e) * 64 + q * 16); };
+    auto read_sw = [&](int slot, int e, int k) { return *(const v4f *)(atSW + slot * STAGE + k * OB * 64 + e * 64); };
     auto read = [&](int s, int slot, Operands &op) {
-        const char *base = lds + (team * NST + slot) * STAGE;
 #pragma unroll
         for (int k = 0; k < NK; ++k)
 #pragma unroll
             for (int f = 0; f < NB; ++f)
-                op.x[k][f] = piece(base + XOFF + (wp * NB + f) * XB + (k * 64 + lane) * KB, std::integral_constant<int, KB>{});
+                op.x[k][f] = piece(atX + slot * STAGE + f * XB + k * 64 * KB, std::integral_constant<int, KB>{});
 #pragma unroll
         for (int k = 0; k < NGS; ++k)
 #pragma unroll
             for (int f = 0; f < NB; ++f) {
-                const float v = *(const float *)(base + SXOFF + k * PB * 64 + (wp * NB + f) * 64 + l16 * 4);
+                const float v = *(const float *)(atSX + slot * STAGE + k * PB * 64 + f * 64);
                 op.sx[k][f] = GS >= SK || s * NGS + k < groups ? v : 0.f;
             }
     };
 
     auto compute = [&](int s, int slot, const Operands &op) {
-        const char *base = lds + (team * NST + slot) * STAGE;
         const bool done = GS <= SK || ((s + 1) * SK & ((1 << a.log2g) - 1)) == 0;   // a group ends with this stage
 #pragma unroll
         for (int e = 0; e < NO; ++e) {
             v4i av[NK];
 #pragma unroll
             for (int k = 0; k < NK; ++k) {
-                av[k] = read_w(base, e, k);
+                av[k] = read_w(slot, e, k);
                 if constexpr (W4) {
                     const unsigned a0 = (unsigned)av[k].x, a1 = (unsigned)av[k].y;
                     av[k] = v4i{(int)((a0 << 4) & 0xf0f0f0f0u), (int)(a0 & 0xf0f0f0f0u), (int)((a1 << 4) & 0xf0f0f0f0u),
@@ -203,7 +200,7 @@ __global__ __launch_bounds__(256 * KS, 2) void k_linear_tile(const wq_linear_arg
                                                                  __builtin_bit_cast(long, v2i{b.x, b.y}), c, 0, 0, 0);
             };
             auto dequant = [&](int k, v4i (&P)[NB]) {
-                v4f sw = read_sw(base, e, k);
+                v4f sw = read_sw(slot, e, k);
                 if constexpr (W4 && !MAGIC) sw *= 0.0625f;
 #pragma unroll
                 for (int f = 0; f < NB; ++f)
@@ -244,20 +241,22 @@ __global__ __launch_bounds__(256 * KS, 2) void k_linear_tile(const wq_linear_arg
     constexpr int LPS = LW + LX + LS;   // a wave's loads of a stage
 #pragma unroll
     for (int d = 0; d < NST - 1; ++d)
-        if (s_beg + d < s_end) issue(s_beg + d, d);
-    int slot = 0;
-    for (int n = 0; n < rounds; ++n) {
-        const int s = s_beg + n;
-        // the stage's loads have landed, every wave's, and the slot of the stage before has been read by all
-        if (NST > 2 && s + NST - 1 <= s_end) wait_and_barrier<(NST - 2) * LPS>();
-        else wait_and_barrier<0>();
-        if (s + NST - 1 < s_end) issue(s + NST - 1, slot == 0 ? NST - 1 : slot - 1);
-        if (s < s_end) {
-            Operands op;
-            read(s, slot, op);
-            compute(s, slot, op);
+        if (s_beg + d < s_end) issue(d);
+    for (int n = 0; n < rounds; n += NST) {
+#pragma unroll
+        for (int slot = 0; slot < NST; ++slot) {   // (a constant: so are the addresses in LDS)
+            if (n + slot >= rounds) break;
+            const int s = s_beg + n + slot;
+            // the stage's loads have landed, every wave's, and the slot of the stage before has been read by all
+            if (NST > 2 && s + NST - 1 <= s_end) wait_and_barrier<(NST - 2) * LPS>();
+            else wait_and_barrier<0>();
+            if (s + NST - 1 < s_end) issue((slot + NST - 1) % NST);
+            if (s < s_end) {
+                Operands op;
+                read(s, slot, op);
+                compute(s, slot, op);
+            }
         }
-        slot = slot == NST - 1 ? 0 : slot + 1;
     }
 
     // ---- epilogue ----
