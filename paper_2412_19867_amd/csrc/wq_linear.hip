@@ -34,85 +34,151 @@ __device__ __forceinline__ double wave_sum(double v) {
 
 // The norm's factor.  The squares of fp32 numbers are exact in 64 bits and their sum is off by some 1e-16, so
 // that the factor, rounded once to fp32, does not depend on the order of the sum, nor do the codes behind it.
+// (Two Newton steps take the hardware's estimate of 1 / sqrt to the last places of 64 bits; a square root and a division
+// are five times as many instructions, one after the other.)
 __device__ __forceinline__ float norm_factor(double squares, int Cin, double eps) {
-    return (float)(1.0 / sqrt(squares / Cin + eps));
+    const double x = squares * (1.0 / Cin) + eps, half = 0.5 * x;
+    double y = __builtin_amdgcn_rsq(x);
+    y = y * __builtin_fma(-half * y, y, 1.5);
+    y = y * __builtin_fma(-half * y, y, 1.5);
+    return (float)y;
 }
 
 // Rows in pieces of eight elements a lane, held in registers: one pass over the data.  A group of g elements is g / 8 adjacent
-// lanes of one wave.  NORM: `wpr` waves share a row of up to 512 V wpr elements; otherwise a wave takes 512 V elements of
-// a row (the rows one after the other, then the next elements of each), wpr = 1.
-template <int TYPE, bool NORM, int V>
-__global__ __launch_bounds__(512) void k_quantize_pieces(const QArgs a, int wpr, int per_xcd) {
+// lanes of one wave.  NORM: `wpr` waves share a row of up to 512 V wpr elements (R = 1); otherwise a wave takes 512
+// elements of R rows (the rows one after the other, then the next elements of each), wpr = V = 1.
+//   bound: memory.  4096x8192 with residual, g 64: fp32 88 us (438 MB at 5.0 TB/s), bf16 56 (4.2); 4096x4096 bf16 22 (5.3, part of
+//   it from the last-level cache).  An addition of two tensors into a third moves 5.5 to 5.7 TB/s; the codes' lines, which
+//   eight (sixteen, g 32) rows fill together, cost a tenth.
+//   h is stored past the caches: 4096x4096 bf16 30 us with plain stores, 22 so.
+//   The order of workgroups: runs of 16 rows to an XCD, one after the other, keep all XCDs in one region of memory and the codes'
+//   lines whole (4096x8192 fp32 94 us, an eighth of the rows to each XCD 107, rows in turn 111); codes alone prefer
+//   the eighths (8192x8192 bf16 45 us, runs of 64 50, of 16 52).
+//   More waves to a row, fewer pieces each, hide more of the latency (4096x4096 bf16, 1, 2, 4, 8 waves: 41, 33, 33, 31).
+//   R = 2: of two lanes with halves of a piece of 16 bytes in both rows, one stores each row's piece: half the stores
+//   (8192x8192 bf16 55 -> 45 us).  The norm loses more in waves than it gains (33 against 31).
+template <int TYPE, bool NORM, int V, int R>
+__global__ __launch_bounds__(512) void k_quantize_pieces(const QArgs a, int wpr, unsigned run) {
     using T = typename Elem<TYPE>::type;
-    __shared__ double part[8];
+    __shared__ double part[8][R];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rpw = (int)(blockDim.x >> 6) / wpr;   // rows of a workgroup
-    // neighbouring rows' codes share lines: an XCD takes a contiguous share of the rows, whose lines its L2 puts together
-    const long unit = ((long)(blockIdx.x & 7u) * per_xcd + (blockIdx.x >> 3)) * rpw + w / wpr;
-    const int p = NORM ? (int)unit : (int)(unit % a.rows);
-    const int c0 = NORM ? (w % wpr) * 512 + lane * 8 : (int)(unit / a.rows) * (512 * V) + lane * 8, step = 512 * wpr;
-    const bool row = NORM ? unit < a.rows : true;
-    const T *x = (const T *)a.x + (size_t)p * a.xs;
-    float v[V][8];
+    const int upw = (int)(blockDim.x >> 6) / wpr;   // units of R rows of a workgroup
+    // neighbouring rows' codes share lines: an XCD takes `run` workgroups in a row, whose lines its L2 puts together
+    const unsigned turn = blockIdx.x >> 3;
+    const long unit = ((long)(turn / run) * 8 * run + (blockIdx.x & 7u) * run + turn % run) * upw + w / wpr;
+    const int pairs = (a.rows + R - 1) / R;
+    const int p = (NORM ? (int)unit : (int)(unit % pairs)) * R;
+    const int c0 = NORM ? (w % wpr) * 512 + lane * 8 : (int)(unit / pairs) * 512 + lane * 8, step = 512 * wpr;
+    const int rows = NORM && unit >= pairs ? 0 : min(R, a.rows - p);   // rows of the unit
+    float v[R][V][8];
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-        const int c = c0 + k * step;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[k][j] = 0.0f;
-        if (row && c < a.Cin) load8<T>(x + c, v[k]);
-    }
-    if constexpr (NORM) {
-        if (a.res) {
-            const T *res = (const T *)a.res + (size_t)p * a.rs;
-            float t[V][8];
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) t[k][j] = 0.0f;
-                if (row && c0 + k * step < a.Cin) load8<T>(res + c0 + k * step, t[k]);
-            }
-#pragma unroll
-            for (int k = 0; k < V; ++k)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[k][j] += t[k][j];
-        }
-        double squares = 0.0;
-#pragma unroll
-        for (int k = 0; k < V; ++k)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) squares = __builtin_fma((double)v[k][j], (double)v[k][j], squares);
-        squares = wave_sum(squares);
-        if (wpr > 1) {
-            if (lane == 0) part[w] = squares;
-            __syncthreads();
-            squares = 0.0;
-            for (int k = 0; k < wpr; ++k) squares += part[w / wpr * wpr + k];
-        }
-        if (a.sum) {   // (all of the row has been read: it may be x or the residual itself)
-            T *sum = (T *)a.sum + (size_t)p * a.hs;
-#pragma unroll
-            for (int k = 0; k < V; ++k)
-                if (row && c0 + k * step < a.Cin) store8<T>(sum + c0 + k * step, v[k]);
-        }
-        const float rho = norm_factor(squares, a.Cin, a.eps);
+    for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            float gm[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-            if (a.gamma && c0 + k * step < a.Cin) load8<float>(a.gamma + c0 + k * step, gm);
+            const int c = c0 + k * step;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[k][j] = v[k][j] * rho * gm[j];
+            for (int j = 0; j < 8; ++j) v[r][k][j] = 0.0f;
+            if (r < rows && c < a.Cin) load8<T>((const T *)a.x + (size_t)(p + r) * a.xs + c, v[r][k]);
+        }
+    if constexpr (NORM) {
+        if (a.res) {
+            float t[R][V][8];
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) t[r][k][j] = 0.0f;
+                    if (r < rows && c0 + k * step < a.Cin) load8<T>((const T *)a.res + (size_t)(p + r) * a.rs + c0 + k * step, t[r][k]);
+                }
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[r][k][j] += t[r][k][j];
+        }
+        // gamma is under way while the sum is formed
+        float gm[V][8];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) gm[k][j] = 1.0f;
+            if (a.gamma && c0 + k * step < a.Cin) load8<float>(a.gamma + c0 + k * step, gm[k]);
+        }
+        double squares[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            squares[r] = 0.0;
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) squares[r] = __builtin_fma((double)v[r][k][j], (double)v[r][k][j], squares[r]);
+            squares[r] = wave_sum(squares[r]);
+        }
+        if (wpr > 1) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (lane == 0) part[w][r] = squares[r];
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                squares[r] = 0.0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {   // (a loop of wpr turns would wait for LDS in each)
+                    const double q = part[w / wpr * wpr + min(k, wpr - 1)][r];
+                    squares[r] += k < wpr ? q : 0.0;
+                }
+            }
+        }
+        if (a.sum) {   // (all of the row has been read: it may be x or the residual itself)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    if (r < rows && c0 + k * step < a.Cin) store8<T>((T *)a.sum + (size_t)(p + r) * a.hs + c0 + k * step, v[r][k]);
+        }
+        float rho[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) rho[r] = norm_factor(squares[r], a.Cin, a.eps);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[r][k][j] = v[r][k][j] * rho[r] * gm[k][j];
         }
     }
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         const int c = c0 + k * step;
-        float s;
-        const uint2 codes = quantize_piece(v[k], a.g, s);
-        if (!row || c >= a.Cin) continue;
-        // planes of 8 bytes a row with groups of 32, else of 16, of which this is a half
-        const size_t at = a.g == 32 ? ((size_t)(c >> 3) * a.P + p) * 8 : ((size_t)(c >> 4) * a.P + p) * 16 + (c & 8);
-        *(uint2 *)(a.xq + at) = codes;
-        if ((c & (a.g - 1)) == 0) a.sx[(size_t)(c / a.g) * a.P + p] = s;
+        float s[R];
+        uint2 codes[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) codes[r] = quantize_piece(v[r][k], a.g, s[r]);
+        if (a.g == 32) {   // planes of 8 bytes a row
+            if (c >= a.Cin) continue;
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (r < rows) *(uint2 *)(a.xq + ((size_t)(c >> 3) * a.P + p + r) * 8) = codes[r];
+        } else if constexpr (R == 1) {   // planes of 16 bytes a row, of which this is a half
+            if (c >= a.Cin || rows == 0) continue;
+            *(uint2 *)(a.xq + ((size_t)(c >> 4) * a.P + p) * 16 + (c & 8)) = codes[0];
+        } else {   // of two lanes with halves of both rows one takes each row
+            const bool odd = lane & 1;
+            const uint2 give = odd ? codes[0] : codes[R - 1], keep = odd ? codes[R - 1] : codes[0];
+            const uint2 got = make_uint2((uint32_t)__builtin_amdgcn_mov_dpp((int)give.x, 0xB1, 0xf, 0xf, true),
+                                         (uint32_t)__builtin_amdgcn_mov_dpp((int)give.y, 0xB1, 0xf, 0xf, true));
+            if (c >= a.Cin) continue;
+            if (odd < rows)
+                *(uint4 *)(a.xq + ((size_t)(c >> 4) * a.P + p + odd) * 16) =
+                    odd ? make_uint4(got.x, got.y, keep.x, keep.y) : make_uint4(keep.x, keep.y, got.x, got.y);
+        }
+        if ((c & (a.g - 1)) == 0) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (r < rows) a.sx[(size_t)(c / a.g) * a.P + p + r] = s[r];
+        }
     }
 }
 
@@ -183,27 +249,26 @@ void launch_quantize(const QArgs &a, hipStream_t s) {
         return;
     }
     const int chunks = (a.Cin + 511) / 512;   // of a wave's 512 elements
-    int wpr = 1, V = 1;
-    long units;
+    int wpr = 1, V = 1, R = !NORM && (long)a.rows * chunks >= 4096 ? 2 : 1;
+    long units = (a.rows + R - 1) / R;
     if (NORM) {
-        // as few waves to a row as hold it in 64 registers each, more while they would leave CUs without work
-        while (8 * wpr < chunks) wpr *= 2;
-        while (wpr < chunks && wpr < 8 && (long)a.rows * wpr < 4096) wpr *= 2;
+        while (wpr < chunks && wpr < 8) wpr *= 2;
         while (V * wpr < chunks) V *= 2;
-        units = a.rows;
     } else {
-        V = (long)a.rows * chunks >= 16384 && chunks >= 4 ? 4 : 1;
-        units = (long)a.rows * ((chunks + V - 1) / V);
+        units *= chunks;
     }
-    const int waves = wpr < 4 ? 4 : wpr, rpw = waves / wpr;
-    const long blocks = (units + rpw - 1) / rpw, per_xcd = (blocks + 7) / 8;
-    const dim3 grid((unsigned)(blocks < 8 ? blocks : per_xcd * 8)), block(64 * waves);
-    const int share = blocks < 8 ? 1 : (int)per_xcd;
-    if (V == 1) hipLaunchKernelGGL((k_quantize_pieces<TYPE, NORM, 1>), grid, block, 0, s, a, wpr, share);
-    if (V == 4) hipLaunchKernelGGL((k_quantize_pieces<TYPE, NORM, 4>), grid, block, 0, s, a, wpr, share);
+    const int waves = wpr < 4 ? 4 : wpr, upw = waves / wpr;
+    const long blocks = (units + upw - 1) / upw, share = (blocks + 7) / 8;
+    const unsigned run = (unsigned)(NORM && share > 16 ? 16 : share);
+    const dim3 grid((unsigned)((share + run - 1) / run * run * 8)), block(64 * waves);
     if constexpr (NORM) {
-        if (V == 2) hipLaunchKernelGGL((k_quantize_pieces<TYPE, NORM, 2>), grid, block, 0, s, a, wpr, share);
-        if (V == 8) hipLaunchKernelGGL((k_quantize_pieces<TYPE, NORM, 8>), grid, block, 0, s, a, wpr, share);
+        if (V == 1) hipLaunchKernelGGL((k_quantize_pieces<TYPE, true, 1, 1>), grid, block, 0, s, a, wpr, run);
+        else if (V == 2) hipLaunchKernelGGL((k_quantize_pieces<TYPE, true, 2, 1>), grid, block, 0, s, a, wpr, run);
+        else if (V == 4) hipLaunchKernelGGL((k_quantize_pieces<TYPE, true, 4, 1>), grid, block, 0, s, a, wpr, run);
+        else hipLaunchKernelGGL((k_quantize_pieces<TYPE, true, 8, 1>), grid, block, 0, s, a, wpr, run);
+    } else {
+        if (R == 1) hipLaunchKernelGGL((k_quantize_pieces<TYPE, false, 1, 1>), grid, block, 0, s, a, wpr, run);
+        else hipLaunchKernelGGL((k_quantize_pieces<TYPE, false, 1, 2>), grid, block, 0, s, a, wpr, run);
     }
 }
 

@@ -41,6 +41,7 @@ __device__ __forceinline__ void load8(const T *p, float (&v)[8]) {
         for (int j = 0; j < 16 / (int)sizeof(T); ++j) v[k * 16 / sizeof(T) + j] = (float)t[j];
     }
 }
+// (stored past the caches: what comes next reads the codes)
 template <typename T>
 __device__ __forceinline__ void store8(T *p, const float (&v)[8]) {
     typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
@@ -49,7 +50,7 @@ __device__ __forceinline__ void store8(T *p, const float (&v)[8]) {
         vec t;
 #pragma unroll
         for (int j = 0; j < 16 / (int)sizeof(T); ++j) t[j] = (T)v[k * 16 / sizeof(T) + j];
-        ((vec *)p)[k] = t;
+        __builtin_nontemporal_store(t, (vec *)p + k);
     }
 }
 
