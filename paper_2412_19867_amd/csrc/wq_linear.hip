@@ -345,12 +345,12 @@ bool quantizes_itself(const wq_linear_args &a, const void *x, int64_t xs) {
     return x1 <= y0 || y1 <= x0;
 }
 
-// Which kernel multiplies: over 279 drawn layers of 4 to 4096 rows, 320 to 8192 input and 32 to 16384 output channels the rules
+// Which kernel multiplies: over 329 drawn layers of 17 to 4096 rows, 320 to 8192 input and 32 to 16384 output channels the rules
 // below are 1.5 % (geometric mean) from the best of the forms.  With n64 and n128 the numbers of tiles of 64 (128) weight
 // rows x 64 (128) rows of x; us of the forms on either side of each line:
 //   rows: one 16-row block a workgroup up to 16 rows, else for up to 256 blocks of 16 columns x 16 rows
 //     (57x1920->1440 g 128, 360 blocks: one 6.7, two 5.5; 55x3328->800 g 32, 200: 7.7, 8.8), two beyond
-//   tiles from 33 rows and 150 tiles of 64 (75x1792->2x3808 g 256, 238: rows 10.5, tiles 8.9; 188x4928->1952 g 64, 93: 16.2, 17.3)
+//   tiles from 33 rows and 100 tiles of 64 (75x1792->2x3808 g 256, 238: rows 10.5, tiles 8.9; 68x5888->2x1904 g 64, 120: 15.3, 17.9)
 //   tiles of 64: four teams share a reduction up to 256 tiles (128x8192->4096 g 128: four 19.2, two 23.4, one 35.3), two
 //     up to 512 (1001x2048->2040 g 256: 16.5, 13.6, 15.6), else one (1024x4096->4096 g 64: 52.5, 44.8, 42.8): CUs with
 //     eight to sixteen waves
@@ -362,7 +362,7 @@ wq_status_t run_product(const wq_direct_plan *plan, const wq_linear_args &a, hip
     auto tiles = [&](int n) { return (long)((Cout + n - 1) / n) * ((a.rows + n - 1) / n); };
     const long n64 = tiles(64), n128 = tiles(128);
     hipError_t e;
-    if (a.rows <= 32 || n64 <= 150) {
+    if (a.rows <= 32 || n64 <= 100) {
         const bool one = a.rows <= 16 || (long)((a.outs + 15) / 16) * ((a.rows + 15) / 16) <= 256;
         e = wq_launch_linear_rows(a, plan->g, plan->wbits, one ? 1 : 2, s);
     } else {

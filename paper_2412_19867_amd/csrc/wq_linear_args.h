@@ -32,26 +32,41 @@ __device__ __forceinline__ float logistic(float e2) { return __builtin_amdgcn_rc
 
 // The division, exponential and error function of the math library, correctly rounded or nearly, take 40 (silu) to 100 (gelu)
 // instructions a value in place of 5 to 17: an eighth of the vector instructions of the product 4096 x 4096 -> 2 x 8192, g 128.
-__device__ __forceinline__ float activate(float z, int act) {
+__device__ __forceinline__ float gelu(float z) {
+    // z Phi(z) = max(z, 0) - |z| e^(-z^2 / 2) G(|z|), G(x) = e^(x^2 / 2) erfc(x / sqrt 2) / 2 as a polynomial in
+    // t = 1 / (1 + 0.28 x): a least-squares fit, 4.3e-9 off the exact gelu; evaluated, 2.4e-7 at |z| near 4
+    const float x = fabsf(z), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.28f, x, 1.0f));
+    float G = -0.1121234f;
+    G = __builtin_fmaf(G, t, 0.418009400f);
+    G = __builtin_fmaf(G, t, -0.288568288f);
+    G = __builtin_fmaf(G, t, 0.318627954f);
+    G = __builtin_fmaf(G, t, 0.0409632139f);
+    G = __builtin_fmaf(G, t, 0.123935819f);
+    G = __builtin_fmaf(G, t, -0.000844957307f);
+    return __builtin_fmaf(-x, __builtin_amdgcn_exp2f(x * x * -0.721347520f) * G, fmaxf(z, 0.0f));
+}
+
+// N values at a time: one (uniform) choice for all of them.
+template <int N>
+__device__ __forceinline__ void activate(float (&z)[N], int act) {
     switch (act) {
-        case WQ_ACT_RELU: return fmaxf(z, 0.0f);
-        case WQ_ACT_SILU: return z * logistic(z * -1.44269504f);
-        case WQ_ACT_GELU: {
-            // z Phi(z) = max(z, 0) - |z| e^(-z^2 / 2) G(|z|), G(x) = e^(x^2 / 2) erfc(x / sqrt 2) / 2 as a polynomial in
-            // t = 1 / (1 + 0.28 x): a least-squares fit, 4.3e-9 off the exact gelu; evaluated, 2.4e-7 at |z| near 4
-            const float x = fabsf(z), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.28f, x, 1.0f));
-            float G = -0.1121234f;
-            G = __builtin_fmaf(G, t, 0.418009400f);
-            G = __builtin_fmaf(G, t, -0.288568288f);
-            G = __builtin_fmaf(G, t, 0.318627954f);
-            G = __builtin_fmaf(G, t, 0.0409632139f);
-            G = __builtin_fmaf(G, t, 0.123935819f);
-            G = __builtin_fmaf(G, t, -0.000844957307f);
-            return __builtin_fmaf(-x, __builtin_amdgcn_exp2f(x * x * -0.721347520f) * G, fmaxf(z, 0.0f));
-        }
-        // z (1 + tanh u) / 2 = z / (1 + e^-2u), u = sqrt(2 / pi) (z + 0.044715 z^3)
-        case WQ_ACT_GELU_TANH: return z * logistic(z * __builtin_fmaf(-0.102943240f, z * z, -2.30220820f));
-        default: return z;
+        case WQ_ACT_RELU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) z[i] = fmaxf(z[i], 0.0f);
+            break;
+        case WQ_ACT_SILU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) z[i] *= logistic(z[i] * -1.44269504f);
+            break;
+        case WQ_ACT_GELU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) z[i] = gelu(z[i]);
+            break;
+        case WQ_ACT_GELU_TANH:   // z (1 + tanh u) / 2 = z / (1 + e^-2u), u = sqrt(2 / pi) (z + 0.044715 z^3)
+#pragma unroll
+            for (int i = 0; i < N; ++i) z[i] *= logistic(z[i] * __builtin_fmaf(-0.102943240f, z[i] * z[i], -2.30220820f));
+            break;
+        default: break;
     }
 }
 
@@ -105,19 +120,27 @@ __device__ __forceinline__ void store_elems(void *p, long i, int type, bool wide
     }
 }
 
-// The epilogue of columns o .. o + 3 of row p, from the sums z (gated: and those of what the gate multiplies, up) with their
-// bias, and the residual's values.
-__device__ __forceinline__ void finish_columns(const wq_linear_args &a, long p, int o, v4f z, v4f up, v4f res) {
+// The epilogue of columns o .. o + 3 of rows p, p + row_step, .. (R of them), from the sums z (gated: and those of what the gate
+// multiplies, up) with their bias, and the residual's values.
+template <int R>
+__device__ __forceinline__ void finish_columns(const wq_linear_args &a, long p, int row_step, int o, const v4f (&zs)[R],
+                                               const v4f (&up)[R], const v4f (&res)[R]) {
     const int n = a.outs - o;
+    float z[4 * R];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) z[r] = activate(z[r], a.act);
-    if (a.gated) z *= up;
-    if (a.res) z += res;
-    store_elems(a.y, p * a.ys + o, a.type, a.wide && n >= 4, n, z);
+    for (int i = 0; i < 4 * R; ++i) z[i] = zs[i / 4][i % 4];
+    activate(z, a.act);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        v4f y = {z[4 * r], z[4 * r + 1], z[4 * r + 2], z[4 * r + 3]};
+        if (a.gated) y *= up[r];
+        if (a.res) y += res[r];
+        if (p + r * row_step < a.rows) store_elems(a.y, (p + r * row_step) * a.ys + o, a.type, a.wide && n >= 4, n, y);
+    }
 }
 __device__ __forceinline__ v4f residual_of(const wq_linear_args &a, long p, int o) {
     const int n = a.outs - o;
-    return a.res ? load_elems(a.res, p * a.rs + o, a.type, a.wide && n >= 4, n) : v4f{};
+    return a.res && p < a.rows ? load_elems(a.res, p * a.rs + o, a.type, a.wide && n >= 4, n) : v4f{};
 }
 
 }  // namespace

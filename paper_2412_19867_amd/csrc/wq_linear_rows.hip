@@ -246,15 +246,15 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
         const int row = tid >> 2, c = (tid & 3) * 4, p = p0 + 16 * f + row, o = ob * 16 + c;
         if (tid >= 64 || p >= a.rows || o >= a.outs) continue;
         const float *s = part_s + row * RS + c;
-        const v4f res = residual_of(a, p, o);
-        v4f z = *(const v4f *)s + *(const v4f *)(a.bias + o), up = {0.f, 0.f, 0.f, 0.f};   // (the bias is padded as the weights are)
-        if constexpr (GATED) up = *(const v4f *)(s + 16) + *(const v4f *)(a.bias + a.outs + o);
+        const v4f res[1] = {residual_of(a, p, o)};
+        v4f z[1] = {*(const v4f *)s + *(const v4f *)(a.bias + o)}, up[1] = {};   // (the bias is padded as the weights are)
+        if constexpr (GATED) up[0] = *(const v4f *)(s + 16) + *(const v4f *)(a.bias + a.outs + o);
         for (int k = 1; k < t.slices; ++k) {
             s += 16 * RS;
-            z += *(const v4f *)s;
-            if constexpr (GATED) up += *(const v4f *)(s + 16);
+            z[0] += *(const v4f *)s;
+            if constexpr (GATED) up[0] += *(const v4f *)(s + 16);
         }
-        finish_columns(a, p, o, z, up, res);
+        finish_columns<1>(a, p, 0, o, z, up, res);
     }
 }
 

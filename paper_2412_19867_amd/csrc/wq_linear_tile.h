@@ -269,6 +269,7 @@ __global__ __launch_bounds__(256 * KS, NO == 4 && SK == 64 ? (W4 ? 3 : 4) : 2) v
     const int quads = a.gated ? 2 * NO : 4 * NO, shift = a.gated ? __builtin_ctz(2 * NO) : __builtin_ctz(4 * NO);
     const int c = (lane & (quads - 1)) * 4, o = (po * 2 + wo) * quads * 4 + c;
     const int items = o < a.outs ? FB * 16 << shift : 0, row_step = (64 * KS) >> shift;
+    constexpr int U = FB * 32 * NO >= 128 * KS ? 2 : 1;   // rows at a time: a divisor of each lane's, gated or not
     v4f bias = {}, bias_up = {};
     if (o < a.outs) {   // (the bias is padded as the weights are)
         bias = *(const v4f *)(a.bias + o);
@@ -285,22 +286,31 @@ __global__ __launch_bounds__(256 * KS, NO == 4 && SK == 64 ? (W4 ? 3 : 4) : 2) v
         if (KS > 1) __syncthreads();
         else __builtin_amdgcn_wave_barrier();
         int row = (team * 64 + lane) >> shift, p = p0 + (wp * NB + f0) * 16 + row;   // (the teams share the rows)
-        v4f res = items && p < a.rows ? residual_of(a, p, o) : v4f{};
-#pragma unroll 1
-        for (int i = team * 64 + lane; i < items; i += 64 * KS) {
-            if (p >= a.rows) break;
-            const v4f next = i + 64 * KS < items && p + row_step < a.rows ? residual_of(a, p + row_step, o) : v4f{};
-            const float *sums = (const float *)lds + w * PART + row * RS + c;
-            v4f z = bias + *(const v4f *)sums, up = a.gated ? bias_up + *(const v4f *)(sums + 8 * NO) : v4f{};
+        v4f res[U] = {};
 #pragma unroll
-            for (int k = 1; k < KS; ++k) {
-                z += *(const v4f *)(sums + 4 * k * PART);
-                if (a.gated) up += *(const v4f *)(sums + 4 * k * PART + 8 * NO);
+        for (int u = 0; u < U; ++u)
+            if (items) res[u] = residual_of(a, p + u * row_step, o);
+#pragma unroll 1
+        for (int i = team * 64 + lane; i < items; i += 64 * KS * U) {
+            if (p >= a.rows) break;
+            v4f next[U] = {}, z[U], up[U] = {};
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (i + 64 * KS * U < items) next[u] = residual_of(a, p + (U + u) * row_step, o);
+                const float *sums = (const float *)lds + w * PART + (row + u * row_step) * RS + c;
+                z[u] = bias + *(const v4f *)sums;
+                if (a.gated) up[u] = bias_up + *(const v4f *)(sums + 8 * NO);
+#pragma unroll
+                for (int k = 1; k < KS; ++k) {
+                    z[u] += *(const v4f *)(sums + 4 * k * PART);
+                    if (a.gated) up[u] += *(const v4f *)(sums + 4 * k * PART + 8 * NO);
+                }
             }
-            finish_columns(a, p, o, z, up, res);
-            res = next;
-            row += row_step;
-            p += row_step;
+            finish_columns<U>(a, p, row_step, o, z, up, res);
+#pragma unroll
+            for (int u = 0; u < U; ++u) res[u] = next[u];
+            row += U * row_step;
+            p += U * row_step;
         }
         __builtin_amdgcn_wave_barrier();
     }
