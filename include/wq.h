@@ -363,7 +363,8 @@ wq_status_t wq_direct_forward(const wq_direct_plan_t *plan, void *stream, const 
  * overlap in time race (two streams, two captured graphs); with a workspace each they do not.  Everything
  * is enqueued on `stream`, may be captured into a graph, and is checked on the host first: a NULL
  * pointer, rows or a stride out of range, a misaligned tensor, an unknown type or activation ->
- * INVALID_ARG; a buffer smaller than the layout says -> WORKSPACE. */
+ * INVALID_ARG; a buffer smaller than the layout says -> WORKSPACE.  wq_direct_plan_tune does not
+ * apply to these calls: they choose by the call's rows. */
 typedef enum { WQ_FP32 = 0, WQ_BF16 = 1, WQ_FP16 = 2 } wq_type_t;
 
 /* z; max(z, 0); z / (1 + e^-z); z (1 + erf(z / sqrt 2)) / 2; z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
@@ -407,8 +408,9 @@ wq_status_t wq_linear_matmul(const wq_direct_plan_t *plan, void *stream, int row
                              int activation, int gated, int type, const void *residual_dev,
                              int64_t residual_stride, void *y_dev, int64_t y_stride);
 
-/* wq_linear_quantize followed by wq_linear_matmul; x, residual and y of one type.  What the workspace holds
- * afterwards is unspecified. */
+/* wq_linear_quantize followed by wq_linear_matmul, for a few thousand elements of x in one launch; x, residual and
+ * y of one type.  y_dev may be x_dev, residual_dev or both (with their strides); any other overlap is the caller's
+ * error.  What the workspace holds afterwards is unspecified. */
 wq_status_t wq_linear_forward(const wq_direct_plan_t *plan, void *stream, int rows, int type, const void *x_dev,
                               int64_t x_stride, const void *weight_blob_dev, size_t blob_bytes,
                               void *workspace_dev, size_t workspace_bytes, int activation, int gated,

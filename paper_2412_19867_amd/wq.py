@@ -526,8 +526,10 @@ class LinearPlan(DirectPlan):
         """The stream's handle; the call's tensors have to be on the current device."""
         if device != self._cuda.current_device():
             raise ValueError("expected tensors on the current device")
-        if stream is None and self._raw_stream is not None:
-            return self._raw_stream(device)
+        if stream is None:
+            return self._raw_stream(device) if self._raw_stream is not None else _stream_handle(None)
+        if stream.device.index != device:
+            raise ValueError("expected a stream of the tensors' device")
         return _stream_handle(stream)
 
     def _buffer(self, t, device, what):

@@ -157,7 +157,16 @@ PRODUCTS = [
     (1030, 1030, 640, 1280, 64, "silu", False, True),
     (2050, 2050, 128, 96, 32, "none", False, False),
     (4100, 4100, 64, 64, 64, "relu", True, True),
+    (16, 16, 512, 96, 64, "silu", True, True),
+    (8, 9, 1024, 48, 256, "relu", False, False),
+    (4, 4, 2048, 64, 512, "none", True, False),
+    (16, 16, 512, 31, 32, "none", False, True),
 ]
+
+# every kernel form, at sizes well inside the rules that choose it: (rows, weight rows) and whether the reduction has to be long
+FORMS = {"rows": (13, 96, False), "rows2": (101, 640, False), "teams4": (199, 2240, False), "teams2": (301, 4480, False),
+         "teams1": (641, 4480, False), "large": (2501, 4480, True)}
+SHORT = {32: 224, 64: 192, 128: 384, 256: 768, 512: 1536}   # 32, 64: the last stage of 128 bytes is not a whole one
 
 
 @pytest.mark.parametrize("bits", [8, 4], ids=["w8", "w4"])
@@ -188,6 +197,67 @@ def test_linear(wq, case, dtype, bits):
         check_product(y, z, S, Cin // g, act, gated, None if res is None else f32(res))
         if pad:
             assert bool(y.as_strided((n, pad), (outs + pad, 1), off + outs).isnan().all())
+
+
+@pytest.mark.parametrize("bits", [8, 4], ids=["w8", "w4"])
+@pytest.mark.parametrize("g", SHORT)
+@pytest.mark.parametrize("form", FORMS)
+def test_every_form_of_the_product(wq, form, g, bits):
+    """Each form with each group size, gated and not, with columns that nothing divides; the oracle on a sample of rows: the
+    ends, both sides of every kind of tile border, and some between."""
+    n, Cout, long_k = FORMS[form]
+    print(form, g, bits, flush=True)
+    rng = np.random.default_rng(g + bits)
+    Cin = 2048 if long_k and g >= 128 else SHORT[g]
+    for gated, less in ((True, 0), (False, 3)):
+        plan, blob, ws, (wcodes, wscales), b = layer(wq, rng, n, Cin, Cout - less, g, bits)
+        outs = Cout // 2 if gated else Cout - less
+        x = hidden(rng, n, Cin, "bf16")
+        y = torch.full((n, outs), float("nan"), dtype=torch.bfloat16, device="cuda")
+        res = torch.from_numpy(rng.standard_normal((n, outs)).astype(np.float32)).bfloat16()
+        plan.linear(x.cuda(), blob, ws, y, activation="silu", gated=gated, residual=res.cuda())
+        torch.cuda.synchronize()
+        assert bool(y.isfinite().all())
+        rows = sorted({r for r in (0, 1, 15, 16, 31, 32, 63, 64, 127, 128, 255, 256, n // 2, n - 2, n - 1) if r < n} |
+                      set(rng.integers(0, n, 12).tolist()))
+        codes, scales = oracle.quantize_pixels(f32(x[rows]), g)
+        z, S = lb.product(codes, scales, wcodes, wscales, b, g)
+        check_product(y[torch.tensor(rows, device="cuda")], z, S, Cin // g, "silu", gated, f32(res[rows]))
+
+
+def test_output_in_the_place_of_its_input(wq):
+    """x + f(x) written over x: by one row, where the product would read x itself, and by many."""
+    rng = np.random.default_rng(17)
+    for n in (1, 6, 70):
+        plan, blob, ws, (wcodes, wscales), b = layer(wq, rng, n, 512, 512, 64, 8)
+        x = hidden(rng, n, 512, "fp32")
+        z, S = lb.product(*oracle.quantize_pixels(f32(x), 64), wcodes, wscales, b, 64)
+        xd = x.cuda()
+        plan.linear(xd, blob, ws, xd, activation="gelu", residual=xd)
+        torch.cuda.synchronize()
+        check_product(xd, z, S, 8, "gelu", False, f32(x))
+
+
+def test_two_streams_at_once(wq):
+    """Calls on two streams with a workspace each, again and again without a wait between them: as if alone."""
+    rng = np.random.default_rng(23)
+    sides = []
+    for n, Cin, Cout, g, bits in ((300, 1024, 768, 64, 4), (7, 1024, 512, 128, 8)):
+        plan, blob, ws, _, _ = layer(wq, rng, n, Cin, Cout, g, bits)
+        x = hidden(rng, n, Cin, "bf16").cuda()
+        y = torch.empty((n, Cout), dtype=torch.bfloat16, device="cuda")
+        h = torch.empty_like(x)
+        plan.rms_norm_quantize(x, ws, residual=x, out=h)
+        plan.matmul(ws, blob, y, activation="relu")
+        torch.cuda.synchronize()
+        sides.append((plan, blob, ws, x, h, y, y.clone(), h.clone(), torch.cuda.Stream()))
+    for k in range(20):
+        for plan, blob, ws, x, h, y, *_, stream in sides:
+            plan.rms_norm_quantize(x, ws, residual=x, out=h, stream=stream)
+            plan.matmul(ws, blob, y, activation="relu", stream=stream)
+    torch.cuda.synchronize()
+    for plan, blob, ws, x, h, y, want_y, want_h, _ in sides:
+        assert torch.equal(y, want_y) and torch.equal(h, want_h)
 
 
 def test_rows_up_to_the_plans(wq):
