@@ -405,13 +405,17 @@ class DirectPlan:
         else:
             _check(lib().wq_direct_plan_create_bits(ctypes.byref(self._h), N, H, W, Cin, Cout, group_size,
                                                     weight_bits), "wq_direct_plan_create_bits")
-        self.layout = DirectLayout()
-        _check(lib().wq_direct_plan_layout(self._h, ctypes.byref(self.layout)), "wq_direct_plan_layout")
+        self.layout = self._read_layout()
+
+    def _read_layout(self):
+        layout = DirectLayout()
+        _check(lib().wq_direct_plan_layout(self._h, ctypes.byref(layout)), "wq_direct_plan_layout")
+        return layout
 
     def tune(self, splits: int):
         """Override how many waves share an output tile's reduction (wq_direct_plan_tune)."""
         _check(lib().wq_direct_plan_tune(self._h, int(splits)), "wq_direct_plan_tune")
-        _check(lib().wq_direct_plan_layout(self._h, ctypes.byref(self.layout)), "wq_direct_plan_layout")
+        self.layout = self._read_layout()
         return self
 
     @property
@@ -517,7 +521,7 @@ class LinearPlan(DirectPlan):
         super().__init__(rows, 1, 1, Cin, Cout, group_size, linear=True, weight_bits=weight_bits)
         self._rows, self._cin, self._cout = self.layout.P, self.layout.Cin, self.layout.Cout
         # a decoding step makes hundreds of these calls: what they look up is looked up once
-        self._tensor_type, self._uint8, self._cuda = torch.Tensor, torch.uint8, torch.cuda
+        self._tensor_type, self._uint8, self._fp32, self._cuda = torch.Tensor, torch.uint8, torch.float32, torch.cuda
         self._types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self._lib = lib()
@@ -590,10 +594,11 @@ class LinearPlan(DirectPlan):
         wp, wn = self._buffer(ws, dev, "workspace")
         gp = None
         if gamma is not None:
-            import torch
-            gp = _dev_ptr(gamma, torch.float32, "gamma", cin)
-            if gamma.get_device() != dev:
-                raise ValueError("gamma: expected a tensor on the device of the others")
+            if not isinstance(gamma, self._tensor_type) or not gamma.is_cuda or gamma.dtype != self._fp32 or not gamma.is_contiguous():
+                raise TypeError("gamma: expected a contiguous fp32 device tensor")
+            if gamma.numel() != cin or gamma.get_device() != dev:
+                raise ValueError(f"gamma: expected {cin} elements on the device of the others")
+            gp = gamma.data_ptr()
         _check(self._lib.wq_rms_norm_quantize(self._h, self._stream(stream, dev), n, code, xp, xs, rp, rs, gp, eps, op, os_, wp,
                                               wn), "wq_rms_norm_quantize")
 
