@@ -42,6 +42,14 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
     const int log2u = a.log2g > 7 ? a.log2g : 7, units = (a.Cin + (1 << log2u) - 1) >> log2u;
     const int c_beg = (ks * units / t.slices) << (log2u - 7), c_end = ((ks + 1) * units / t.slices) << (log2u - 7);
     const int steps = a.Cin / KSTEP;
+    // Neighbouring tiles walk their parts from different places on: from the same one they would ask for addresses that lie a
+    // power of two apart where Cin is one, all in a few of the memory's channels (16 rows 4096->2x8192 g 128 W8: in step
+    // 18.1 us, so 14.7; 4224->2x8192 14.6 either way).  The order of a column's sum depends on the column alone.
+    const int len = c_end - c_beg, spu = GS >= 256 ? 1 << (a.log2g - 7) : 1, first = len ? ob % (len / spu) * spu : 0;
+    auto chunk = [&](int i) {   // the i-th of the wave's chunks; past the last: that again
+        const int c = c_beg + first + min(i, len - 1);
+        return c < c_end ? c : c - len;
+    };
 
     unsigned vW[NE], vSW[NE], vX[NB], vSX[NB];
 #pragma unroll
@@ -64,8 +72,8 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
     int wv[D][NE][NK][WREGS], xv[FUSED ? 1 : D][NB][NK][XREGS];
     float swv[D][NE][NGS];
     float sxv[FUSED ? 1 : D][NB][NGS];
-    auto fetch = [&](int d, int c) {   // chunk c into slot d (a constant after unrolling); past the wave's part: its last one again
-        c = min(c, c_end - 1);
+    auto fetch = [&](int d, int i) {   // into slot d (a constant after unrolling)
+        const int c = chunk(i);
 #pragma unroll
         for (int k = 0; k < NK; ++k) {
             const int step = min(c * NK + k, steps - 1);
@@ -117,7 +125,8 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
             M[e][f] = v4f{0.f, 0.f, 0.f, 0.f};
             acc[e][f] = v4i{start, start, start, start};
         }
-    auto compute = [&](int d, int c) {
+    auto compute = [&](int d, int i) {
+        const int c = chunk(i);
         const int xd = FUSED ? 0 : d;
         if constexpr (FUSED) {
 #pragma unroll
@@ -200,10 +209,10 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
         load_piece(ks);
         __builtin_amdgcn_sched_barrier(0);
     }
-    if (c_beg < c_end) {
+    if (len) {
 #pragma unroll
         for (int d = 0; d < D; ++d) {
-            fetch(d, c_beg + d);
+            fetch(d, d);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -219,20 +228,20 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
         }
         __syncthreads();
     }
-    if (c_beg < c_end) {
-        int c = c_beg;
-        for (; c + D <= c_end; c += D) {   // whole rounds of the ring, then the rest
+    if (len) {
+        int i = 0;
+        for (; i + D <= len; i += D) {   // whole rounds of the ring, then the rest
 #pragma unroll
             for (int d = 0; d < D; ++d) {
-                compute(d, c + d);
+                compute(d, i + d);
                 __builtin_amdgcn_sched_barrier(0);
-                fetch(d, c + d + D);
+                fetch(d, i + d + D);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
 #pragma unroll
         for (int d = 0; d < D - 1; ++d)
-            if (c + d < c_end) compute(d, c + d);
+            if (i + d < len) compute(d, i + d);
     }
 
     // ---- the waves' sums through LDS, 16 rows at a time, then the epilogue ----
