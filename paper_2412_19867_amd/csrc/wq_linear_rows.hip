@@ -13,6 +13,11 @@ struct RArgs {
 // waves takes a contiguous part of K for all of them and asks for D chunks of 128 bytes of K ahead: with nothing staged, a
 // wave waits for nothing but its own loads, and the weights stream from memory in runs of the blob's order.
 // FUSED: the workgroup quantizes the rows of x itself, into LDS, while its first weights are on their way: a launch less.
+//   bound: the weights' bytes where there are many of them (16 rows, g 128, 8 bits: 4096->2x8192 14.3 us for 69 MB, 4.8 TB/s;
+//   8192->8192 g 256 13.9), else the length of one wave's chain of start, loads, sums and exchange (1024->1024 3.7 us in a
+//   sequence of launches; 8192->4096 W4 7.0 for 18 MB).  Six or eight chunks in flight, or six or eight waves, bring nothing
+//   (4096->4096 g 128 W4 with 4, 6, 8 chunks 4.9, 5.1, 5.4); 4-bit weights need two thirds of the time for half of the bytes, their
+//   loads being half as wide.
 template <int GS, bool W4, bool GATED, int NB, bool FUSED>
 __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, const RArgs t) {
     constexpr bool K64 = GS != 32;

@@ -28,6 +28,17 @@ struct wq_tile_grid {
 // 16 x 16 blocks; KS such teams share a tile's reduction, each a contiguous part of K.  A stage is SK bytes of K: the
 // operand blocks, in the MFMA's order in memory already, go straight into LDS with the scales of the groups that the
 // stage meets, into a ring of NST stages per team, NST - 1 of them in flight.
+//   z[p][o] = bias[o] + sum over groups G of float(P[p][o][G]) * (sw[o][G] * sx[p][G]), P the exact int32 product of a group: per 16 x 16
+//   block and group one MFMA per K-step and 12 vector instructions (sum to float, product of the scales, multiply-add; four
+//   values a lane).  The two do not overlap on a SIMD, so groups of 64 cap the matrix core at a third, of 128 at half.
+//   bound: issue.  4096x4096->2x8192 g 128 W4 330 us (1.66 POP/s): 262000 cycles of MFMA and 290 vector instructions per stage
+//   and wave, of which 192 are the sums and 48 unpack the weights, fill 89 % of the cycles at the 1.9 GHz that this load
+//   leaves.  A library's int8 product without scales runs at 2.0 POP/s here.
+//   wave tiles of 64 x 64: an operand byte read from LDS serves four blocks and a weight's unpacking four MFMAs; of 32 x 32 where tiles
+//   are few: 16 waves a CU count for more then (one wave a SIMD issues a vector instruction every seven cycles, two every
+//   three).  Wave tiles of 64 x 32 and 32 x 64 lie between the two everywhere (4096x4096->2x8192 W4 392, 403; 512x8192->4096
+//   35 like the others).
+//   Two stages suffice: three and four of the small tile's brought nothing, nor did reading a stage's operands a stage early.
 template <int GS, bool W4, int NO, int NB, int SK, int NST, int KS>
 __global__ __launch_bounds__(256 * KS, NO == 4 && SK == 64 ? (W4 ? 3 : 4) : 2) void k_linear_tile(const wq_linear_args a, const wq_tile_grid t) {
     constexpr bool K64 = GS != 32;
