@@ -333,13 +333,13 @@ wq_linear_args product_args(const wq_direct_plan_t *plan, int rows, const void *
     return a;
 }
 
-// Whether the product takes the rows of x as they are: a few thousand elements, in aligned pieces, and apart from y (which
-// some workgroups write while others still read x).  Every workgroup quantizes all of x then, which costs less than a
-// launch as long as that is two pieces a wave (us, 4-bit weights, g 128, both launches and one: 1x4096->4096 7.0, 5.5;
-// 1x8192->4096 9.4, 8.3; 2x4096->4096 7.1, 6.1; 4x4096->4096 7.1, 7.5; 8x4096->4096 7.1, 10.2).
+// Whether the product takes the rows of x as they are: up to 16384 elements, in aligned pieces, and apart from y (which some
+// workgroups write while others still read x).  Every workgroup quantizes all of x then.  us, 4-bit weights, g 128, two
+// launches and one, in a graph: 1x4096->4096 7.0, 5.5; 1x8192->4096 9.4, 8.3; 2x4096->4096 7.1, 6.1; 4x4096->4096 7.1, 7.5;
+// 8x4096->4096 7.1, 10.2.  Launched one by one from Python two take 10.2 at least and one 7, hence 16384 and not 8192.
 bool quantizes_itself(const wq_linear_args &a, const void *x, int64_t xs) {
     const int64_t e = type_size(a.type);
-    if (a.rows > 16 || a.rows * a.Cin > 8192 || (uintptr_t)x % 16 != 0 || (a.rows > 1 && xs * e % 16 != 0)) return false;
+    if (a.rows > 16 || a.rows * a.Cin > 16384 || (uintptr_t)x % 16 != 0 || (a.rows > 1 && xs * e % 16 != 0)) return false;
     const char *x0 = (const char *)x, *x1 = x0 + ((a.rows - 1) * xs + a.Cin) * e;
     const char *y0 = (const char *)a.y, *y1 = y0 + ((a.rows - 1) * a.ys + a.outs) * e;
     return x1 <= y0 || y1 <= x0;

@@ -161,6 +161,10 @@ PRODUCTS = [
     (8, 9, 1024, 48, 256, "relu", False, False),
     (4, 4, 2048, 64, 512, "none", True, False),
     (16, 16, 512, 31, 32, "none", False, True),
+    (16, 16, 1024, 64, 128, "gelu", True, False),   # the most that one launch quantizes and multiplies
+    (4, 4, 4096, 80, 512, "none", False, True),
+    (1, 1, 16384, 48, 64, "none", False, False),
+    (16, 16, 1056, 64, 32, "none", False, False),   # a little more
 ]
 
 # every kernel form, at sizes well inside the rules that choose it: (rows, weight rows) and whether the reduction has to be long
