@@ -333,18 +333,6 @@ wq_linear_args product_args(const wq_direct_plan_t *plan, int rows, const void *
     return a;
 }
 
-// Whether the product takes the rows of x as they are: up to 16384 elements, in aligned pieces, and apart from y (which some
-// workgroups write while others still read x).  Every workgroup quantizes all of x then.  us, 4-bit weights, g 128, two
-// launches and one, in a graph: 1x4096->4096 7.0, 5.5; 1x8192->4096 9.4, 8.3; 2x4096->4096 7.1, 6.1; 4x4096->4096 7.1, 7.5;
-// 8x4096->4096 7.1, 10.2.  Launched one by one from Python two take 10.2 at least and one 7, hence 16384 and not 8192.
-bool quantizes_itself(const wq_linear_args &a, const void *x, int64_t xs) {
-    const int64_t e = type_size(a.type);
-    if (a.rows > 16 || a.rows * a.Cin > 16384 || (uintptr_t)x % 16 != 0 || (a.rows > 1 && xs * e % 16 != 0)) return false;
-    const char *x0 = (const char *)x, *x1 = x0 + ((a.rows - 1) * xs + a.Cin) * e;
-    const char *y0 = (const char *)a.y, *y1 = y0 + ((a.rows - 1) * a.ys + a.outs) * e;
-    return x1 <= y0 || y1 <= x0;
-}
-
 // Which kernel multiplies: over 329 drawn layers of 17 to 4096 rows, 320 to 8192 input and 32 to 16384 output channels the rules
 // below are 1.5 % (geometric mean) from the best of the forms.  With n64 and n128 the numbers of tiles of 64 (128) weight
 // rows x 64 (128) rows of x; us of the forms on either side of each line:
@@ -357,18 +345,37 @@ bool quantizes_itself(const wq_linear_args &a, const void *x, int64_t xs) {
 //   tiles of 128: long reductions from 400 of them (4096x4096->2x8192 g 128: 64 427, 128 336; 512x4096->2x8192: 59.7, 51.3), where
 //     their prologue and epilogue weigh less (1740x896->10144 g 128: 47, 55); groups of up to 64 from 640, whose
 //     shorter stages leave room for more workgroups on a CU (4096x1280->2x5120 g 64: 130, 107)
-wq_status_t run_product(const wq_direct_plan *plan, const wq_linear_args &a, hipStream_t s) {
+struct Form {
+    int row_blocks;   // few rows: 16-row blocks of a workgroup, 1 or 2; 0: tiles
+    bool large;       // tiles of 128
+    int teams;        // of tiles of 64
+};
+
+Form choose_form(const wq_linear_args &a, int g) {
     const int Cout = a.gated ? 2 * a.outs : a.outs;
     auto tiles = [&](int n) { return (long)((Cout + n - 1) / n) * ((a.rows + n - 1) / n); };
-    const long n64 = tiles(64), n128 = tiles(128);
+    const long n64 = tiles(64), n128 = tiles(128), blocks = (long)((a.outs + 15) / 16) * ((a.rows + 15) / 16);
+    if (a.rows <= 32 || n64 <= 100) return {a.rows <= 16 || blocks <= 256 ? 1 : 2, false, 0};
+    return {0, g <= 64 ? n128 >= 640 : n128 >= 400 && a.Cin >= 2048, n64 <= 256 ? 4 : n64 <= 512 ? 2 : 1};
+}
+
+// Whether the product takes the rows of x as they are: up to 16384 elements of a workgroup's 16 rows, in aligned pieces, and
+// apart from y (which some workgroups write while others still read x).  Every workgroup quantizes its rows then.  us, 4-bit weights, g 128, two
+// launches and one, in a graph: 1x4096->4096 7.0, 5.5; 1x8192->4096 9.4, 8.3; 2x4096->4096 7.1, 6.1; 4x4096->4096 7.1, 7.5;
+// 8x4096->4096 7.1, 10.2.  Launched one by one from Python two take 10.2 at least and one 7, hence 16384 and not 8192.
+// Several blocks of rows, each quantized by the workgroups that multiply it: 60x512->800 g 256 6.3, 6.0; 24x1024->1024 g 64 6.4, 7.0.
+bool quantizes_itself(const wq_linear_args &a, const Form &form, const void *x, int64_t xs) {
+    const int64_t e = type_size(a.type);
+    if (form.row_blocks != 1 || (a.rows < 16 ? a.rows : 16) * (int64_t)a.Cin > 16384 || (uintptr_t)x % 16 != 0 || (a.rows > 1 && xs * e % 16 != 0)) return false;
+    const char *x0 = (const char *)x, *x1 = x0 + ((a.rows - 1) * xs + a.Cin) * e;
+    const char *y0 = (const char *)a.y, *y1 = y0 + ((a.rows - 1) * a.ys + a.outs) * e;
+    return x1 <= y0 || y1 <= x0;
+}
+
+wq_status_t run_product(const wq_direct_plan *plan, const wq_linear_args &a, const Form &form, hipStream_t s) {
     hipError_t e;
-    if (a.rows <= 32 || n64 <= 100) {
-        const bool one = a.rows <= 16 || (long)((a.outs + 15) / 16) * ((a.rows + 15) / 16) <= 256;
-        e = wq_launch_linear_rows(a, plan->g, plan->wbits, one ? 1 : 2, s);
-    } else {
-        const bool large = plan->g <= 64 ? n128 >= 640 : n128 >= 400 && a.Cin >= 2048;
-        e = (plan->wbits == 4 ? wq_launch_linear_tile4 : wq_launch_linear_tile8)(a, plan->g, large, n64 <= 256 ? 4 : n64 <= 512 ? 2 : 1, s);
-    }
+    if (form.row_blocks) e = wq_launch_linear_rows(a, plan->g, plan->wbits, form.row_blocks, s);
+    else e = (plan->wbits == 4 ? wq_launch_linear_tile4 : wq_launch_linear_tile8)(a, plan->g, form.large, form.teams, s);
     return e == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;
 }
 
@@ -418,7 +425,7 @@ wq_status_t wq_linear_matmul(const wq_direct_plan_t *plan, void *stream, int row
     if (st != WQ_OK || rows == 0) return st;
     wq_linear_args a = product_args(plan, rows, workspace_dev, weight_blob_dev, activation, gated, type, residual_dev,
                                     residual_stride, y_dev, y_stride);
-    return run_product(plan, a, (hipStream_t)stream);
+    return run_product(plan, a, choose_form(a, plan->g), (hipStream_t)stream);
 }
 
 wq_status_t wq_linear_forward(const wq_direct_plan_t *plan, void *stream, int rows, int type, const void *x_dev,
@@ -432,13 +439,14 @@ wq_status_t wq_linear_forward(const wq_direct_plan_t *plan, void *stream, int ro
     if (rows == 0) return WQ_OK;
     wq_linear_args a = product_args(plan, rows, workspace_dev, weight_blob_dev, activation, gated, type, residual_dev,
                                     residual_stride, y_dev, y_stride);
-    if (quantizes_itself(a, x_dev, x_stride)) {
+    const Form form = choose_form(a, plan->g);
+    if (quantizes_itself(a, form, x_dev, x_stride)) {
         a.x = x_dev; a.xs = x_stride;
     } else {
         st = wq_linear_quantize(plan, stream, rows, type, x_dev, x_stride, workspace_dev, workspace_bytes);
         if (st != WQ_OK) return st;
     }
-    return run_product(plan, a, (hipStream_t)stream);
+    return run_product(plan, a, form, (hipStream_t)stream);
 }
 
 }  // extern "C"

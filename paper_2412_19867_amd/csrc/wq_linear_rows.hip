@@ -69,10 +69,10 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
         vX[f] = ((unsigned)q * (unsigned)a.P + p) * KB;
         vSX[f] = p * 4u;
     }
-    // FUSED: codes [Cin / KB][rows][KB] and scales [groups][rows] of x in LDS
-    const int lrow = min(l16, last_row);
+    // FUSED: codes [Cin / KB][rows][KB] and scales [groups][rows] of the workgroup's rows of x in LDS
+    const int x_rows = min(16, a.rows - p0), lrow = min(l16, x_rows - 1);
     char *codes_s = (char *)part_s + t.x_off;
-    float *scales_s = (float *)(codes_s + a.rows * a.Cin);
+    float *scales_s = (float *)(codes_s + x_rows * a.Cin);
 
     int wv[D][NE][NK][WREGS], xv[FUSED ? 1 : D][NB][NK][XREGS];
     float swv[D][NE][NGS];
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
         if constexpr (FUSED) {
 #pragma unroll
             for (int k = 0; k < NK; ++k) {
-                const char *p = codes_s + ((min(c * NK + k, steps - 1) * 4 + q) * a.rows + lrow) * KB;
+                const char *p = codes_s + ((min(c * NK + k, steps - 1) * 4 + q) * x_rows + lrow) * KB;
                 if constexpr (K64) {
                     const v4i v = *(const v4i *)p;
                     xv[0][0][k][0] = v.x; xv[0][0][k][1] = v.y; xv[0][0][k][2] = v.z; xv[0][0][k][3] = v.w;
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
             }
 #pragma unroll
             for (int k = 0; k < NGS; ++k)
-                sxv[0][0][k] = scales_s[min(GS >= 256 ? (c * 128) >> a.log2g : c * NGS + k, groups - 1) * a.rows + lrow];
+                sxv[0][0][k] = scales_s[min(GS >= 256 ? (c * 128) >> a.log2g : c * NGS + k, groups - 1) * x_rows + lrow];
         }
         const bool done = GS < 256 || ((c + 1) * 128 & ((1 << a.log2g) - 1)) == 0;   // a group ends with this chunk
 #pragma unroll
@@ -198,14 +198,14 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
     };
 
     // x: pieces of 512 elements of a row, a wave's first one asked for ahead of the weights (loads come back in order)
-    const int chunks = (a.Cin + 511) / 512, pieces = FUSED ? a.rows * chunks : 0;
+    const int chunks = (a.Cin + 511) / 512, pieces = FUSED ? x_rows * chunks : 0;
     float v[8];
     auto load_piece = [&](int i) {
         const int c = i % chunks * 512 + lane * 8;
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = 0.f;
         if (i >= pieces || c >= a.Cin) return;
-        const long at = i / chunks * a.xs + c;
+        const long at = (p0 + i / chunks) * a.xs + c;
         if (a.type == WQ_FP32) load8((const float *)a.x + at, v);
         else if (a.type == WQ_BF16) load8((const __bf16 *)a.x + at, v);
         else load8((const _Float16 *)a.x + at, v);
@@ -228,8 +228,8 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
             float s;
             const uint2 codes = quantize_piece(v, 1 << a.log2g, s);
             if (c >= a.Cin) continue;
-            *(uint2 *)(codes_s + (c / KB * a.rows + row) * KB + c % KB) = codes;
-            if ((c & ((1 << a.log2g) - 1)) == 0) scales_s[(c >> a.log2g) * a.rows + row] = s;
+            *(uint2 *)(codes_s + (c / KB * x_rows + row) * KB + c % KB) = codes;
+            if ((c & ((1 << a.log2g) - 1)) == 0) scales_s[(c >> a.log2g) * x_rows + row] = s;
         }
         __syncthreads();
     }
@@ -280,7 +280,7 @@ void launch(const wq_linear_args &a, int slices, hipStream_t s) {
     t.total = t.nO * ((a.rows + 16 * NB - 1) / (16 * NB));
     t.per_xcd = (t.total + 7) / 8;
     t.x_off = slices * 16 * (16 * (GATED ? 2 : 1) + 4) * 4;
-    const size_t lds = t.x_off + (FUSED ? (size_t)a.rows * (a.Cin + 4 * (a.Cin >> a.log2g)) : 0);
+    const size_t lds = t.x_off + (FUSED ? (size_t)min(a.rows, 16) * (a.Cin + 4 * (a.Cin >> a.log2g)) : 0);
     hipLaunchKernelGGL((k_linear_rows<GS, W4, GATED, NB, FUSED>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * slices), lds, s, a, t);
 }
 
@@ -289,7 +289,7 @@ void launch(const wq_linear_args &a, int slices, hipStream_t s) {
 // the columns are many (1x4096->2x8192 W8 14.3, 18.0; 1x8192->8192 15.6, 14.1; 1x4096->4096 g 128 W4 6.3, 5.7).
 template <int GS, bool W4, bool GATED>
 void launch_nb(const wq_linear_args &a, int nb, hipStream_t s) {
-    if (a.x) launch<GS, W4, GATED, 1, true>(a, a.outs >= 8192 && a.rows * a.Cin <= 4096 ? 4 : 8, s);
+    if (a.x) launch<GS, W4, GATED, 1, true>(a, a.outs >= 8192 && a.rows <= 16 && a.rows * a.Cin <= 4096 ? 4 : 8, s);
     else if (nb == 1) launch<GS, W4, GATED, 1, false>(a, 4, s);
     else launch<GS, W4, GATED, 2, false>(a, 4, s);
 }

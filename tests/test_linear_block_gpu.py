@@ -165,6 +165,9 @@ PRODUCTS = [
     (4, 4, 4096, 80, 512, "none", False, True),
     (1, 1, 16384, 48, 64, "none", False, False),
     (16, 16, 1056, 64, 32, "none", False, False),   # a little more
+    (50, 50, 768, 288, 32, "silu", True, True),     # several blocks of rows, each quantized by the workgroups that multiply it
+    (100, 130, 1024, 150, 256, "none", False, False),
+    (33, 33, 64, 1000, 64, "relu", False, True),
 ]
 
 # every kernel form, at sizes well inside the rules that choose it: (rows, weight rows) and whether the reduction has to be long
