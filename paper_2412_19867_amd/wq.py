@@ -405,17 +405,13 @@ class DirectPlan:
         else:
             _check(lib().wq_direct_plan_create_bits(ctypes.byref(self._h), N, H, W, Cin, Cout, group_size,
                                                     weight_bits), "wq_direct_plan_create_bits")
-        self.layout = self._read_layout()
-
-    def _read_layout(self):
-        layout = DirectLayout()
-        _check(lib().wq_direct_plan_layout(self._h, ctypes.byref(layout)), "wq_direct_plan_layout")
-        return layout
+        self.layout = DirectLayout()
+        _check(lib().wq_direct_plan_layout(self._h, ctypes.byref(self.layout)), "wq_direct_plan_layout")
 
     def tune(self, splits: int):
         """Override how many waves share an output tile's reduction (wq_direct_plan_tune)."""
         _check(lib().wq_direct_plan_tune(self._h, int(splits)), "wq_direct_plan_tune")
-        self.layout = self._read_layout()
+        _check(lib().wq_direct_plan_layout(self._h, ctypes.byref(self.layout)), "wq_direct_plan_layout")
         return self
 
     @property
