@@ -402,7 +402,8 @@ wq_status_t wq_linear_quantize(const wq_direct_plan_t *plan, void *stream, int r
  * (a gated feed-forward layer: the first half of the weight rows is the gate's; Cout has to be a multiple of 32
  * then, else UNSUPPORTED).  Computed in fp32, rounded once to `type`, which y and residual (NULL: none) share;
  * y_dev may be residual_dev itself with the same stride.  NOT_PREPARED before wq_direct_weight_prepare.  The sums over groups
- * are fp32; their order, and with it the last bits of y, may depend on `rows`. */
+ * are fp32; their order, and with it the last bits of y, may depend on `rows`.  Unlike the library's other calls this one
+ * gives what the formulas give for infinities and NaN in z; an infinity in x makes its group's scale infinite and its row of z NaN. */
 wq_status_t wq_linear_matmul(const wq_direct_plan_t *plan, void *stream, int rows, const void *workspace_dev,
                              size_t workspace_bytes, const void *weight_blob_dev, size_t blob_bytes,
                              int activation, int gated, int type, const void *residual_dev,

@@ -43,7 +43,8 @@ __device__ __forceinline__ float gelu(float z) {
     G = __builtin_fmaf(G, t, 0.0409632139f);
     G = __builtin_fmaf(G, t, 0.123935819f);
     G = __builtin_fmaf(G, t, -0.000844957307f);
-    return __builtin_fmaf(-x, __builtin_amdgcn_exp2f(x * x * -0.721347520f) * G, fmaxf(z, 0.0f));
+    const float y = __builtin_fmaf(-x, __builtin_amdgcn_exp2f(x * x * -0.721347520f) * G, fmaxf(z, 0.0f));
+    return z > 64.0f ? z : y;   // (the same but for z = inf, where y is inf times 0)
 }
 
 // N values at a time: one (uniform) choice for all of them.
@@ -52,7 +53,7 @@ __device__ __forceinline__ void activate(float (&z)[N], int act) {
     switch (act) {
         case WQ_ACT_RELU:
 #pragma unroll
-            for (int i = 0; i < N; ++i) z[i] = fmaxf(z[i], 0.0f);
+            for (int i = 0; i < N; ++i) z[i] = z[i] <= 0.0f ? 0.0f : z[i];   // (a maximum would make 0 of a NaN)
             break;
         case WQ_ACT_SILU:
 #pragma unroll

@@ -1,0 +1,73 @@
+"""Values at which the linear layer's surroundings can go wrong: infinities and NaN, activations by place."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+ACTS = ("none", "relu", "silu", "gelu", "gelu_tanh")
+ROWS = {"rows": 1, "tiles": 130}   # the two kernels' epilogues
+
+
+def through(wq, z, act, n, gated=False):
+    """act(z) [n][len(z)] in fp32, as a layer's epilogue computes it: rows of zeros, so that the products are the bias."""
+    C = z.numel()
+    assert C % 4096 == 0   # enough columns for the tiled kernels at 130 rows
+    bias = torch.cat((z, torch.ones(C))) if gated else z
+    plan = wq.LinearPlan(n, 32, bias.numel(), 32)
+    blob, ws = plan.alloc_blob(), plan.alloc_workspace()
+    plan.weight_prepare(torch.ones(bias.numel(), 32, device="cuda"), bias.cuda(), blob)
+    y = torch.full((n, C), 7.0, device="cuda")
+    plan.linear(torch.zeros(n, 32, device="cuda"), blob, ws, y, activation=act, gated=gated)
+    return y.cpu()
+
+
+def exact(z, act):
+    """The activation's formula in 64 bits; gelu by erfc, which keeps the negative tail's digits."""
+    z = z.double()
+    if act == "relu":
+        return torch.where(z <= 0, torch.zeros_like(z), z)
+    if act == "silu":
+        return z / (1.0 + torch.exp(-z))
+    if act == "gelu":
+        return z * torch.erfc(z * -math.sqrt(0.5)) * 0.5
+    if act == "gelu_tanh":
+        return z / (1.0 + torch.exp(-2.0 * math.sqrt(2.0 / math.pi) * (z + 0.044715 * z ** 3)))
+    return z
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("act", ACTS)
+def test_activations_of_infinities_and_nan(wq, act, rows, gated):
+    """What the formulas give: NaN stays NaN, +inf stays +inf, -inf is -inf, 0 (relu) or the undefined -inf times 0."""
+    print(act, rows, gated, flush=True)
+    special = torch.tensor([math.nan, math.inf, -math.inf, 3e38, -3e38, 0.0, -0.0, 1e30, -1e30, 1e-30])
+    z = torch.zeros(4096)
+    z[5:4085].view(-1, 10)[:, :] = special
+    y = through(wq, z, act, ROWS[rows], gated)
+    want = exact(z, act).float()
+    for r in range(y.shape[0]):
+        assert torch.equal(y[r].isnan(), want.isnan())
+        assert torch.equal(y[r].nan_to_num(1.0, 2e38, -2e38).abs() > 1e37, want.nan_to_num(1.0, 2e38, -2e38).abs() > 1e37)
+        assert torch.equal(y[r].isinf(), want.isinf()) and torch.equal(y[r] > 0, want > 0)
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_infinities_and_nan_stay_in_their_row(wq, act):
+    """An infinity in a row of x makes that row of y NaN, through every activation, and leaves the others alone."""
+    for n, Cin, Cout in ((3, 256, 64), (40, 2048, 64), (130, 256, 4096)):
+        print(act, n, flush=True)
+        gen = torch.Generator().manual_seed(n)
+        plan = wq.LinearPlan(n, Cin, Cout, 64)
+        blob, ws = plan.alloc_blob(), plan.alloc_workspace()
+        plan.weight_prepare(torch.randn(Cout, Cin, generator=gen).cuda(), None, blob)
+        x = torch.randn(n, Cin, generator=gen).cuda()
+        want, y = torch.empty(n, Cout, device="cuda"), torch.empty(n, Cout, device="cuda")
+        plan.linear(x, blob, ws, want, activation=act)
+        x[1, 70] = math.inf
+        plan.linear(x, blob, ws, y, activation=act)
+        rest = [r for r in range(n) if r != 1]
+        assert bool(y[1].isnan().all()) and torch.equal(y[rest], want[rest]) and bool(want.isfinite().all())
