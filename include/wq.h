@@ -367,7 +367,9 @@ wq_status_t wq_direct_forward(const wq_direct_plan_t *plan, void *stream, const 
  * apply to these calls: they choose by the call's rows. */
 typedef enum { WQ_FP32 = 0, WQ_BF16 = 1, WQ_FP16 = 2 } wq_type_t;
 
-/* z; max(z, 0); z / (1 + e^-z); z (1 + erf(z / sqrt 2)) / 2; z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+/* z; max(z, 0); z / (1 + e^-z); z (1 + erf(z / sqrt 2)) / 2; z (1 + tanh(u)) / 2, u = sqrt(2 / pi) (z + 0.044715 z^3).
+ * In fp32, relative to the value: silu within (8 + 1.3 |z|) 2^-24, gelu within (24 + 2 z^2) 2^-24 down to z = -10 (2^-80 in
+ * absolute terms below), gelu_tanh within (8 + 7 |u|) 2^-24; values below 2^-118 may be flushed to zero. */
 typedef enum {
     WQ_ACT_NONE = 0,
     WQ_ACT_RELU = 1,

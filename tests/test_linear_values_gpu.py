@@ -55,6 +55,34 @@ def test_activations_of_infinities_and_nan(wq, act, rows, gated):
         assert torch.equal(y[r].isinf(), want.isinf()) and torch.equal(y[r] > 0, want > 0)
 
 
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("act", ACTS)
+def test_activations_by_place(wq, act, rows):
+    """The error of each value against itself, not against the largest: what include/wq.h states, from counted roundings.  u = 2^-24.
+      silu: the exponent's argument is off by 1.22 u of itself (its constant by 0.22), the exponential and the reciprocal by a unit
+        in the last place (2 u) each, the sum and the product by u: 6 u + 1.22 u |z|;
+      gelu_tanh: a square, a multiply-add and a product form the argument, their constants are off by 0.33 u: 3.4 u of it;
+      gelu: z^2 / 2 is off by 2.3 u of itself, the polynomial by 15 u at most down to -8 and by 21 u to -10 (its rounding steps, the
+        reciprocal's error in its argument, and 1.2 u to -6, 8 u to -8, 14 u to -10 of the fit), the exponential by 2 u, two products and the sum by u each;
+      the hardware flushes reciprocals below 2^-126, so that z times one is off by 2^-118 at most (|z| < 256)."""
+    print(act, rows, flush=True)
+    z = torch.cat((torch.linspace(-14, 14, 40000), torch.linspace(-120, -14, 8000), torch.linspace(14, 200, 1536),
+                   torch.logspace(-36, 0, 8000), -torch.logspace(-36, 0, 8000)))
+    y = through(wq, z, act, ROWS[rows])
+    want, wide, u = exact(z, act), z.double(), 2.0 ** -24
+    arg = 2.0 * math.sqrt(2.0 / math.pi) * (wide.abs() + 0.044715 * wide.abs() ** 3)
+    steps = {"none": 0.0 * wide, "relu": 0.0 * wide, "silu": 8.0 + 1.3 * wide.abs(), "gelu": 24.0 + 2.0 * wide ** 2,
+             "gelu_tanh": 8.0 + 3.5 * arg}[act]
+    bound = steps * u * want.abs() + (2.0 ** -118 if act in ("silu", "gelu_tanh") else 2.0 ** -149)
+    if act == "gelu":
+        bound = torch.where(wide < -10, 2.0 ** -80 * torch.ones_like(wide), bound)
+    for r in (0, y.shape[0] - 1):
+        off = (y[r].double() - want).abs()
+        worst = int((off / bound).argmax())
+        print("row %d: %.3f of the bound at %g" % (r, float(off[worst] / bound[worst]), float(z[worst])), flush=True)
+        assert bool((off <= bound).all())
+
+
 @pytest.mark.parametrize("act", ACTS)
 def test_infinities_and_nan_stay_in_their_row(wq, act):
     """An infinity in a row of x makes that row of y NaN, through every activation, and leaves the others alone."""
