@@ -393,7 +393,8 @@ wq_status_t wq_rms_norm_quantize(const wq_direct_plan_t *plan, void *stream, int
                                  int64_t residual_stride, const float *gamma_dev, double eps, void *sum_dev,
                                  int64_t sum_stride, void *workspace_dev, size_t workspace_bytes);
 
-/* wq_direct_quantize for rows of any type: the codes and scales of x (converted to fp32, which is exact). */
+/* wq_direct_quantize for rows of any type: the codes and scales of x (converted to fp32, which is exact).  Both calls
+ * give a group with a NaN a scale of zero and one with an infinity (and no NaN) an infinite one, wherever the rows lie. */
 wq_status_t wq_linear_quantize(const wq_direct_plan_t *plan, void *stream, int rows, int type,
                                const void *x_dev, int64_t x_stride, void *workspace_dev, size_t workspace_bytes);
 

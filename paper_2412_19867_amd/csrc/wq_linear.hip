@@ -206,7 +206,7 @@ __global__ __launch_bounds__(256) void k_quantize_row(const QArgs a) {
     const int KB = a.g == 32 ? 8 : 16;
     for (int gi = w; gi < a.Cin / a.g; gi += 4) {
         float v[8];
-        float top = 0.0f;
+        uint32_t top = 0;   // (the magnitudes' bits, as everywhere: a NaN is the largest)
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const int j = lane + 64 * k, c = gi * a.g + j;
@@ -215,12 +215,12 @@ __global__ __launch_bounds__(256) void k_quantize_row(const QArgs a) {
             const float h = load(c);
             if (NORM && sum) sum[c] = (T)h;
             v[k] = NORM ? (a.gamma ? h * rho * a.gamma[c] : h * rho) : h;
-            top = fmaxf(top, fabsf(v[k]));
+            top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
         }
 #pragma unroll
-        for (int m = 32; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+        for (int m = 32; m > 0; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
         float s, r;
-        group_scale(top, s, r);
+        group_scale(__uint_as_float(top), s, r);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const int j = lane + 64 * k, c = gi * a.g + j;

@@ -83,6 +83,35 @@ def test_activations_by_place(wq, act, rows):
         assert bool((off <= bound).all())
 
 
+@pytest.mark.parametrize("g", [32, 64, 128, 256, 512])
+def test_codes_of_infinities_and_nan(wq, g):
+    """Rows with infinities and NaN have the codes and scales that the older quantizer gives them, wherever the rows lie: a group
+    with a NaN a scale of zero, one with an infinity an infinite scale, and every other group its own."""
+    print(g, flush=True)
+    R, C = 6, 4 * g
+    gen = torch.Generator().manual_seed(g)
+    x = torch.randn(R, C, generator=gen)
+    x[0, 3] = math.nan
+    x[1, g + 5] = math.inf
+    x[2, 2 * g + 1], x[2, 2 * g + 9] = -math.inf, math.nan
+    x[3, C - 1] = -math.nan
+    x[4] = math.nan
+    plan = wq.LinearPlan(R, C, 32, g)
+    ws = plan.alloc_workspace()
+    plan.quantize(x.cuda(), ws)
+    codes, scales = plan.workspace_views(ws)
+    kept = scales.cpu()
+    assert kept[0, 0] == 0 and kept[1, 1] == math.inf and kept[2, 2] == 0 and kept[3, 3] == 0 and not kept[4].any() and kept[5].all()
+    for pad, off in ((0, 0), (16, 4), (3, 1)):
+        v = torch.zeros(off + R * (C + pad), device="cuda")[off:].view(R, C + pad)[:, :C]
+        v.copy_(x)
+        ws.fill_(0xA5)
+        plan.quantize_rows(v, ws)
+        c, s = plan.workspace_views(ws)
+        assert torch.equal(s.cpu(), kept), (pad, off)
+        assert torch.equal(c, codes), (pad, off)
+
+
 @pytest.mark.parametrize("act", ACTS)
 def test_infinities_and_nan_stay_in_their_row(wq, act):
     """An infinity in a row of x makes that row of y NaN, through every activation, and leaves the others alone."""
