@@ -32,8 +32,9 @@ __device__ __forceinline__ double wave_sum(double v) {
     return v;
 }
 
-// The norm's factor.  The squares of fp32 numbers are exact in 64 bits and their sum is off by some 1e-16, so
-// that the factor, rounded once to fp32, does not depend on the order of the sum, nor do the codes behind it.
+// The norm's factor.  The squares of fp32 numbers are exact in 64 bits and their sum is off by some 1e-16 of itself: the factor,
+// rounded once to fp32, is the exact one's unless that lies so close to the middle between two fp32 numbers.  For such rows
+// too it is the same from every kernel, which all add in one order.
 // (Two Newton steps take the hardware's estimate of 1 / sqrt to the last places of 64 bits; a square root and a division
 // are five times as many instructions, one after the other.)
 __device__ __forceinline__ float norm_factor(double squares, int Cin, double eps) {
@@ -182,26 +183,40 @@ __global__ __launch_bounds__(512) void k_quantize_pieces(const QArgs a, int wpr,
     }
 }
 
-// Rows of any alignment and any length, read twice: a workgroup to a row, a wave to a group at a time.
+// Rows of any alignment and any length, read twice: a workgroup to a row, a wave to a group at a time.  The squares are added
+// in the order of k_quantize_pieces, each wave in the place of every fourth of its wpr: a row's factor depends on its values
+// alone, not on where they lie.  us, rows one element off (aligned ones with k_quantize_pieces): norm with residual 4096x8192
+// fp32 188 (90), 4096x4096 bf16 66 (24), 16x4096 14 (4); codes alone 98 (39), 32 (12.5), 9 (3); 2x65536 bf16 243, 512x65536 370.
+// bound: addresses, one element a lane and load in the second reading, and stores of single bytes.
 template <int TYPE, bool NORM>
-__global__ __launch_bounds__(256) void k_quantize_row(const QArgs a) {
+__global__ __launch_bounds__(256) void k_quantize_row(const QArgs a, int wpr) {
     using T = typename Elem<TYPE>::type;
-    __shared__ double part[4];
+    __shared__ double part[8];
     const int p = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const T *x = (const T *)a.x + (size_t)p * a.xs, *res = a.res ? (const T *)a.res + (size_t)p * a.rs : nullptr;
     T *sum = a.sum ? (T *)a.sum + (size_t)p * a.hs : nullptr;
     auto load = [&](int c) { return res ? (float)x[c] + (float)res[c] : (float)x[c]; };
     float rho = 1.0f;
     if constexpr (NORM) {
-        double q = 0.0;
-        for (int c = tid; c < a.Cin; c += 256) {
-            const double h = (double)load(c);
-            q += h * h;
+        for (int i = w; i < wpr; i += 4) {
+            double q = 0.0;
+            for (int c = i * 512 + lane * 8; c < a.Cin; c += 512 * wpr) {
+                float h[8], t[8] = {};
+                load8_anywhere<T>(x + c, h);
+                if (res) load8_anywhere<T>(res + c, t);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const double d = (double)(res ? h[j] + t[j] : h[j]);
+                    q = __builtin_fma(d, d, q);
+                }
+            }
+            q = wave_sum(q);
+            if (lane == 0) part[i] = q;
         }
-        q = wave_sum(q);
-        if (lane == 0) part[w] = q;
         __syncthreads();
-        rho = norm_factor(part[0] + part[1] + part[2] + part[3], a.Cin, a.eps);
+        double squares = 0.0;
+        for (int i = 0; i < wpr; ++i) squares += part[i];
+        rho = norm_factor(squares, a.Cin, a.eps);
     }
     const int KB = a.g == 32 ? 8 : 16;
     for (int gi = w; gi < a.Cin / a.g; gi += 4) {
@@ -244,15 +259,16 @@ void launch_quantize(const QArgs &a, hipStream_t s) {
     const int64_t e = type_size(TYPE);
     auto whole = [&](const void *t, int64_t stride) { return !t || ((uintptr_t)t % 16 == 0 && (a.rows == 1 || stride * e % 16 == 0)); };
     const bool pieces = whole(a.x, a.xs) && whole(a.res, a.rs) && whole(a.sum, a.hs) && ((uintptr_t)a.gamma % 16 == 0);
-    if (!pieces || (NORM && a.Cin > 32768)) {
-        hipLaunchKernelGGL((k_quantize_row<TYPE, NORM>), dim3((unsigned)a.rows), dim3(256), 0, s, a);
-        return;
-    }
     const int chunks = (a.Cin + 511) / 512;   // of a wave's 512 elements
     int wpr = 1, V = 1, R = !NORM && (long)a.rows * chunks >= 4096 ? 2 : 1;
+    if (NORM)
+        while (wpr < chunks && wpr < 8) wpr *= 2;
+    if (!pieces || (NORM && a.Cin > 32768)) {
+        hipLaunchKernelGGL((k_quantize_row<TYPE, NORM>), dim3((unsigned)a.rows), dim3(256), 0, s, a, wpr);
+        return;
+    }
     long units = (a.rows + R - 1) / R;
     if (NORM) {
-        while (wpr < chunks && wpr < 8) wpr *= 2;
         while (V * wpr < chunks) V *= 2;
     } else {
         units *= chunks;

@@ -41,6 +41,14 @@ __device__ __forceinline__ void load8(const T *p, float (&v)[8]) {
         for (int j = 0; j < 16 / (int)sizeof(T); ++j) v[k * 16 / sizeof(T) + j] = (float)t[j];
     }
 }
+// The same of elements that are aligned to themselves only.
+template <typename T>
+__device__ __forceinline__ void load8_anywhere(const T *p, float (&v)[8]) {
+    T t[8];
+    __builtin_memcpy(t, p, sizeof t);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (float)t[j];
+}
 // (stored past the caches: what comes next reads the codes)
 template <typename T>
 __device__ __forceinline__ void store8(T *p, const float (&v)[8]) {

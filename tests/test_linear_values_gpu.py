@@ -128,3 +128,34 @@ def test_infinities_and_nan_stay_in_their_row(wq, act):
         plan.linear(x, blob, ws, y, activation=act)
         rest = [r for r in range(n) if r != 1]
         assert bool(y[1].isnan().all()) and torch.equal(y[rest], want[rest]) and bool(want.isfinite().all())
+
+
+@pytest.mark.parametrize("C,g", [(4096, 128), (1280, 64), (512, 512), (32, 32), (13312, 256), (32768, 512)])
+def test_the_norms_codes_do_not_depend_on_where_rows_lie(wq, C, g):
+    """Rows in aligned pieces and rows at odd addresses go through different kernels.  Where the norm's factor lies next to the
+    middle between two fp32 numbers, the last place of a sum of squares decides it: eps is moved over such a place in the smallest
+    steps of 64 bits, and all codes and scales stay alike."""
+    plan = wq.LinearPlan(1, C, 32, g)
+    even, odd = plan.alloc_workspace(), plan.alloc_workspace()
+    even.zero_(), odd.zero_()   # (what lies between codes and scales is compared too)
+    moved = 0
+    for seed in range(12):
+        print(C, g, seed, flush=True)
+        x = np.random.default_rng(seed).standard_normal(C).astype(np.float32)
+        mean = math.fsum((x.astype(np.float64) ** 2).tolist()) / C
+        low = np.float32(1.0 / math.sqrt(mean + 1e-3))
+        middle = (float(low) + float(np.nextafter(low, np.float32(0)))) / 2.0   # factors round differently on its two sides
+        eps = 1.0 / (middle * middle) - mean
+        step = float(np.spacing(1.0 / (middle * middle)))
+        a = torch.from_numpy(x).cuda().view(1, C)
+        flat = torch.zeros(C + 1, device="cuda")
+        flat[1:] = a[0]
+        scales = set()
+        for k in range(-16, 17):
+            plan.rms_norm_quantize(a, even, eps=eps + k * step)
+            plan.rms_norm_quantize(flat[1:].view(1, C), odd, eps=eps + k * step)
+            same = torch.equal(even, odd)
+            assert same, (seed, k)
+            scales.add(float(plan.workspace_views(even)[1][0, 0]))
+        moved += len(scales) == 2
+    assert moved >= 6   # such places were met
