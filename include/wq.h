@@ -362,8 +362,8 @@ wq_status_t wq_direct_forward(const wq_direct_plan_t *plan, void *stream, const 
  * 0..rows-1 alone, rows = 0 launches nothing (tensor pointers may then be NULL).  Calls on one workspace that
  * overlap in time race (two streams, two captured graphs); with a workspace each they do not.  Everything
  * is enqueued on `stream`, may be captured into a graph, and is checked on the host first: a NULL
- * pointer, rows or a stride out of range, a misaligned tensor, an unknown type or activation ->
- * INVALID_ARG; a buffer smaller than the layout says -> WORKSPACE.  wq_direct_plan_tune does not
+ * pointer, rows or a stride out of range, a misaligned tensor, a workspace or blob not aligned to 16 bytes,
+ * an unknown type or activation -> INVALID_ARG; a buffer smaller than the layout says -> WORKSPACE.  wq_direct_plan_tune does not
  * apply to these calls: they choose by the call's rows. */
 typedef enum { WQ_FP32 = 0, WQ_BF16 = 1, WQ_FP16 = 2 } wq_type_t;
 

@@ -246,6 +246,9 @@ __global__ __launch_bounds__(256) void k_quantize_row(const QArgs a, int wpr) {
 }
 
 // ------------------------------------------------------------ product
+// Workspace and blob are moved in aligned pieces of 16 bytes, and the loads into LDS drop the low bits of an address.
+bool good_buffer(const void *b) { return b && (uintptr_t)b % 16 == 0; }
+
 bool good_type(int type) { return type == WQ_FP32 || type == WQ_BF16 || type == WQ_FP16; }
 
 // A tensor [rows][cols] of the type with a row stride: aligned to its elements, rows that do not overlap.
@@ -316,7 +319,7 @@ int ilog2(int v) {
 wq_status_t check_product(const wq_direct_plan_t *plan, int rows, const void *workspace, size_t workspace_bytes,
                           const void *blob, size_t blob_bytes, int activation, int gated, int type, const void *res,
                           int64_t res_stride, const void *y, int64_t y_stride) {
-    if (!plan || !workspace || !blob || (rows != 0 && !y)) return WQ_ERR_INVALID_ARG;
+    if (!plan || !good_buffer(workspace) || !good_buffer(blob) || (rows != 0 && !y)) return WQ_ERR_INVALID_ARG;
     if (plan->taps != 1) return WQ_ERR_UNSUPPORTED;
     if (rows < 0 || rows > plan->P || !good_type(type) || activation < WQ_ACT_NONE || activation > WQ_ACT_GELU_TANH ||
         (gated != 0 && gated != 1))
@@ -404,7 +407,7 @@ wq_status_t wq_rms_norm_quantize(const wq_direct_plan_t *plan, void *stream, int
                                  int64_t x_stride, const void *residual_dev, int64_t residual_stride,
                                  const float *gamma_dev, double eps, void *sum_dev, int64_t sum_stride,
                                  void *workspace_dev, size_t workspace_bytes) {
-    if (!plan || (rows != 0 && !x_dev) || !workspace_dev) return WQ_ERR_INVALID_ARG;
+    if (!plan || (rows != 0 && !x_dev) || !good_buffer(workspace_dev)) return WQ_ERR_INVALID_ARG;
     if (plan->taps != 1) return WQ_ERR_UNSUPPORTED;
     if (rows < 0 || rows > plan->P || !good_type(type) || !(eps >= FLT_MIN && eps <= DBL_MAX))
         return WQ_ERR_INVALID_ARG;
@@ -422,7 +425,7 @@ wq_status_t wq_rms_norm_quantize(const wq_direct_plan_t *plan, void *stream, int
 
 wq_status_t wq_linear_quantize(const wq_direct_plan_t *plan, void *stream, int rows, int type, const void *x_dev,
                                int64_t x_stride, void *workspace_dev, size_t workspace_bytes) {
-    if (!plan || (rows != 0 && !x_dev) || !workspace_dev) return WQ_ERR_INVALID_ARG;
+    if (!plan || (rows != 0 && !x_dev) || !good_buffer(workspace_dev)) return WQ_ERR_INVALID_ARG;
     if (plan->taps != 1) return WQ_ERR_UNSUPPORTED;
     if (rows < 0 || rows > plan->P || !good_type(type) || !good_rows(x_dev, x_stride, rows, plan->Cin, type))
         return WQ_ERR_INVALID_ARG;
