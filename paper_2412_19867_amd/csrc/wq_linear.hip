@@ -8,6 +8,7 @@
 #include <float.h>
 
 #include "wq_linear_args.h"
+#include "wq_linear_form.h"
 #include "wq_quantize_piece.h"
 
 namespace {
@@ -262,20 +263,14 @@ void launch_quantize(const QArgs &a, hipStream_t s) {
     const int64_t e = type_size(TYPE);
     auto whole = [&](const void *t, int64_t stride) { return !t || ((uintptr_t)t % 16 == 0 && (a.rows == 1 || stride * e % 16 == 0)); };
     const bool pieces = whole(a.x, a.xs) && whole(a.res, a.rs) && whole(a.sum, a.hs) && ((uintptr_t)a.gamma % 16 == 0);
-    const int chunks = (a.Cin + 511) / 512;   // of a wave's 512 elements
-    int wpr = 1, V = 1, R = !NORM && (long)a.rows * chunks >= 4096 ? 2 : 1;
-    if (NORM)
-        while (wpr < chunks && wpr < 8) wpr *= 2;
-    if (!pieces || (NORM && a.Cin > 32768)) {
+    const wq_quantize_form form = wq_quantize_choose_form(a.rows, a.Cin, NORM, pieces);
+    const int wpr = form.wpr, V = form.V, R = form.R;
+    if (!form.pieces) {
         hipLaunchKernelGGL((k_quantize_row<TYPE, NORM>), dim3((unsigned)a.rows), dim3(256), 0, s, a, wpr);
         return;
     }
     long units = (a.rows + R - 1) / R;
-    if (NORM) {
-        while (V * wpr < chunks) V *= 2;
-    } else {
-        units *= chunks;
-    }
+    if (!NORM) units *= (a.Cin + 511) / 512;
     const int waves = wpr < 4 ? 4 : wpr, upw = waves / wpr;
     const long blocks = (units + upw - 1) / upw, share = (blocks + 7) / 8;
     const unsigned run = (unsigned)(NORM && share > 16 ? 16 : share);
@@ -352,46 +347,21 @@ wq_linear_args product_args(const wq_direct_plan_t *plan, int rows, const void *
     return a;
 }
 
-// Which kernel multiplies: over 329 drawn layers of 17 to 4096 rows, 320 to 8192 input and 32 to 16384 output channels the rules
-// below are 1.5 % (geometric mean) from the best of the forms.  With n64 and n128 the numbers of tiles of 64 (128) weight
-// rows x 64 (128) rows of x; us of the forms on either side of each line:
-//   rows: one 16-row block a workgroup up to 16 rows, else for up to 256 blocks of 16 columns x 16 rows
-//     (57x1920->1440 g 128, 360 blocks: one 6.7, two 5.5; 55x3328->800 g 32, 200: 7.7, 8.8), two beyond
-//   tiles from 33 rows and 100 tiles of 64 (75x1792->2x3808 g 256, 238: rows 10.5, tiles 8.9; 68x5888->2x1904 g 64, 120: 15.3, 17.9)
-//   tiles of 64: four teams share a reduction up to 256 tiles (128x8192->4096 g 128: four 19.2, two 23.4, one 35.3), two
-//     up to 512 (1001x2048->2040 g 256: 16.5, 13.6, 15.6), else one (1024x4096->4096 g 64: 52.5, 44.8, 42.8): CUs with
-//     eight to sixteen waves
-//   tiles of 128: long reductions from 400 of them (4096x4096->2x8192 g 128: 64 427, 128 336; 512x4096->2x8192: 59.7, 51.3), where
-//     their prologue and epilogue weigh less (1740x896->10144 g 128: 47, 55); groups of up to 64 from 640, whose
-//     shorter stages leave room for more workgroups on a CU (4096x1280->2x5120 g 64: 130, 107)
-struct Form {
-    int row_blocks;   // few rows: 16-row blocks of a workgroup, 1 or 2; 0: tiles
-    bool large;       // tiles of 128
-    int teams;        // of tiles of 64
-};
-
-Form choose_form(const wq_linear_args &a, int g) {
-    const int Cout = a.gated ? 2 * a.outs : a.outs;
-    auto tiles = [&](int n) { return (long)((Cout + n - 1) / n) * ((a.rows + n - 1) / n); };
-    const long n64 = tiles(64), n128 = tiles(128), blocks = (long)((a.outs + 15) / 16) * ((a.rows + 15) / 16);
-    if (a.rows <= 32 || n64 <= 100) return {a.rows <= 16 || blocks <= 256 ? 1 : 2, false, 0};
-    return {0, g <= 64 ? n128 >= 640 : n128 >= 400 && a.Cin >= 2048, n64 <= 256 ? 4 : n64 <= 512 ? 2 : 1};
+wq_linear_form choose_form(const wq_linear_args &a, int g) {
+    return wq_linear_choose_form(a.rows, a.Cin, a.gated ? 2 * a.outs : a.outs, a.outs, g);
 }
 
-// Whether the product takes the rows of x as they are: up to 16384 elements of a workgroup's 16 rows, in aligned pieces, and
-// apart from y (which some workgroups write while others still read x).  Every workgroup quantizes its rows then.  us, 4-bit weights, g 128, two
-// launches and one, in a graph: 1x4096->4096 7.0, 5.5; 1x8192->4096 9.4, 8.3; 2x4096->4096 7.1, 6.1; 4x4096->4096 7.1, 7.5;
-// 8x4096->4096 7.1, 10.2.  Launched one by one from Python two take 10.2 at least and one 7, hence 16384 and not 8192.
-// Several blocks of rows, each quantized by the workgroups that multiply it: 60x512->800 g 256 6.3, 6.0; 24x1024->1024 g 64 6.4, 7.0.
-bool quantizes_itself(const wq_linear_args &a, const Form &form, const void *x, int64_t xs) {
+// Whether the product takes the rows of x as they are: few of them, in aligned pieces, and apart from y, which some workgroups
+// write while others still read x.
+bool quantizes_itself(const wq_linear_args &a, const wq_linear_form &form, const void *x, int64_t xs) {
     const int64_t e = type_size(a.type);
-    if (form.row_blocks != 1 || (a.rows < 16 ? a.rows : 16) * (int64_t)a.Cin > 16384 || (uintptr_t)x % 16 != 0 || (a.rows > 1 && xs * e % 16 != 0)) return false;
+    if (!wq_linear_takes_rows(form, a.rows, a.Cin) || (uintptr_t)x % 16 != 0 || (a.rows > 1 && xs * e % 16 != 0)) return false;
     const char *x0 = (const char *)x, *x1 = x0 + ((a.rows - 1) * xs + a.Cin) * e;
     const char *y0 = (const char *)a.y, *y1 = y0 + ((a.rows - 1) * a.ys + a.outs) * e;
     return x1 <= y0 || y1 <= x0;
 }
 
-wq_status_t run_product(const wq_direct_plan *plan, const wq_linear_args &a, const Form &form, hipStream_t s) {
+wq_status_t run_product(const wq_direct_plan *plan, const wq_linear_args &a, const wq_linear_form &form, hipStream_t s) {
     hipError_t e;
     if (form.row_blocks) e = wq_launch_linear_rows(a, plan->g, plan->wbits, form.row_blocks, s);
     else e = (plan->wbits == 4 ? wq_launch_linear_tile4 : wq_launch_linear_tile8)(a, plan->g, form.large, form.teams, s);
@@ -458,7 +428,7 @@ wq_status_t wq_linear_forward(const wq_direct_plan_t *plan, void *stream, int ro
     if (rows == 0) return WQ_OK;
     wq_linear_args a = product_args(plan, rows, workspace_dev, weight_blob_dev, activation, gated, type, residual_dev,
                                     residual_stride, y_dev, y_stride);
-    const Form form = choose_form(a, plan->g);
+    const wq_linear_form form = choose_form(a, plan->g);
     if (quantizes_itself(a, form, x_dev, x_stride)) {
         a.x = x_dev; a.xs = x_stride;
     } else {

@@ -1,5 +1,6 @@
 // The quantized linear layer's product for few rows (down to one: decoding): the weights are what is read.
 #include "wq_linear_args.h"
+#include "wq_linear_form.h"
 #include "wq_quantize_piece.h"
 
 namespace {
@@ -284,14 +285,12 @@ void launch(const wq_linear_args &a, int slices, hipStream_t s) {
     hipLaunchKernelGGL((k_linear_rows<GS, W4, GATED, NB, FUSED>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * slices), lds, s, a, t);
 }
 
-// Waves to a workgroup: four stream the weights as fast as eight with fewer sums to add (us at 1 to 16 rows, 4096->4096 g 128
-// W4 4.9, 5.4; 5120->5120 g 32 W8 11.5, 13.9).  Eight quantize x in half the time, which is what counts unless x is short and
-// the columns are many (1x4096->2x8192 W8 14.3, 18.0; 1x8192->8192 15.6, 14.1; 1x4096->4096 g 128 W4 6.3, 5.7).
 template <int GS, bool W4, bool GATED>
 void launch_nb(const wq_linear_args &a, int nb, hipStream_t s) {
-    if (a.x) launch<GS, W4, GATED, 1, true>(a, a.outs >= 8192 && a.rows <= 16 && a.rows * a.Cin <= 4096 ? 4 : 8, s);
-    else if (nb == 1) launch<GS, W4, GATED, 1, false>(a, 4, s);
-    else launch<GS, W4, GATED, 2, false>(a, 4, s);
+    const int waves = wq_linear_row_waves(a.x != nullptr, a.rows, a.Cin, a.outs);
+    if (a.x) launch<GS, W4, GATED, 1, true>(a, waves, s);
+    else if (nb == 1) launch<GS, W4, GATED, 1, false>(a, waves, s);
+    else launch<GS, W4, GATED, 2, false>(a, waves, s);
 }
 
 template <int GS, bool W4>
