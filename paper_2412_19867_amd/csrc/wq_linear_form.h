@@ -3,8 +3,8 @@
 #pragma once
 
 // ---- the product ----
-// Over 329 drawn layers of 17 to 4096 rows, 320 to 8192 input and 32 to 16384 output channels the rules
-// below are 1.5 % (geometric mean) from the best of the forms.  With n64 and n128 the numbers of tiles of 64 (128) weight
+// Over 355 drawn layers of 17 to 4096 rows, 256 to 8192 input and 32 to 16384 output channels the rules
+// below are 1.5 % (geometric mean) from the best of the forms, 28 % at most.  With n64 and n128 the numbers of tiles of 64 (128) weight
 // rows x 64 (128) rows of x; us of the forms on either side of each line:
 //   rows: one 16-row block a workgroup up to 16 rows, else for up to 256 blocks of 16 columns x 16 rows
 //     (57x1920->1440 g 128, 360 blocks: one 6.7, two 5.5; 55x3328->800 g 32, 200: 7.7, 8.8), two beyond
@@ -39,10 +39,14 @@ inline bool wq_linear_takes_rows(const wq_linear_form &form, int rows, int Cin) 
 }
 
 // Waves to a workgroup of the kernel for few rows: four stream the weights as fast as eight with fewer sums to add (us at 1 to 16
-// rows, 4096->4096 g 128 W4 4.9, 5.4; 5120->5120 g 32 W8 11.5, 13.9).  Eight quantize x in half the time, which is what counts unless x is short and
-// the columns are many (1x4096->2x8192 W8 14.3, 18.0; 1x8192->8192 15.6, 14.1; 1x4096->4096 g 128 W4 6.3, 5.7).
-inline int wq_linear_row_waves(bool takes_rows, int rows, int Cin, int outs) {
-    return takes_rows && !(outs >= 8192 && rows <= 16 && rows * Cin <= 4096) ? 8 : 4;
+// rows, 4096->4096 g 128 W4 4.9, 5.4; 5120->5120 g 32 W8 11.5, 13.9).  Where they quantize x first, eight take half the time for
+// it.  That counts from some 2000 elements on while the workgroups of eight are all on the card at once, up to 512
+// blocks of 16 weight rows, and later the more blocks there are.  us with four, eight: 1x8192->8192 W8 15.5, 14.1; 1x4096->4096 W4 6.2, 5.6;
+// 1x5120->2x13824 W8 31.6, 37.6; 1x4096->2x8192 W8 14.2, 17.9.  Over 360 drawn layers 0.5 % from the better of the
+// two, 9 % at most.
+inline int wq_linear_row_waves(bool takes_rows, int rows, int Cin, int Cout) {
+    const long elements = (long)(rows < 16 ? rows : 16) * Cin, blocks = (long)((Cout + 15) / 16) * ((rows + 15) / 16);
+    return takes_rows && elements >= (blocks <= 512 ? 2048 : 10240 + 8 * (blocks - 512)) ? 8 : 4;
 }
 
 // ---- norm, quantization ----

@@ -287,7 +287,7 @@ void launch(const wq_linear_args &a, int slices, hipStream_t s) {
 
 template <int GS, bool W4, bool GATED>
 void launch_nb(const wq_linear_args &a, int nb, hipStream_t s) {
-    const int waves = wq_linear_row_waves(a.x != nullptr, a.rows, a.Cin, a.outs);
+    const int waves = wq_linear_row_waves(a.x != nullptr, a.rows, a.Cin, GATED ? 2 * a.outs : a.outs);
     if (a.x) launch<GS, W4, GATED, 1, true>(a, waves, s);
     else if (nb == 1) launch<GS, W4, GATED, 1, false>(a, waves, s);
     else launch<GS, W4, GATED, 2, false>(a, waves, s);

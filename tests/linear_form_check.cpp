@@ -8,9 +8,9 @@
 
 #include "wq_linear_form.h"
 
-static std::string product(const wq_linear_form &f, bool itself, int rows, int Cin, int outs) {
+static std::string product(const wq_linear_form &f, bool itself, int rows, int Cin, int Cout) {
     if (!f.row_blocks) return f.large ? "tiles128" : "tiles64 " + std::to_string(f.teams);
-    return "rows" + std::to_string(f.row_blocks) + " x" + std::to_string(wq_linear_row_waves(itself, rows, Cin, outs)) + (itself ? " itself" : "");
+    return "rows" + std::to_string(f.row_blocks) + " x" + std::to_string(wq_linear_row_waves(itself, rows, Cin, Cout)) + (itself ? " itself" : "");
 }
 
 int main() {
@@ -22,7 +22,7 @@ int main() {
         if (p) {
             const int outs = v[4] ? v[2] / 2 : v[2];
             const wq_linear_form f = wq_linear_choose_form(v[0], v[1], v[2], outs, v[3]);
-            std::cout << product(f, wq_linear_takes_rows(f, v[0], v[1]), v[0], v[1], outs) << ", " << product(f, false, v[0], v[1], outs) << "\n";
+            std::cout << product(f, wq_linear_takes_rows(f, v[0], v[1]), v[0], v[1], v[2]) << ", " << product(f, false, v[0], v[1], v[2]) << "\n";
         } else {
             const wq_quantize_form f = wq_quantize_choose_form(v[0], v[1], v[2], v[3]);
             if (f.pieces) std::cout << "pieces " << f.wpr << " " << f.V << " " << f.R << "\n";

@@ -42,6 +42,14 @@ def test_product_cases_take_the_forms_that_they_name(ask):
         assert got == want, question
 
 
+@pytest.mark.parametrize("layer,waves", [((1, 5120, 27648, 128, 1), 4), ((1, 8192, 28672, 128, 1), 4), ((2, 4096, 16384, 128, 0), 4),
+                                         ((1, 4096, 14336, 128, 0), 4), ((4, 2048, 12288, 128, 0), 4), ((1, 8192, 8192, 128, 0), 8),
+                                         ((2, 2048, 8192, 64, 0), 8), ((1, 4096, 4096, 128, 0), 8), ((1, 2048, 4096, 64, 0), 8)])
+def test_waves_of_one_launch_follow_the_measured_side(ask, layer, waves):
+    """Layers whose two sides were measured."""
+    assert ask([("product", *layer)])[0].split(",")[0] == f"rows1 x{waves} itself"
+
+
 def test_every_product_kernel_is_reached(ask):
     """Forms of the product x group sizes (256 and 512 share their code, but not how a group ends) x gated; each with both widths."""
     cases = list(product_cases())
