@@ -412,8 +412,8 @@ wq_status_t wq_linear_matmul(const wq_direct_plan_t *plan, void *stream, int row
                              int activation, int gated, int type, const void *residual_dev,
                              int64_t residual_stride, void *y_dev, int64_t y_stride);
 
-/* wq_linear_quantize followed by wq_linear_matmul, where rows and columns are few in one launch; x, residual and
- * y of one type.  y_dev may be x_dev, residual_dev or both (with their strides); any other overlap is the caller's
+/* wq_linear_quantize followed by wq_linear_matmul, with the same bits in y, where rows and columns are few in one launch;
+ * x, residual and y of one type.  y_dev may be x_dev, residual_dev or both (with their strides); any other overlap is the caller's
  * error.  What the workspace holds afterwards is unspecified. */
 wq_status_t wq_linear_forward(const wq_direct_plan_t *plan, void *stream, int rows, int type, const void *x_dev,
                               int64_t x_stride, const void *weight_blob_dev, size_t blob_bytes,

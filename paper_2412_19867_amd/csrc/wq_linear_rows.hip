@@ -6,14 +6,16 @@
 namespace {
 
 struct RArgs {
-    int slices, nO, total, per_xcd;   // waves that share a tile's reduction, tiles along channels, their number, the share of each XCD
-    int x_off;                        // FUSED: bytes of LDS before the codes of x
+    int waves, nO, total, per_xcd;   // waves to a workgroup, tiles along channels, their number, the share of each XCD
 };
+
+constexpr int kSlices = 4;   // waves that share a tile's reduction (others only help to quantize x)
 
 // A workgroup owns 16 columns of y (gated: and the 16 weight rows that go with them in the second half) x 16 NB rows; each of its
 // waves takes a contiguous part of K for all of them and asks for D chunks of 128 bytes of K ahead: with nothing staged, a
 // wave waits for nothing but its own loads, and the weights stream from memory in runs of the blob's order.
-// FUSED: the workgroup quantizes the rows of x itself, into LDS, while its first weights are on their way: a launch less.
+// FUSED: the workgroup quantizes the rows of x itself, into LDS, while its first weights are on their way: a launch less.  Eight
+// waves may do that; four of them multiply, so that the sums are those of two launches, bit for bit.
 //   bound: the weights' bytes where there are many of them (16 rows, g 128, 8 bits: 4096->2x8192 14.3 us for 69 MB, 4.8 TB/s;
 //   8192->8192 g 256 13.9), else the length of one wave's chain of start, loads, sums and exchange (1024->1024 3.7 us in a
 //   sequence of launches; 8192->4096 W4 7.0 for 18 MB).  Six or eight chunks in flight, or six or eight waves, bring nothing
@@ -27,7 +29,8 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
     constexpr int D = NB == 1 ? 4 : 2;              // chunks in flight
     constexpr int WREGS = K64 ? (W4 ? 2 : 4) : (W4 ? 1 : 2), XREGS = K64 ? 4 : 2;
     constexpr int RS = 16 * NE + 4;
-    extern __shared__ __attribute__((aligned(16))) float part_s[];   // [waves][16][RS]
+    constexpr int XOFF = kSlices * 16 * RS * 4;     // FUSED: bytes of LDS before the codes of x
+    extern __shared__ __attribute__((aligned(16))) float part_s[];   // [kSlices][16][RS]
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, q = lane >> 4;
     const int ks = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int logical = (int)(blockIdx.x & 7u) * t.per_xcd + (int)(blockIdx.x >> 3);
@@ -46,7 +49,7 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
 
     // the wave's part of K: whole groups, and whole chunks of 128 bytes where groups are shorter
     const int log2u = a.log2g > 7 ? a.log2g : 7, units = (a.Cin + (1 << log2u) - 1) >> log2u;
-    const int c_beg = (ks * units / t.slices) << (log2u - 7), c_end = ((ks + 1) * units / t.slices) << (log2u - 7);
+    const int c_beg = (min(ks, kSlices) * units / kSlices) << (log2u - 7), c_end = (min(ks + 1, kSlices) * units / kSlices) << (log2u - 7);
     const int steps = a.Cin / KSTEP;
     // Neighbouring tiles walk their parts from different places on: from the same one they would ask for addresses that lie a
     // power of two apart where Cin is one, all in a few of the memory's channels (16 rows 4096->2x8192 g 128 W8: in step
@@ -72,7 +75,7 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
     }
     // FUSED: codes [Cin / KB][rows][KB] and scales [groups][rows] of the workgroup's rows of x in LDS
     const int x_rows = min(16, a.rows - p0), lrow = min(l16, x_rows - 1);
-    char *codes_s = (char *)part_s + t.x_off;
+    char *codes_s = (char *)part_s + XOFF;
     float *scales_s = (float *)(codes_s + x_rows * a.Cin);
 
     int wv[D][NE][NK][WREGS], xv[FUSED ? 1 : D][NB][NK][XREGS];
@@ -223,7 +226,7 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
         }
     }
     if constexpr (FUSED) {
-        for (int i = ks; i < pieces; i += t.slices) {
+        for (int i = ks; i < pieces; i += t.waves) {
             if (i != ks) load_piece(i);
             const int row = i / chunks, c = i % chunks * 512 + lane * 8;
             float s;
@@ -256,7 +259,8 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
     for (int f = 0; f < NB; ++f) {
         if (f) __syncthreads();   // the rows before have been read
 #pragma unroll
-        for (int e = 0; e < NE; ++e) *(v4f *)&mine[l16 * RS + 16 * e + 4 * q] = M[e][f];
+        for (int e = 0; e < NE; ++e)
+            if (!FUSED || ks < kSlices) *(v4f *)&mine[l16 * RS + 16 * e + 4 * q] = M[e][f];
         __syncthreads();
         const int row = tid >> 2, c = (tid & 3) * 4, p = p0 + 16 * f + row, o = ob * 16 + c;
         if (tid >= 64 || p >= a.rows || o >= a.outs) continue;
@@ -264,7 +268,7 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
         const v4f res[1] = {residual_of(a, p, o)};
         v4f z[1] = {*(const v4f *)s + *(const v4f *)(a.bias + o)}, up[1] = {};   // (the bias is padded as the weights are)
         if constexpr (GATED) up[0] = *(const v4f *)(s + 16) + *(const v4f *)(a.bias + a.outs + o);
-        for (int k = 1; k < t.slices; ++k) {
+        for (int k = 1; k < kSlices; ++k) {
             s += 16 * RS;
             z[0] += *(const v4f *)s;
             if constexpr (GATED) up[0] += *(const v4f *)(s + 16);
@@ -274,15 +278,14 @@ __global__ __launch_bounds__(512) void k_linear_rows(const wq_linear_args a, con
 }
 
 template <int GS, bool W4, bool GATED, int NB, bool FUSED>
-void launch(const wq_linear_args &a, int slices, hipStream_t s) {
+void launch(const wq_linear_args &a, int waves, hipStream_t s) {
     RArgs t;
-    t.slices = slices;
+    t.waves = waves;
     t.nO = (a.outs + 15) / 16;
     t.total = t.nO * ((a.rows + 16 * NB - 1) / (16 * NB));
     t.per_xcd = (t.total + 7) / 8;
-    t.x_off = slices * 16 * (16 * (GATED ? 2 : 1) + 4) * 4;
-    const size_t lds = t.x_off + (FUSED ? (size_t)min(a.rows, 16) * (a.Cin + 4 * (a.Cin >> a.log2g)) : 0);
-    hipLaunchKernelGGL((k_linear_rows<GS, W4, GATED, NB, FUSED>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * slices), lds, s, a, t);
+    const size_t lds = kSlices * 16 * (16 * (GATED ? 2 : 1) + 4) * 4 + (FUSED ? (size_t)min(a.rows, 16) * (a.Cin + 4 * (a.Cin >> a.log2g)) : 0);
+    hipLaunchKernelGGL((k_linear_rows<GS, W4, GATED, NB, FUSED>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * waves), lds, s, a, t);
 }
 
 template <int GS, bool W4, bool GATED>

@@ -48,6 +48,23 @@ def test_product_of_few_rows(wq, case, g, bits):
             check_product(y, z, S, Cin // g, "silu", gated, f32(res))
 
 
+@pytest.mark.parametrize("bits", [8, 4], ids=["w8", "w4"])
+@pytest.mark.parametrize("g", SHORT)
+def test_one_launch_has_the_bits_of_two(wq, g, bits):
+    """linear() adds a column's groups in the order of matmul(), whichever quantizes the rows."""
+    for n, Cin, Cout in ((1, 4 * SHORT[g], 544), (3, SHORT[g], 8224), (9, SHORT[g], 96), (16, 1024, 64), (40, SHORT[g], 160), (2, 4096, 96),
+                         (90, SHORT[g], 1920), (300, SHORT[g], 4480)):
+        print(n, Cin, Cout, g, bits, flush=True)
+        plan, blob, ws, _, _ = layer(wq, np.random.default_rng(n), n, Cin, Cout, g, bits)
+        x = hidden(np.random.default_rng(Cin), n, Cin, "fp32").cuda()
+        for gated in (False, True):
+            y = [torch.full((n, Cout // 2 if gated else Cout), float("nan"), device="cuda") for _ in range(2)]
+            plan.linear(x, blob, ws, y[0], activation="gelu", gated=gated)
+            plan.quantize_rows(x, ws)
+            plan.matmul(ws, blob, y[1], activation="gelu", gated=gated)
+            assert bool(y[0].isfinite().all()) and torch.equal(*y), (n, Cin, Cout, gated)
+
+
 # rows, rows of the plan, Cin, g: two rows a wave, an odd number of rows and of a chunk's elements among them
 MANY = [(1367, 1400, 1312, 32), (4096, 4097, 480, 32), (2049, 2050, 1088, 64), (4097, 4100, 512, 512), (2051, 2051, 896, 128),
         (1025, 1030, 1792, 256), (257, 300, 8192, 64), (4098, 4098, 32, 32)]
