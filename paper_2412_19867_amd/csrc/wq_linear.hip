@@ -351,11 +351,18 @@ wq_linear_form choose_form(const wq_linear_args &a, int g) {
     return wq_linear_choose_form(a.rows, a.Cin, a.gated ? 2 * a.outs : a.outs, a.outs, g);
 }
 
+bool is_captured(hipStream_t s) {
+    hipStreamCaptureStatus status;
+    if (hipStreamIsCapturing(s, &status) == hipSuccess) return status != hipStreamCaptureStatusNone;
+    (void)hipGetLastError();   // (the question's own: the launch that follows has its answer checked)
+    return false;
+}
+
 // Whether the product takes the rows of x as they are: few of them, in aligned pieces, and apart from y, which some workgroups
 // write while others still read x.
-bool quantizes_itself(const wq_linear_args &a, const wq_linear_form &form, const void *x, int64_t xs) {
+bool quantizes_itself(const wq_linear_args &a, const wq_linear_form &form, const void *x, int64_t xs, hipStream_t s) {
     const int64_t e = type_size(a.type);
-    if (!wq_linear_takes_rows(form, a.rows, a.Cin) || (uintptr_t)x % 16 != 0 || (a.rows > 1 && xs * e % 16 != 0)) return false;
+    if (!wq_linear_takes_rows(form, a.rows, a.Cin, false) || (!wq_linear_takes_rows(form, a.rows, a.Cin, true) && is_captured(s)) || (uintptr_t)x % 16 != 0 || (a.rows > 1 && xs * e % 16 != 0)) return false;
     const char *x0 = (const char *)x, *x1 = x0 + ((a.rows - 1) * xs + a.Cin) * e;
     const char *y0 = (const char *)a.y, *y1 = y0 + ((a.rows - 1) * a.ys + a.outs) * e;
     return x1 <= y0 || y1 <= x0;
@@ -429,7 +436,7 @@ wq_status_t wq_linear_forward(const wq_direct_plan_t *plan, void *stream, int ro
     wq_linear_args a = product_args(plan, rows, workspace_dev, weight_blob_dev, activation, gated, type, residual_dev,
                                     residual_stride, y_dev, y_stride);
     const wq_linear_form form = choose_form(a, plan->g);
-    if (quantizes_itself(a, form, x_dev, x_stride)) {
+    if (quantizes_itself(a, form, x_dev, x_stride, (hipStream_t)stream)) {
         a.x = x_dev; a.xs = x_stride;
     } else {
         st = wq_linear_quantize(plan, stream, rows, type, x_dev, x_stride, workspace_dev, workspace_bytes);

@@ -29,13 +29,13 @@ inline wq_linear_form wq_linear_choose_form(int rows, int Cin, int Cout, int out
     return {0, g <= 64 ? n128 >= 640 : n128 >= 400 && Cin >= 2048, n64 <= 256 ? 4 : n64 <= 512 ? 2 : 1};
 }
 
-// Whether the product may take rows of x as they are, as far as sizes go: up to 16384 elements of a workgroup's 16 rows.  Every workgroup
-// quantizes its rows then.  us, 4-bit weights, g 128, two
-// launches and one, in a graph: 1x4096->4096 7.0, 5.5; 1x8192->4096 9.4, 8.3; 2x4096->4096 7.1, 6.1; 4x4096->4096 7.1, 7.5;
-// 8x4096->4096 7.1, 10.2.  Launched one by one from Python two take 10.2 at least and one 7, hence 16384 and not 8192.
-// Several blocks of rows, each quantized by the workgroups that multiply it: 60x512->800 g 256 6.3, 6.0; 24x1024->1024 g 64 6.4, 7.0.
-inline bool wq_linear_takes_rows(const wq_linear_form &form, int rows, int Cin) {
-    return form.row_blocks == 1 && (rows < 16 ? rows : 16) * (long)Cin <= 16384;
+// Whether the product may take rows of x as they are, as far as sizes go: up to 16384 elements of a workgroup's 16 rows, every
+// workgroup quantizing its own.  A launch more costs some 2 us of the card's time and 4 of the host's, elements cost the card alone: a
+// stream that is being captured has only the first to save and draws the line at 12288.  us of one launch and of two in a graph,
+// one by one from Python: 1x8192->4096 W4 8.8, 9.5, 7.9, 11.2; 64x640->640 6.4, 6.2, 6.9, 11.4; 3x4096->4096 W8 8.0, 8.9, 7.3, 11.6; 5x2560->6912 gated
+// W4 7.8, 7.7, 7.3, 11.4; 16x1024->1024 6.3, 6.2, 6.8, 11.1; 4x4096->4096 W4 7.9, 7.1, 7.3, 11.1; 1x16384->4096 W4 13.5, 12.4, 12.3, 11.6.
+inline bool wq_linear_takes_rows(const wq_linear_form &form, int rows, int Cin, bool captured) {
+    return form.row_blocks == 1 && (rows < 16 ? rows : 16) * (long)Cin <= (captured ? 12288 : 16384);
 }
 
 // Waves to a workgroup of the kernel for few rows.  Four multiply: they stream the weights as fast as eight with fewer sums to add

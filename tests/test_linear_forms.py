@@ -50,6 +50,15 @@ def test_waves_of_one_launch_follow_the_measured_side(ask, layer, waves):
     assert ask([("product", *layer)])[0].split(",")[0] == f"rows1 x{waves} itself"
 
 
+@pytest.mark.parametrize("layer,launches", [((4, 4096, 4096, 128, 0), 2), ((24, 1024, 1024, 64, 0), 2), ((8, 2048, 2048, 128, 0), 2),
+                                            ((1, 16384, 4096, 128, 0), 2), ((1, 8192, 4096, 128, 0), 1), ((3, 4096, 4096, 128, 0), 1),
+                                            ((60, 512, 800, 256, 0), 1)])
+def test_a_graph_gets_the_form_that_takes_less_of_the_cards_time(ask, layer, launches):
+    """Layers whose two sides were measured in a graph; launched one by one, where a launch costs the host more, all take one."""
+    assert ask([("captured", *layer)])[0].split(",")[0].endswith("itself") == (launches == 1)
+    assert ask([("product", *layer)])[0].split(",")[0].endswith("itself")
+
+
 def test_every_product_kernel_is_reached(ask):
     """Forms of the product x group sizes (256 and 512 share their code, but not how a group ends) x gated; each with both widths."""
     cases = list(product_cases())

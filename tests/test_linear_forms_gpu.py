@@ -65,6 +65,33 @@ def test_one_launch_has_the_bits_of_two(wq, g, bits):
             assert bool(y[0].isfinite().all()) and torch.equal(*y), (n, Cin, Cout, gated)
 
 
+def test_captured_calls_of_both_forms(wq):
+    """A graph of calls on either side of its own limit for one launch, replayed between eager passes: the same bits."""
+    calls = []
+    for n, Cin, Cout, g, bits in ((4, 4096, 256, 128, 4), (24, 1024, 96, 64, 8), (3, 4096, 96, 128, 8), (1, 16384, 64, 512, 4), (1, 12320, 64, 32, 8)):
+        print(n, Cin, Cout, g, bits, flush=True)
+        plan, blob, ws, _, _ = layer(wq, np.random.default_rng(n), n, Cin, Cout, g, bits)
+        x = hidden(np.random.default_rng(Cin), n, Cin, "bf16").cuda()
+        calls.append((plan, x, blob, ws, torch.empty((n, Cout), dtype=torch.bfloat16, device="cuda")))
+
+    def run():
+        for plan, x, blob, ws, y in calls:
+            plan.linear(x, blob, ws, y, activation="silu", residual=None)
+
+    run()
+    torch.cuda.synchronize()
+    want = [c[4].clone() for c in calls]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for k in range(5):
+        for c in calls:
+            c[4].fill_(float("nan"))
+        graph.replay() if k % 2 == 0 else run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(c[4], w) for c, w in zip(calls, want)), k
+
+
 # rows, rows of the plan, Cin, g: two rows a wave, an odd number of rows and of a chunk's elements among them
 MANY = [(1367, 1400, 1312, 32), (4096, 4097, 480, 32), (2049, 2050, 1088, 64), (4097, 4100, 512, 512), (2051, 2051, 896, 128),
         (1025, 1030, 1792, 256), (257, 300, 8192, 64), (4098, 4098, 32, 32)]
