@@ -405,7 +405,9 @@ wq_status_t wq_linear_quantize(const wq_direct_plan_t *plan, void *stream, int r
  * (a gated feed-forward layer: the first half of the weight rows is the gate's; Cout has to be a multiple of 32
  * then, else UNSUPPORTED).  Computed in fp32, rounded once to `type`, which y and residual (NULL: none) share;
  * y_dev may be residual_dev itself with the same stride.  NOT_PREPARED before wq_direct_weight_prepare.  The sums over groups
- * are fp32; their order, and with it the last bits of y, may depend on `rows`.  Unlike the library's other calls this one
+ * are fp32, up to all of a column's in one chain (wq_direct_conv adds fewer and then in fp64): z is within (groups + 18) 2^-24 of
+ * |bias| + the sum of the terms' magnitudes, and for terms of either sign some sqrt(groups) 0.3 2^-24 of z in the root mean
+ * square (256 groups: 3e-7).  Their order, and with it the last bits of y, may depend on `rows`.  Unlike the library's other calls this one
  * gives what the formulas give for infinities and NaN in z; an infinity in x makes its group's scale infinite and its row of z NaN. */
 wq_status_t wq_linear_matmul(const wq_direct_plan_t *plan, void *stream, int rows, const void *workspace_dev,
                              size_t workspace_bytes, const void *weight_blob_dev, size_t blob_bytes,

@@ -1,9 +1,13 @@
-"""Values at which the linear layer's surroundings can go wrong: infinities and NaN, activations by place."""
+"""Values at which the linear layer's surroundings can go wrong: infinities and NaN, activations by place, the norm's factor
+next to a rounding's border, sums over many groups."""
 import math
 
 import numpy as np
 import pytest
 import torch
+
+import oracle
+from oracle import linear_block as lb
 
 pytestmark = pytest.mark.gpu
 
@@ -159,3 +163,33 @@ def test_the_norms_codes_do_not_depend_on_where_rows_lie(wq, C, g):
             scales.add(float(plan.workspace_views(even)[1][0, 0]))
         moved += len(scales) == 2
     assert moved >= 6   # such places were met
+
+
+# rows and weight rows of the forms that add all groups of a column one after the other, and of the others
+LONG = {"rows": (5, 96), "rows2": (50, 1440), "teams4": (199, 2240), "teams2": (301, 4480), "teams1": (641, 4480), "large": (2501, 4480)}
+
+
+@pytest.mark.parametrize("form", LONG)
+def test_sums_over_many_groups(wq, form):
+    """256 groups of 32 in fp32.  n terms of either sign, of size s, add up to some s sqrt(n); the k-th addition rounds a sum of
+    s sqrt(k) by up to u of it, and independent roundings add up to u s sqrt(n (n + 1) / 2): sqrt((n + 1) / 2) u of the result
+    where nothing splits the sum.  Each term's two products and the bias add less than 3 u.  Root mean squares over the sample."""
+    n, Cout = LONG[form]
+    print(form, flush=True)
+    rng = np.random.default_rng(n)
+    Cin, g, u = 8192, 32, 2.0 ** -24
+    plan = wq.LinearPlan(n, Cin, Cout, g)
+    blob, ws = plan.alloc_blob(), plan.alloc_workspace()
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    w = torch.randn((Cout, Cin), generator=gen, device="cuda") * 0.05
+    x = torch.randn((n, Cin), generator=gen, device="cuda")
+    plan.weight_prepare(w, None, blob)
+    y = torch.empty((n, Cout), device="cuda")
+    plan.linear(x, blob, ws, y)
+    rows, cols = sorted(set(rng.integers(0, n, 12).tolist())), sorted(set(rng.integers(0, Cout, 96).tolist()))
+    wcodes, wscales = oracle.quantize_weight_rows(w[cols].cpu().numpy(), g, 8)
+    z, _ = lb.product(*oracle.quantize_pixels(x[rows].cpu().numpy(), g), wcodes, wscales, None, g)
+    e = y[rows][:, cols].double().cpu().numpy() - z
+    rms = float(np.sqrt((e ** 2).mean() / (z ** 2).mean()))
+    print("rms %.2e, %.2f u" % (rms, rms / u), flush=True)
+    assert rms <= (math.sqrt((Cin // g + 1) / 2) + 3.0) * u
