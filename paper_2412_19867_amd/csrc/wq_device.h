@@ -3,6 +3,7 @@
 // round-half-to-even, one reciprocal per group).
 #pragma once
 
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -21,6 +22,13 @@ template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
     // bound_ctrl with a zero fill lets the compiler fold the move into v_max_u32_dpp
     return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true));
+}
+
+// The group quantizer's scale and reciprocal of a group with this largest magnitude.
+__device__ __forceinline__ void group_scale(float top, float &s, float &r) {
+    const bool live = top >= 127.0f * FLT_MIN;
+    s = live ? top / 127.0f : 0.0f;   // correctly rounded
+    r = live ? 127.0f / top : 0.0f;
 }
 
 // rint(v*r) as the low byte of a two's-complement code; |v*r| <= 127 + ulp.

@@ -9,7 +9,6 @@
 //                                                                 k_direct_conv
 // k_direct_conv is an implicit GEMM without LDS staging: both operands lie in memory in the order
 // the MFMA reads them, a wave loads them straight into its registers (see the kernel).
-#include <float.h>
 
 #include <cstdlib>
 #include <cstring>
@@ -51,12 +50,8 @@ __global__ __launch_bounds__(256) void k_quantize_pixels(const float *__restrict
     a = dpp_max<0xB1>(a);    // quad_perm [1,0,3,2]
     a = dpp_max<0x4E>(a);    // quad_perm [2,3,0,1]
     a = dpp_max<0x141>(a);   // row_half_mirror: the 8 lanes of the unit
-    const float af = __uint_as_float(a);
-    float s = 0.0f, r = 0.0f;
-    if (af >= 127.0f * FLT_MIN) {
-        s = af / 127.0f;   // correctly rounded
-        r = 127.0f / af;
-    }
+    float s, r;
+    group_scale(__uint_as_float(a), s, r);
     uint32_t words[CPL / 4];
 #pragma unroll
     for (int k = 0; k < CPL / 4; ++k)

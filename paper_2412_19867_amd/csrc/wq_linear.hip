@@ -1,8 +1,9 @@
 // What stands around a quantized linear layer in a transformer block, in the formats of the layer itself:
-//   k_rms_norm_quantize   h = x + residual, v = h rho gamma with rho = 1 / sqrt(mean(h^2) + eps), group-wise
-//                         int8 codes and scales of v
-//   k_quantize_rows       the same codes of rows of any float type
-//   k_linear              y = act(x W^T + bias) (or, gated, act(gate) * up) + residual
+//   k_quantize_pieces   norm: h = x + residual, v = h rho gamma with rho = 1 / sqrt(mean(h^2) + eps), group-wise int8 codes and
+//                       scales of v; or the codes and scales of rows of any float type alone
+//   k_quantize_row      both for rows at odd addresses, and the norm of very long rows
+//   k_linear_rows       y = act(x W^T + bias) (or, gated, act(gate) * up) + residual for few rows (wq_linear_rows.hip)
+//   k_linear_tile       the same for many (wq_linear_tile.h)
 // Activations lie in the workspace as the standard convolution keeps them (planes of one K-quarter of one MFMA
 // K-step, rows in order inside a plane), weights in the blob in MFMA operand order.
 #include <float.h>

@@ -1,8 +1,6 @@
 // Rows of any float type in pieces of eight elements a lane, and the group quantizer over adjacent lanes.
 #pragma once
 
-#include <float.h>
-
 #include "wq_device.h"
 #include "wq.h"
 
@@ -22,13 +20,6 @@ template <>
 struct Elem<WQ_FP16> {
     using type = _Float16;
 };
-
-// The group quantizer's scale and reciprocal of a group with this largest magnitude.
-__device__ __forceinline__ void group_scale(float top, float &s, float &r) {
-    const bool live = top >= 127.0f * FLT_MIN;
-    s = live ? top / 127.0f : 0.0f;   // correctly rounded
-    r = live ? 127.0f / top : 0.0f;
-}
 
 // Eight adjacent elements (aligned to 16 bytes) as fp32, and back.
 template <typename T>

@@ -510,7 +510,8 @@ class LinearPlan(DirectPlan):
     around it: the root-mean-square norm with the residual's addition in front of it, bias, activation,
     gate and residual behind it.  x, residual and outputs are [n][columns] tensors of one float type
     (fp32, bf16, fp16) with adjacent columns and any row stride, n <= rows; blob and workspace are
-    DirectPlan's.  All tensors are on the current device, which is the stream's."""
+    DirectPlan's.  quantize, conv and forward are the older calls, for all rows in contiguous fp32 without an epilogue: their
+    sums are partly in fp64, linear's in fp32, which takes as long or less for most layers.  All tensors are on the current device, which is the stream's."""
 
     def __init__(self, rows, Cin, Cout, group_size, weight_bits: int = 8):
         import torch

@@ -8,6 +8,7 @@ import pytest
 
 import test_linear_block_gpu as block
 import test_linear_forms_gpu as forms
+import test_linear_values_gpu as values
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -57,6 +58,12 @@ def test_a_graph_gets_the_form_that_takes_less_of_the_cards_time(ask, layer, lau
     """Layers whose two sides were measured in a graph; launched one by one, where a launch costs the host more, all take one."""
     assert ask([("captured", *layer)])[0].split(",")[0].endswith("itself") == (launches == 1)
     assert ask([("product", *layer)])[0].split(",")[0].endswith("itself")
+
+
+def test_the_long_sums_take_the_forms_that_they_name(ask):
+    want = {"rows": "rows1 x4", "rows2": "rows2 x4", "teams4": "tiles64 4", "teams2": "tiles64 2", "teams1": "tiles64 1", "large": "tiles128"}
+    got = ask([("product", n, 8192, Cout, 32, False) for n, Cout in values.LONG.values()])
+    assert {k: v.split(", ")[0] for k, v in zip(values.LONG, got)} == want
 
 
 def test_every_product_kernel_is_reached(ask):
