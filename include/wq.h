@@ -289,7 +289,7 @@ wq_status_t wq_conv_forward_debug_slab(const wq_plan_t *plan, void *stream, cons
  * and never synchronise, every argument is checked on the host.  Errors:
  * non-positive sizes, NULL pointers, Cin not a multiple of group_size ->
  * INVALID_ARG; group_size not in {32,64,128,256,512}, a tensor of 2 GiB or
- * more, or more than 4193280 pixels (rows) -> UNSUPPORTED; a buffer smaller than the layout says -> WORKSPACE;
+ * more, or more than 4194240 pixels (rows) -> UNSUPPORTED; a buffer smaller than the layout says -> WORKSPACE;
  * conv before weight_prepare -> NOT_PREPARED. */
 typedef struct wq_direct_plan wq_direct_plan_t;
 

@@ -342,7 +342,7 @@ hipError_t launch_tile(const wq_linear_args &a, hipStream_t s) {
 // Tiles of 128 x 128.  Groups of up to 64 take stages of one group of 64 (two of 32): fewer registers and less LDS, so that
 // three or four workgroups share a CU where two would (4096x1280->2x5120 g 64, 8-bit: 107 us, 124 with stages of 128;
 // 4-bit, whose stages are small enough for a third of them: 101.5, in two 107.8).  8-bit, groups of 32: four workgroups a CU
-// cost 5 registers' spill outside the loop and are no slower than three without one (4096x1280->2x5120 167, 167; 4096x4096->4096 199, 201;
+// cost a spill of 5 registers and are no slower than three without one (4096x1280->2x5120 167, 167; 4096x4096->4096 199, 201;
 // 8192x2048->2048 105, 109).
 template <int GS, bool W4>
 hipError_t launch_large(const wq_linear_args &a, hipStream_t s) {
