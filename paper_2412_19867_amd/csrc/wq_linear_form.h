@@ -42,7 +42,7 @@ inline bool wq_linear_takes_rows(const wq_linear_form &form, int rows, int Cin, 
 // (us at 1 to 16 rows, 4096->4096 g 128 W4 4.9, 5.4; 5120->5120 g 32 W8 11.5, 13.9).  Where the workgroup quantizes x first, four more
 // halve the time for it.  That counts from some 2000 elements on while the workgroups of eight are all on the card at once, up to 512
 // blocks of 16 weight rows, and later the more blocks there are.  us with four, eight: 16x1024->1024 8.6, 6.5; 1x8192->4096 W4 10.2, 8.8;
-// 1x4096->4096 W8 7.7, 7.1; 1x5120->2x13824 W8 31.6, 37.6.  Over 340 drawn layers 0.2 % from the better of the two.
+// 1x4096->4096 W8 7.7, 7.1; 1x5120->2x13824 W8 31.6, 37.6.  Over 338 drawn layers 0.2 % from the better of the two.
 inline int wq_linear_row_waves(bool takes_rows, int rows, int Cin, int Cout) {
     const long elements = (long)(rows < 16 ? rows : 16) * Cin, blocks = (long)((Cout + 15) / 16) * ((rows + 15) / 16);
     return takes_rows && elements >= (blocks <= 512 ? 2048 : 10240 + 8 * (blocks - 512)) ? 8 : 4;
