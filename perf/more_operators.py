@@ -13,10 +13,11 @@ passes (plan, weights, workspace, output buffers) in hand:
   block       norm_codes -> gated product -> product with residual, in turn
 
 Plain forms (`own` false) compute the same from elementary torch operations in fp32.  What decides a code is
-defined to the last bit: a group's or block's scale is fl(a / 448), a code the e4m3 number nearest to
-fl(v fl(448 / a)), ties to even, a the largest magnitude; a group below 448 times the smallest normal number has
-scale and codes zero.  Gradients are quantized like activations: in groups of 128 columns for the product with
-the weights, in groups of 128 rows for the product with x.
+defined to the last bit: a group's or block's scale is the smallest power of two s >= 2^-126 with a <= 448 s, a the
+largest magnitude, a code the e4m3 number nearest to v / s, ties to even.  Gradients are quantized like
+activations: in groups of 128 columns for the product with the weights, in groups of 128 rows for the product
+with x.  Weights may also come from a checkpoint that holds codes with any fp32 scales.  The layer norm that ends
+in codes is fl(fl(fl(o r) gamma) + beta) with o = fl(h - mean), r = fl(1 / sqrt(var + eps)), mean and var in 64 bits.
 """
 import math
 
@@ -26,7 +27,6 @@ own = False
 
 TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
 SIZES = {"fp32": 4, "bf16": 2, "fp16": 2}
-TINY = 2.0 ** -126   # the smallest normal fp32 number
 EPS = 1e-5
 TOP = 448.0          # the largest e4m3 number
 G = 128
@@ -36,9 +36,9 @@ def _norm(name, kind, rows, C, dtype, residual):
     return {"name": name, "kind": kind, "rows": rows, "C": C, "dtype": dtype, "residual": residual}
 
 
-def _linear(name, rows, Cin, Cout, dtype, act="none", gated=False, residual=False, keep=False):
+def _linear(name, rows, Cin, Cout, dtype, act="none", gated=False, residual=False, keep=False, loaded=False):
     return {"name": name, "kind": "linear", "rows": rows, "Cin": Cin, "Cout": Cout, "dtype": dtype, "act": act,
-            "gated": gated, "residual": residual, "keep": keep}
+            "gated": gated, "residual": residual, "keep": keep, "loaded": loaded}
 
 
 def _grad(name, rows, Cin, Cout, dtype, wtype, act="none", gated=False):
@@ -56,17 +56,17 @@ def listed():
         _norm("norm_grad_4096x8192", "norm_grad", 4096, 8192, "fp32", False),
         # fine-tuning on few images: an odd number of tokens, the residual stream's gradient joins
         _norm("norm_grad_333x1280", "norm_grad", 333, 1280, "bf16", True),
-        # decoding one token: the down projection with its residual, the weights are all that is read
-        _linear("token_8192_4096", 1, 8192, 4096, "bf16", residual=True),
+        # decoding one token: the down projection of a checkpoint with its residual, the weights are all that is read
+        _linear("token_8192_4096", 1, 8192, 4096, "bf16", residual=True, loaded=True),
         # a few tokens at once: the wide gated projection
         _linear("batch16_gated_4096", 16, 4096, 2 * 8192, "bf16", "silu", gated=True),
         # a text encoder's feed-forward layer: 77 tokens, a last block of columns that is not whole
         _linear("encoder_77x768", 77, 768, 2040, "fp16", "gelu_tanh"),
-        # an odd number of tokens, a last group of the reduction that is half of one, fp32
-        _linear("prompt_1001x2112", 1001, 2112, 2048, "fp32", residual=True),
+        # a checkpoint's projection, an odd number of tokens, a last group of the reduction that is half of one
+        _linear("prompt_1001x2112", 1001, 2112, 2048, "bf16", residual=True, loaded=True),
         # the largest product: a training step's wide gated projection, the values before the gate kept
         _linear("train_gated_4096", 4096, 4096, 2 * 8192, "bf16", "silu", gated=True, keep=True),
-        # a training step's backward pass through an attention's projection, weights' gradient in fp32
+        # a training step's backward pass through an attention's projection, the weights' gradient in fp32
         _grad("grad_4096x4096", 4096, 4096, 4096, "bf16", "fp32"),
         # the same through a diffusion transformer's gated layer, tokens of one image less some
         _grad("grad_gated_1000x1280", 1000, 1280, 2 * 5120, "bf16", "bf16", "gelu", gated=True),
@@ -91,24 +91,26 @@ def _channels(rng, lo, hi, step):
 def draw(rng):
     while True:
         kind = rng.choices(("norm", "norm_codes", "norm_grad", "linear", "grad", "block"), (8, 8, 16, 38, 22, 8))[0]
-        dtype = rng.choice(("bf16", "bf16", "fp16", "fp32"))
+        dtype = rng.choice(("bf16", "bf16", "fp16"))   # the product's tensors; the norm's may also be fp32
         if kind.startswith("norm"):
+            dtype = rng.choice((dtype, "fp32"))
             c = _norm(None, kind, _log(rng, 1, 8192), _channels(rng, 320, 16384, 1), dtype, rng.random() < 0.5)
         elif kind == "linear":
             gated = rng.random() < 0.4
             out = 2 * _channels(rng, 320, 8192, 32) if gated else _channels(rng, 320, 16384, 1)
             c = _linear(None, _log(rng, 1, 8192), _channels(rng, 320, 8192, 1), out, dtype,
-                        rng.choice(("none", "relu", "silu", "gelu", "gelu_tanh")), gated, rng.random() < 0.5, rng.random() < 0.25)
+                        rng.choice(("none", "relu", "silu", "gelu", "gelu_tanh")), gated, rng.random() < 0.5, rng.random() < 0.25,
+                        rng.random() < 0.35)
         elif kind == "grad":
             gated = rng.random() < 0.4
             act = rng.choice(("relu", "silu", "gelu", "gelu_tanh")) if gated or rng.random() < 0.4 else "none"
             # behind an activation a last bit decides codes here and there: outputs of narrow types
-            dtype, wtype = (rng.choice(("bf16", "fp16")),) * 2 if act != "none" else (dtype, "fp32")
+            wtype = dtype if act != "none" else rng.choice((dtype, "fp32"))
             out = 2 * _channels(rng, 320, 8192, 32) if gated else _channels(rng, 320, 8192, 1)
             c = _grad(None, _log(rng, 1, 8192), _channels(rng, 320, 8192, 1), out, dtype, wtype, act, gated)
         else:
             c = {"kind": kind, "rows": _log(rng, 1, 2048), "Cin": _channels(rng, 320, 4096, 8),
-                 "width": _channels(rng, 640, 8192, 32), "dtype": rng.choice(("bf16", "fp16"))}
+                 "width": _channels(rng, 640, 8192, 32), "dtype": dtype}
         c.pop("name", None)
         w = work(c)
         if w["bytes"] <= 440e6 and w["flops"] <= 560e9:
@@ -172,24 +174,24 @@ def _gradients(gen, rows, C, dtype):
     return (d * size).to(TYPES[dtype])
 
 
-def _weights(gen, Cin, Cout):
-    """A layer's weights: fp32 as trained, and the codes and scales that a checkpoint keeps of them."""
+def _weights(gen, Cin, Cout, loaded):
+    """A layer's weights: fp32 as trained, with their codes and scales, or those that a checkpoint has."""
     w = torch.randn((Cout, Cin), generator=gen, device="cuda") * 0.02
     w[torch.randperm(Cout, generator=gen, device="cuda")[:max(1, Cout // 100)]] *= 8.0
     bias = torch.randn((Cout,), generator=gen, device="cuda") * 0.1
-    codes, scales = _quantize_blocks(w)
-    return w, bias, codes, scales
+    codes, scales = _quantize_blocks(w, loaded)
+    return None if loaded else w, bias, codes, scales
 
 
 def _plan(rows, Cin, Cout, layer, train):
     from paper_2412_19867_amd import wq
     w, bias, codes, scales = layer
-    plan = wq.Fp8LinearPlan(rows, Cin, Cout, backward=train)
+    plan = wq.Fp8LinearPlan(rows, Cin, Cout, backward=train, fp32_scales=w is None)
     blob = plan.alloc_blob()
-    if train:   # weights as the optimizer holds them
-        plan.weight_prepare(w, bias, blob)
-    else:       # weights as a checkpoint holds them
+    if w is None:
         plan.weight_load(codes, scales, bias, blob)
+    else:
+        plan.weight_prepare(w, bias, blob)
     return plan, blob, plan.alloc_workspace()
 
 
@@ -210,7 +212,7 @@ def prepare(case, seed):
         outs = C if c["kind"] != "linear" else c["Cout"] // 2 if c["gated"] else c["Cout"]
         s["res"] = torch.randn((rows, outs), generator=gen, device="cuda").to(dt)
     sizes = {"linear": ((C, c.get("Cout")),), "grad": ((C, c.get("Cout")),), "block": ((C, 2 * c.get("width", 0)), (c.get("width"), C))}
-    layers = [_weights(gen, *size) for size in sizes.get(c["kind"], ())]
+    layers = [_weights(gen, *size, c.get("loaded", False)) for size in sizes.get(c["kind"], ())]
     if c["kind"] == "grad":
         s["dy"] = _gradients(gen, rows, c["Cout"] // 2 if c["gated"] else c["Cout"], c["dtype"])
         if c["act"] != "none":   # what the forward pass kept
@@ -247,11 +249,11 @@ def prepare(case, seed):
 # ---- plain forms ----
 
 def _scales(a):
-    """(scale, reciprocal) of groups with the largest magnitude a: the division in 64 bits and rounded to 32 is the
-    correctly rounded one in 32."""
-    live = a >= TOP * TINY
-    wide, tops = a.double(), torch.full_like(a, TOP, dtype=torch.float64)
-    return torch.where(live, (wide / tops).float(), 0.0), torch.where(live, (tops / wide).float(), 0.0)
+    """(scale, reciprocal) of groups with the largest magnitude a = m 2^e, 1/2 <= m < 1: 448 is 7/8 of 2^9.  Powers of two
+    are put together from their bits."""
+    m, e = torch.frexp(a)
+    e = torch.where(a > 0, e - 9 + (m > 0.875).int(), -126).clamp(-126, 127)
+    return ((e + 127) << 23).view(torch.float32), ((127 - e) << 23).view(torch.float32)
 
 
 def _e4m3(v):
@@ -270,11 +272,13 @@ def _quantize(v):
     return _e4m3(v * r[..., None]), scale
 
 
-def _quantize_blocks(w):
-    """Codes (e4m3) [rows][cols] and scales [row blocks][column blocks] of fp32 weights."""
+def _quantize_blocks(w, loaded):
+    """Codes (e4m3) [rows][cols] and scales [row blocks][column blocks] of fp32 weights; a checkpoint's scales (`loaded`) take
+    each block's largest magnitude to 448."""
     blocks = _padded(w, G, G).view((w.shape[0] + G - 1) // G, G, -1, G)
-    scale, r = _scales(blocks.abs().amax(dim=(1, 3)))
-    codes = _e4m3(blocks * r[:, None, :, None])
+    a = blocks.abs().amax(dim=(1, 3))
+    scale, r = (a / TOP, TOP / a) if loaded else _scales(a)
+    codes = _e4m3((blocks * r[:, None, :, None]).clamp(-TOP, TOP))
     return codes.view(blocks.shape[0] * G, -1)[:w.shape[0], :w.shape[1]].contiguous(), scale
 
 
@@ -316,7 +320,7 @@ def _act_slope(z, act):
 
 
 def _plain_norm(x, res, gamma, beta):
-    """(h, y), both fp32.  Mean and variance in 64 bits: rows may lie far from zero."""
+    """(h, y), both fp32.  Mean and variance in 64 bits: rows may lie far from zero, and a last bit decides codes."""
     h = x.float() if res is None else x.float() + res.float()
     wide = h.double()
     off = wide - wide.mean(dim=1, keepdim=True)
@@ -432,19 +436,16 @@ def run(state):
 
 def _exact_codes(v):
     """(values that the codes stand for before their scale, scales) as fp64 [rows][groups][128] and [rows][groups], of fp64 rows
-    whose entries are fp32 numbers: the quantizer's definition, its roundings taken literally."""
-    def fl(t):
-        return t.to(torch.float32).to(torch.float64)
-
+    whose entries are fp32 numbers: the quantizer's definition."""
     groups = -(-v.shape[1] // G)
     room = v.new_zeros((v.shape[0], groups * G))
     room[:, :v.shape[1]] = v
     room = room.view(v.shape[0], groups, G)
     top = torch.maximum(room.max(dim=2).values, -room.min(dim=2).values)
-    full = torch.full_like(top, TOP)
-    dead = top < TOP * TINY
-    s, r = fl(torch.div(top, full)).masked_fill(dead, 0.0), fl(torch.div(full, top)).masked_fill(dead, 0.0)
-    p = fl(room * r.unsqueeze(2))
+    share, _ = torch.frexp(top)
+    whole = torch.where(top == 0, top, top / share)   # the power of two above it
+    s = torch.where(share > 0.875, whole / 256.0, whole / 512.0).clamp_min(2.0 ** -126)
+    p = room / s.unsqueeze(2)
     # the numbers of e4m3: 2^-9 apart below 2^-6, then a sixteenth to an eighth of the value; torch.round takes ties to even.
     # (p / mantissa is the power of two, exactly; powers by torch.pow are not)
     mantissa, _ = torch.frexp(p)
@@ -497,9 +498,14 @@ def _exact_product(rows, layer, act, gated, res):
     return (y if res is None else y + res.double()), z
 
 
-def _exact_norm(h, gamma, beta):
+def _exact_norm(h, gamma, beta, rounded):
+    """`rounded`: with the roundings to fp32 that the codes' definition has, taken literally."""
+    def fl(t):
+        return t.to(torch.float32).to(torch.float64) if rounded else t
+
     centred = h - h.sum(dim=1, keepdim=True) / h.shape[1]
-    return centred * torch.rsqrt(centred.pow(2).sum(dim=1, keepdim=True) / h.shape[1] + EPS) * gamma.double() + beta.double()
+    r = torch.rsqrt(centred.pow(2).sum(dim=1, keepdim=True) / h.shape[1] + EPS)
+    return fl(fl(fl(fl(centred) * fl(r)) * gamma.double()) + beta.double())
 
 
 def exact(case, seed):
@@ -514,12 +520,13 @@ def exact(case, seed):
     dt = TYPES[c["dtype"]]
     if c["kind"] in ("norm", "norm_codes", "block"):
         h = x + s["res"].double() if "res" in s else x
-        y = _exact_norm(h.float().double(), s["gamma"], s["beta"])
+        y = _exact_norm(h.float().double(), s["gamma"], s["beta"], c["kind"] != "norm")
         if c["kind"] == "norm":
             return {"y": y, "h": h} if "res" in s else {"y": y}
-        codes, scales = _exact_codes(y.float().double())
-        if c["kind"] == "norm_codes":   # (a value next to a border between two codes has no code of its own)
-            return {"codes": None, "scales": scales, "h": h} if "res" in s else {"codes": None, "scales": scales}
+        codes, scales = _exact_codes(y)
+        if c["kind"] == "norm_codes":
+            codes = codes.view(codes.shape[0], -1, 8, 16)
+            return {"codes": codes, "scales": scales, "h": h} if "res" in s else {"codes": codes, "scales": scales}
         rows = (codes * scales.unsqueeze(2)).reshape(x.shape[0], -1)[:, :x.shape[1]]
         mid, _ = _exact_product(rows, s["layers"][0], "silu", True, None)
         mid, low = mid.to(dt).double(), h.to(dt).double()   # the layers exchange values of their type
