@@ -426,6 +426,127 @@ wq_status_t wq_linear_forward(const wq_direct_plan_t *plan, void *stream, int ro
                               void *workspace_dev, size_t workspace_bytes, int activation, int gated,
                               const void *residual_dev, int64_t residual_stride, void *y_dev, int64_t y_stride);
 
+/* ---------------------------------------------------------------------------
+ * The linear layer in 8-bit floating point (OCP e4m3), served and trained: y = x W^T + bias with one scale for each
+ * 128 columns of a row of x and one for each block of 128 x 128 of W (the last ones may be partial).
+ *   scales that the library chooses: the smallest power of two s >= 2^-126 with max|v| <= 448 s, NaN not counted;
+ *   codes: the e4m3 number nearest to v / s (exact but for that one rounding), ties to even; NaN and infinity give NaN.
+ * Weights of a checkpoint may have any fp32 scales instead (a plan made with fp32_scales), at a multiply-add per group and value.
+ * Precision: a code times a power of two is a bf16 number, products of those are exact and the matrix core adds them with 24 bits:
+ * z is within (Cin + 16) 2^-24 of |bias| + the sum of the terms' magnitudes.  Gradients that are stored as bf16 or fp16 (dx, dw) are formed from the
+ * codes directly at up to twice the rate: of eight neighbouring products the matrix core then drops what lies 2^-13 below the largest,
+ * some 1.5e-5 of the result in the root mean square, where the type's own rounding is 1e-4 or more.
+ * Formats (sizes and offsets from wq_fp8_plan_layout; B = in_blocks, O = out_blocks, a piece is 16 codes of a row):
+ *   weight blob : codes [ceil(Cout/16)][B][8 pieces][16 rows][16]          at blob_codes_off
+ *                 scales fp32 [O][B], bias fp32 [ceil(Cout/16) 16]         at blob_scales_off, blob_bias_off
+ *                 backward: the transpose's codes [ceil(Cin/16)][O][8][16][16]   at blob_codes_t_off
+ *                 and scales fp32 [B][O]                                   at blob_scales_t_off
+ *   workspace   : codes of x [B][8 pieces][rows][16]                       at ws_codes_off
+ *                 scales of x fp32 [B][rows]                               at ws_scales_off
+ *                 behind them what wq_fp8_backward keeps for itself.
+ * Tensors are rows of one type with a row stride in elements as for wq_linear_matmul; any Cin and Cout of at least 1.
+ * Conventions as above: caller-owned device memory, calls enqueue on `stream`, never synchronise, may be captured, and are
+ * checked on the host first.  Calls on one workspace that overlap in time race.  A call touches the first `rows` rows of its tensors
+ * alone; rows = 0 launches nothing (but see wq_fp8_backward).  NULL pointers, sizes, strides or types out of range,
+ * a misaligned tensor, a workspace or blob not aligned to 16 bytes -> INVALID_ARG; codes of 2 GiB or more -> UNSUPPORTED; a buffer smaller
+ * than the layout says -> WORKSPACE; a product before weight_prepare or weight_load -> NOT_PREPARED. */
+typedef struct wq_fp8_plan wq_fp8_plan_t;
+
+typedef struct {
+    int32_t rows, Cin, Cout, in_blocks, out_blocks, backward, fp32_scales, pad;
+    uint64_t blob_bytes, blob_codes_off, blob_scales_off, blob_bias_off, blob_codes_t_off, blob_scales_t_off;
+    uint64_t ws_bytes, ws_codes_off, ws_scales_off;
+    uint64_t ws_dz_codes_off, ws_dz_scales_off;       /* backward: codes of dz as those of x, [O][8][rows][16], [O][rows] */
+    uint64_t ws_xt_off, ws_xt_scales_off;             /* of x along the rows: codes, or bf16 values, and scales */
+    uint64_t ws_dzt_off, ws_dzt_scales_off;           /* of dz along the rows */
+    uint64_t ws_db_off, ws_part_off;                  /* partial sums of the bias's and the weights' gradients */
+} wq_fp8_layout_t;
+
+wq_status_t wq_fp8_plan_create(wq_fp8_plan_t **out, int rows, int Cin, int Cout, int backward, int fp32_scales);
+wq_status_t wq_fp8_plan_destroy(wq_fp8_plan_t *plan);
+wq_status_t wq_fp8_plan_layout(const wq_fp8_plan_t *plan, wq_fp8_layout_t *out);
+
+/* Weights of any float type [Cout][Cin] into the blob, quantized in blocks (scales powers of two); bias_dev fp32 [Cout] (NULL = zeros). */
+wq_status_t wq_fp8_weight_prepare(wq_fp8_plan_t *plan, void *stream, int type, const void *w_dev, int64_t w_stride,
+                                  const float *bias_dev, void *weight_blob_dev, size_t blob_bytes);
+
+/* Weights as a checkpoint holds them: e4m3 codes [Cout][Cin] (row stride in bytes) and scales [out_blocks][in_blocks], contiguous,
+ * either fp32 (any finite numbers; a plan without fp32_scales -> UNSUPPORTED) or e8m0 bytes (2^(byte - 127); 0 counts as 2^-126,
+ * 255, which is NaN, as 2^127).  Codes that are NaN stay NaN. */
+typedef enum { WQ_SCALE_FP32 = 0, WQ_SCALE_E8M0 = 1 } wq_scale_type_t;
+wq_status_t wq_fp8_weight_load(wq_fp8_plan_t *plan, void *stream, const void *codes_dev, int64_t codes_stride, int scale_type,
+                               const void *scales_dev, const float *bias_dev, void *weight_blob_dev, size_t blob_bytes);
+
+/* Codes and scales of rows of any float type into the workspace. */
+wq_status_t wq_fp8_quantize(const wq_fp8_plan_t *plan, void *stream, int rows, int type, const void *x_dev, int64_t x_stride,
+                            void *workspace_dev, size_t workspace_bytes);
+
+/* Layer norm with the residual's addition, quantized:
+ *   h = x + residual (residual_dev NULL: h = x), in fp32;  mean, var: of a row of h, in fp64;
+ *   o = fl(h - mean), r = fl(1 / sqrt(var + eps)), v = fl(fl(fl(o r) gamma) + beta) (gamma_dev, beta_dev fp32 [Cin]; NULL: 1, 0),
+ * codes and scales of v into the workspace.  sum_dev (NULL: not wanted) gets h rounded to the type, the norm goes on from the
+ * unrounded h; it may be x_dev or residual_dev itself with the same stride.  eps: at least 2^-126 and finite. */
+wq_status_t wq_fp8_layer_norm_quantize(const wq_fp8_plan_t *plan, void *stream, int rows, int type, const void *x_dev,
+                                       int64_t x_stride, const void *residual_dev, int64_t residual_stride,
+                                       const float *gamma_dev, const float *beta_dev, double eps, void *sum_dev,
+                                       int64_t sum_stride, void *workspace_dev, size_t workspace_bytes);
+
+/* The product with its epilogue, of the codes in the workspace:
+ *   z = bias + x W^T;   gated 0: y = act(z) + residual;   gated 1: y[o] = act(z[o]) z[Cout/2 + o] + residual[o]
+ * as wq_linear_matmul, in fp32 and rounded once to `type`.  Gated: Cout a multiple of 64, else UNSUPPORTED.  pre_dev (NULL: not wanted): z [rows][Cout] rounded to the type, for the backward pass.
+ * y_dev may be residual_dev itself with the same stride. */
+wq_status_t wq_fp8_matmul(const wq_fp8_plan_t *plan, void *stream, int rows, const void *workspace_dev, size_t workspace_bytes,
+                          const void *weight_blob_dev, size_t blob_bytes, int activation, int gated, int type,
+                          const void *residual_dev, int64_t residual_stride, void *pre_dev, int64_t pre_stride, void *y_dev,
+                          int64_t y_stride);
+
+/* wq_fp8_quantize followed by wq_fp8_matmul, where rows are few in one launch; x, residual, pre and y of one type.  y_dev
+ * may be x_dev, residual_dev or both (with their strides).  What the workspace holds afterwards is unspecified. */
+wq_status_t wq_fp8_forward(const wq_fp8_plan_t *plan, void *stream, int rows, int type, const void *x_dev, int64_t x_stride,
+                           const void *weight_blob_dev, size_t blob_bytes, void *workspace_dev, size_t workspace_bytes,
+                           int activation, int gated, const void *residual_dev, int64_t residual_stride, void *pre_dev,
+                           int64_t pre_stride, void *y_dev, int64_t y_stride);
+
+/* Gradients of wq_fp8_forward, for plans made with backward (others -> UNSUPPORTED).  dy is the gradient of y, [rows][outs]; the
+ * residual's gradient is dy itself.
+ *   dz = dy act'(z); gated: dz[o] = dy[o] z[F + o] act'(z[o]), dz[F + o] = dy[o] act(z[o]); in fp32, z as pre_dev holds it
+ *     (needed with an activation or a gate, else not looked at).  relu's slope at 0 is 0.
+ *   dx = D1 Wq        D1: dz in codes with a scale for each 128 columns of a row, Wq: the weights that the blob's codes stand for
+ *   dw = D2^T X2      D2, X2: dz and x in codes with a scale for each 128 rows (from row 0 on, the last group may be partial) of a column
+ *   db = sum of dz over the rows, in fp32
+ * dx_dev [rows][Cin] of `type` (x's, dy's and pre's too), dw_dev [Cout][Cin] of `type` or fp32, db_dev fp32 [Cout]; each may be
+ * NULL and is then not computed (x_dev is looked at for dw alone, the blob for dx alone).  accumulate 1: dw and db are added to what
+ * is there, in fp32 and rounded once.  dx_dev may be x_dev or dy_dev itself (with their strides).  rows = 0: dw and db become zero unless they
+ * accumulate.  The results have the same bits in every call with the same arguments. */
+wq_status_t wq_fp8_backward(const wq_fp8_plan_t *plan, void *stream, int rows, int type, const void *x_dev, int64_t x_stride,
+                            const void *dy_dev, int64_t dy_stride, const void *pre_dev, int64_t pre_stride,
+                            const void *weight_blob_dev, size_t blob_bytes, void *workspace_dev, size_t workspace_bytes,
+                            int activation, int gated, void *dx_dev, int64_t dx_stride, int dw_type, void *dw_dev,
+                            int64_t dw_stride, float *db_dev, int accumulate);
+
+/* ---------------------------------------------------------------------------
+ * Layer norm of rows of any float type and any length C >= 1 (strides, alignment and errors as above; more than 2^25 rows or 2^30
+ * columns -> UNSUPPORTED):
+ *   h = x + residual in fp32, y = (h - mean) / sqrt(var + eps) gamma + beta, rounded as wq_fp8_layer_norm_quantize's v and then
+ *   once to the type.  sum_dev as there.  y_dev may be x_dev or residual_dev itself with the same stride; sum_dev and y_dev are
+ *   two tensors. */
+wq_status_t wq_layer_norm(void *stream, int rows, int C, int type, const void *x_dev, int64_t x_stride,
+                          const void *residual_dev, int64_t residual_stride, const float *gamma_dev, const float *beta_dev,
+                          double eps, void *sum_dev, int64_t sum_stride, void *y_dev, int64_t y_stride);
+
+/* Its gradient.  h_dev: what was normalized (sum_dev of the forward call, or x), whose mean and variance are formed again;
+ *   n = (h - mean) r, g = dy gamma:  dx = r (g - mean(g) - n mean(g n)) + residual_grad, rounded once to the type
+ *   dgamma = sum of dy n over the rows, dbeta = sum of dy, fp32 [C]; accumulate 1: added to what is there.
+ * residual_grad_dev (NULL: none): the gradient that reached h on its other way (the residual stream's).  dx_dev, dgamma_dev and
+ * dbeta_dev may each be NULL.  dx_dev may be dy_dev, h_dev or residual_grad_dev itself with the same stride.  The workspace (16-byte aligned) has
+ * the size that wq_layer_norm_workspace gives for the same C and at least as many rows.  rows = 0: dgamma and dbeta become
+ * zero unless they accumulate.  The results have the same bits in every call with the same arguments. */
+wq_status_t wq_layer_norm_workspace(int rows, int C, uint64_t *bytes);
+wq_status_t wq_layer_norm_grad(void *stream, int rows, int C, int type, const void *dy_dev, int64_t dy_stride, const void *h_dev,
+                               int64_t h_stride, const float *gamma_dev, double eps, const void *residual_grad_dev,
+                               int64_t residual_grad_stride, void *dx_dev, int64_t dx_stride, float *dgamma_dev,
+                               float *dbeta_dev, int accumulate, void *workspace_dev, size_t workspace_bytes);
+
 /* Issue-rate microbenchmark of the contraction's inner loop, without memory traffic: every
  * wave repeats, `iters` times (even), the int8 MFMAs of one quantization group on
  * `blocks_per_wave` (2 or 4) 16x16 blocks followed by the per-group dequantization the second

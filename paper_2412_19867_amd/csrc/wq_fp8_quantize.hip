@@ -1,0 +1,406 @@
+// Rows into e4m3 codes with power-of-two scales: along the rows' columns, along the rows (for the weights' gradient), weights in blocks; the
+// gradient through activation and gate on the way.
+#include "wq_fp8_quantize.h"
+#include "wq_layer_norm.h"
+
+namespace {
+
+__device__ __forceinline__ uint32_t wave_max16(uint32_t v) {   // over 16 adjacent lanes
+    v = dpp_max<0xB1>(v);
+    v = dpp_max<0x4E>(v);
+    v = dpp_max<0x141>(v);
+    return dpp_max<0x140>(v);
+}
+
+// The other lane of a pair's value.
+__device__ __forceinline__ uint32_t neighbour(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xf, 0xf, true); }
+
+// A wave takes 16 rows x 128 columns: four lanes to a row, each with four runs of eight elements 32 apart.  Two lanes' runs make a
+// piece of 16 codes; they exchange halves so that each stores whole pieces, 16 rows of a plane side by side.
+template <int TYPE>
+__global__ __launch_bounds__(256) void k_fp8_quantize(const wq_fp8_rows_args a) {
+    using T = typename Elem<TYPE>::type;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, part = lane & 3;
+    const long unit = (long)blockIdx.x * 4 + w;
+    const int bands = (a.rows + 15) / 16;
+    const int g = (int)(unit / bands), p = (int)(unit % bands) * 16 + (lane >> 2);
+    if (g >= a.groups) return;
+    const bool live = p < a.rows;
+    const T *x = (const T *)a.x + (size_t)(live ? p : a.rows - 1) * a.xs;
+    float v[4][8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = g * kGroup + i * 32 + part * 8;
+        load8_some<T>(x + c, a.cols - c, v[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[i][j]));
+    }
+    top = dpp_max<0xB1>(top);
+    top = dpp_max<0x4E>(top);
+    float s, r;
+    pow2_scale(top, s, r);
+    uint2 codes[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] *= r;
+        codes[i] = make_uint2(e4m3x4(v[i][0], v[i][1], v[i][2], v[i][3]), e4m3x4(v[i][4], v[i][5], v[i][6], v[i][7]));
+    }
+    const bool odd = lane & 1;
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {   // an even lane takes run i's piece, an odd one run i + 1's
+        const uint2 give = odd ? codes[i] : codes[i + 1], keep = odd ? codes[i + 1] : codes[i];
+        const uint2 got = make_uint2(neighbour(give.x), neighbour(give.y));
+        const uint4 piece = odd ? make_uint4(got.x, got.y, keep.x, keep.y) : make_uint4(keep.x, keep.y, got.x, got.y);
+        if (live) *(uint4 *)(a.codes + ((size_t)(g * 8 + 2 * (i + odd) + (part >> 1)) * a.P + p) * 16) = piece;
+    }
+    if (live && part == 0) a.scales[(size_t)g * a.P + p] = s;
+}
+
+// ------------------------------------------------------------ along the rows, and the gradient through the epilogue
+// Slope and value of the activation at N values (act'(z), act(z)), in fp32.
+template <int N>
+__device__ __forceinline__ void activation_slope(const float (&z)[N], int act, float (&slope)[N], float (&value)[N]) {
+    switch (act) {
+        case WQ_ACT_RELU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                slope[i] = z[i] > 0.0f ? 1.0f : z[i] == z[i] ? 0.0f : z[i];
+                value[i] = __builtin_elementwise_maximum(z[i], 0.0f);
+            }
+            break;
+        case WQ_ACT_SILU:   // s (1 + z (1 - s)), s = 1 / (1 + e^-z)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float s = logistic(z[i] * -1.44269504f), c = logistic(z[i] * 1.44269504f);
+                value[i] = z[i] * s;
+                slope[i] = __builtin_fmaf(value[i], c, s);
+            }
+            break;
+        case WQ_ACT_GELU:   // Phi(z) + z phi(z)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float cdf = 0.5f * erfcf(z[i] * -0.707106781f), pdf = 0.398942280f * __expf(-0.5f * z[i] * z[i]);
+                value[i] = z[i] * cdf;
+                slope[i] = __builtin_fmaf(z[i], pdf, cdf);
+            }
+            break;
+        case WQ_ACT_GELU_TANH:   // s + z s (1 - s) 2 u', s = 1 / (1 + e^-2u), u = sqrt(2 / pi) (z + 0.044715 z^3)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float z2 = z[i] * z[i], e2 = z[i] * __builtin_fmaf(-0.102943240f, z2, -2.30220820f);
+                const float s = logistic(e2), c = logistic(-e2);
+                value[i] = z[i] * s;
+                slope[i] = __builtin_fmaf(value[i] * c, __builtin_fmaf(0.214064488f, z2, 1.59576912f), s);
+            }
+            break;
+        default:
+#pragma unroll
+            for (int i = 0; i < N; ++i) slope[i] = 1.0f, value[i] = z[i];
+    }
+}
+
+// A workgroup takes 128 rows x 128 columns of v (x itself, or dz), each lane eight adjacent rows x eight adjacent columns in registers:
+// the groups along the columns are 16 lanes', those along the rows a lane's eight and its counterparts' in the other 15 sixteenths of
+// the workgroup.  Codes leave through LDS, where they lie as in memory.
+//   ALONG: 0 no codes along the rows, 1 codes, 2 values in bf16.
+template <int TYPE, int ALONG>
+__global__ __launch_bounds__(256) void k_fp8_both(const wq_fp8_both_args a) {
+    using T = typename Elem<TYPE>::type;
+    constexpr int STRIDE = 16 * 128 + 16 * 16;   // bytes of a plane of 128 columns' pieces in LDS, 16 of them between each eight columns
+    __shared__ __attribute__((aligned(16))) char image[16 * STRIDE];
+    __shared__ uint32_t top_s[4][128];
+    __shared__ float sum_s[4][128];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, octet = lane & 15, sub = tid >> 4;
+    const int g = blockIdx.x % a.groups, tb = blockIdx.x / a.groups;
+    const int c = g * kGroup + octet * 8, p0 = tb * kGroup + sub * 8;
+    const int outs = a.gated ? a.cols / 2 : a.cols;
+    const bool up = a.gated && c >= outs;   // (outs is a multiple of 32: all eight columns are of one half)
+    const int cy = up ? c - outs : c;       // the column of dy
+    const int n = (a.gated ? (up ? a.cols : outs) : a.cols) - c;
+    float v[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const long p = p0 + i;
+        const int m = p < a.rows ? n : 0;
+        load8_some<T>((const T *)a.v + p * a.vs + cy, m, v[i]);
+        if (!a.pre) continue;
+        float z[8], slope[8], value[8];
+        load8_some<T>((const T *)a.pre + p * a.ps + cy, m, z);
+        activation_slope(z, a.act, slope, value);
+        if (up) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] *= value[j];
+        } else if (a.gated) {
+            float u[8];
+            load8_some<T>((const T *)a.pre + p * a.ps + outs + cy, m, u);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * u[j] * slope[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] *= slope[j];
+        }
+        // (0 times an infinite or NaN slope, where nothing exists)
+        if (m < 8) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j >= m) v[i][j] = 0.0f;
+        }
+    }
+    if (ALONG || a.db) {
+        uint32_t top[8];
+        float sum[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            top[j] = 0;
+            sum[j] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                top[j] = max(top[j], magnitude(v[i][j]));
+                sum[j] += v[i][j];
+            }
+            top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 16));
+            top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 32));
+            sum[j] += __shfl_xor(sum[j], 16);
+            sum[j] += __shfl_xor(sum[j], 32);
+        }
+        if (lane < 16) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                top_s[w][octet * 8 + j] = top[j];
+                sum_s[w][octet * 8 + j] = sum[j];
+            }
+        }
+        __syncthreads();
+    }
+    if (tid < 128 && a.db && g * kGroup + tid < a.cols)
+        a.db[(size_t)tb * a.cols + g * kGroup + tid] = sum_s[0][tid] + sum_s[1][tid] + sum_s[2][tid] + sum_s[3][tid];
+    if constexpr (ALONG != 0) {
+        float s[8], r[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int k = octet * 8 + j;
+            pow2_scale(max(max(top_s[0][k], top_s[1][k]), max(top_s[2][k], top_s[3][k])), s[j], r[j]);
+            if (sub == 0 && c + j < a.colsT) a.scalesT[(size_t)tb * a.colsT + c + j] = s[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float t[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = v[i][j] * r[j];
+            const uint2 codes = make_uint2(e4m3x4(t[0], t[1], t[2], t[3]), e4m3x4(t[4], t[5], t[6], t[7]));
+            if constexpr (ALONG == 1) {
+                *(uint2 *)(image + (sub >> 1) * STRIDE + octet * 144 + j * 16 + (sub & 1) * 8) = codes;
+            } else {   // the values that the codes stand for are bf16 numbers, a piece has eight of them
+                *(v8bf *)(image + sub * STRIDE + octet * 144 + j * 16) = bf16_of_codes((int)codes.x, (int)codes.y, s[j]);
+            }
+        }
+        __syncthreads();
+        constexpr int PLANES = ALONG == 1 ? 8 : 16;
+#pragma unroll
+        for (int i = 0; i < PLANES / 2; ++i) {
+            const int k = (i * 256 + tid) & 127, plane = (i * 256 + tid) >> 7;
+            if (g * kGroup + k >= a.colsT) continue;
+            *(uint4 *)(a.codesT + ((size_t)(tb * PLANES + plane) * a.colsT + g * kGroup + k) * 16) =
+                *(const uint4 *)(image + plane * STRIDE + (k >> 3) * 144 + (k & 7) * 16);
+        }
+        __syncthreads();
+    }
+    if (!a.codes) return;
+    // along the columns: a row's piece is two lanes' eight codes
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[i][j]));
+        top = wave_max16(top);
+        float s, r;
+        pow2_scale(top, s, r);
+        if (octet == 0 && p0 + i < a.rows) a.scales[(size_t)g * a.P + p0 + i] = s;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] *= r;
+        const int row = sub * 8 + i;
+        *(uint2 *)(image + (octet >> 1) * STRIDE + (row >> 3) * 144 + (row & 7) * 16 + (octet & 1) * 8) =
+            make_uint2(e4m3x4(v[i][0], v[i][1], v[i][2], v[i][3]), e4m3x4(v[i][4], v[i][5], v[i][6], v[i][7]));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = (i * 256 + tid) & 127, plane = (i * 256 + tid) >> 7;
+        if (tb * kGroup + row >= a.rows) continue;
+        *(uint4 *)(a.codes + ((size_t)(g * 8 + plane) * a.P + tb * kGroup + row) * 16) =
+            *(const uint4 *)(image + plane * STRIDE + (row >> 3) * 144 + (row & 7) * 16);
+    }
+}
+
+// db of partial sums [blocks][cols], or the weights' gradient of K's slices [blocks][rows cols]: one value a lane, in the slices' order.
+__global__ __launch_bounds__(256) void k_fp8_db(const float *part, int blocks, int cols, float *db, int accumulate) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= cols) return;
+    double s = accumulate ? (double)db[c] : 0.0;
+    for (int b = 0; b < blocks; ++b) s += (double)part[(size_t)b * cols + c];
+    db[c] = (float)s;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_fp8_join(const float *part, int slices, int rows, int cols, T *dw, long stride, int accumulate) {
+    const long i = (long)blockIdx.x * 256 + threadIdx.x, n = (long)rows * cols;
+    if (i >= n) return;
+    float s = 0.0f;
+    for (int k = 0; k < slices; ++k) s += part[(size_t)k * n + i];
+    T *at = dw + i / cols * stride + i % cols;
+    *at = (T)(accumulate ? s + (float)*at : s);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_fp8_zero(T *dw, int rows, int cols, long stride, float *db) {
+    const long i = (long)blockIdx.x * 256 + threadIdx.x;
+    if (dw && i < (long)rows * cols) dw[i / cols * stride + i % cols] = (T)0.0f;
+    if (db && i < rows) db[i] = 0.0f;
+}
+
+// ------------------------------------------------------------ weights
+// A workgroup takes a block of 128 x 128: lanes as in k_fp8_both, the block's scale over all of them.  Codes in both orders leave
+// through LDS: 16-row blocks of eight pieces.  LOAD: w are codes already.
+template <int TYPE, bool LOAD>
+__global__ __launch_bounds__(256) void k_fp8_weights(const wq_fp8_weight_args a) {
+    using T = typename Elem<TYPE>::type;
+    constexpr int STRIDE = 16 * 128 + 16 * 16;
+    __shared__ __attribute__((aligned(16))) char image[8 * STRIDE];
+    __shared__ uint32_t top_s[4];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, octet = lane & 15, sub = tid >> 4;
+    const int ib = blockIdx.x % a.in_blocks, ob = blockIdx.x / a.in_blocks;
+    const int c = ib * kGroup + octet * 8, o0 = ob * kGroup + sub * 8;
+    uint2 codes[8];   // of a row's eight columns
+    float v[8][8];
+    if constexpr (LOAD) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t t[2] = {0, 0};
+            const uint8_t *row = (const uint8_t *)a.w + (long)(o0 + i) * a.ws + c;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (o0 + i < a.Cout && c + j < a.Cin) t[j >> 2] |= (uint32_t)row[j] << (8 * (j & 3));
+            codes[i] = make_uint2(t[0], t[1]);
+        }
+        if (tid == 0) {
+            const int at = ob * a.in_blocks + ib;
+            const float s = a.scale_type == WQ_SCALE_FP32 ? ((const float *)a.given)[at]
+                                                          : __uint_as_float((uint32_t)min(max((int)((const uint8_t *)a.given)[at], 1), 254) << 23);
+            a.scales[at] = s;
+            if (a.codesT) a.scalesT[ib * a.out_blocks + ob] = s;
+        }
+    } else {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            load8_some<T>((const T *)a.w + (long)(o0 + i) * a.ws + c, o0 + i < a.Cout ? a.Cin - c : 0, v[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[i][j]));
+        }
+#pragma unroll
+        for (int m = 32; m > 0; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+        if (lane == 0) top_s[w] = top;
+        __syncthreads();
+        float s, r;
+        pow2_scale(max(max(top_s[0], top_s[1]), max(top_s[2], top_s[3])), s, r);
+        if (tid == 0) {
+            a.scales[ob * a.in_blocks + ib] = s;
+            if (a.codesT) a.scalesT[ib * a.out_blocks + ob] = s;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] *= r;
+            codes[i] = make_uint2(e4m3x4(v[i][0], v[i][1], v[i][2], v[i][3]), e4m3x4(v[i][4], v[i][5], v[i][6], v[i][7]));
+        }
+    }
+    if (ib == 0 && tid < 128 && ob * kGroup + tid < a.Cout16) {
+        const int o = ob * kGroup + tid;
+        a.bias_out[o] = a.bias && o < a.Cout ? a.bias[o] : 0.0f;
+    }
+    auto leave = [&](uint8_t *to, int blocks, int first_block, int group, int groups) {   // 128 rows' pieces, from LDS
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = i * 256 + tid, block = at >> 7, piece = (at >> 4) & 7, row = at & 15, k = block * 16 + row;
+            if (first_block + block >= blocks) continue;
+            *(uint4 *)(to + ((size_t)(first_block + block) * groups + group) * 2048 + piece * 256 + row * 16) =
+                *(const uint4 *)(image + piece * STRIDE + (k >> 3) * 144 + (k & 7) * 16);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int row = sub * 8 + i;
+        *(uint2 *)(image + (octet >> 1) * STRIDE + (row >> 3) * 144 + (row & 7) * 16 + (octet & 1) * 8) = codes[i];
+    }
+    leave(a.codes, a.Cout16 / 16, ob * 8, ib, a.in_blocks);
+    if (!a.codesT) return;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {   // byte j of eight rows' codes
+        uint32_t t[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i >> 2] |= (((j < 4 ? codes[i].x : codes[i].y) >> (8 * (j & 3))) & 0xffu) << (8 * (i & 3));
+        *(uint2 *)(image + (sub >> 1) * STRIDE + octet * 144 + j * 16 + (sub & 1) * 8) = make_uint2(t[0], t[1]);
+    }
+    leave(a.codesT, a.Cin16 / 16, ib * 8, ob, a.out_blocks);
+}
+
+template <int TYPE>
+void launch_both(const wq_fp8_both_args &a, int along, hipStream_t s) {
+    const dim3 grid((unsigned)a.groups * (unsigned)((a.rows + kGroup - 1) / kGroup)), block(256);
+    if (along == 0) hipLaunchKernelGGL((k_fp8_both<TYPE, 0>), grid, block, 0, s, a);
+    else if (along == 1) hipLaunchKernelGGL((k_fp8_both<TYPE, 1>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_fp8_both<TYPE, 2>), grid, block, 0, s, a);
+}
+
+}  // namespace
+
+hipError_t wq_launch_fp8_quantize(const wq_fp8_rows_args &a, int type, hipStream_t s) {
+    const long units = (long)a.groups * ((a.rows + 15) / 16);
+    const dim3 grid((unsigned)((units + 3) / 4)), block(256);
+    if (type == WQ_FP32) hipLaunchKernelGGL((k_fp8_quantize<WQ_FP32>), grid, block, 0, s, a);
+    else if (type == WQ_BF16) hipLaunchKernelGGL((k_fp8_quantize<WQ_BF16>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_fp8_quantize<WQ_FP16>), grid, block, 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t wq_launch_fp8_both(const wq_fp8_both_args &a, int type, int along, hipStream_t s) {
+    if (type == WQ_FP32) launch_both<WQ_FP32>(a, along, s);
+    else if (type == WQ_BF16) launch_both<WQ_BF16>(a, along, s);
+    else launch_both<WQ_FP16>(a, along, s);
+    return hipGetLastError();
+}
+
+hipError_t wq_launch_fp8_db(const float *part, int blocks, int cols, float *db, int accumulate, hipStream_t s) {
+    hipLaunchKernelGGL(k_fp8_db, dim3((unsigned)((cols + 255) / 256)), dim3(256), 0, s, part, blocks, cols, db, accumulate);
+    return hipGetLastError();
+}
+
+hipError_t wq_launch_fp8_join(const float *part, int slices, int rows, int cols, void *dw, long stride, int type, int accumulate, hipStream_t s) {
+    const dim3 grid((unsigned)(((long)rows * cols + 255) / 256)), block(256);
+    if (type == WQ_FP32) hipLaunchKernelGGL((k_fp8_join<float>), grid, block, 0, s, part, slices, rows, cols, (float *)dw, stride, accumulate);
+    else if (type == WQ_BF16) hipLaunchKernelGGL((k_fp8_join<__bf16>), grid, block, 0, s, part, slices, rows, cols, (__bf16 *)dw, stride, accumulate);
+    else hipLaunchKernelGGL((k_fp8_join<_Float16>), grid, block, 0, s, part, slices, rows, cols, (_Float16 *)dw, stride, accumulate);
+    return hipGetLastError();
+}
+
+hipError_t wq_launch_fp8_zero(void *dw, int rows, int cols, long stride, int type, float *db, hipStream_t s) {
+    const long n = dw ? (long)rows * cols : rows;
+    const dim3 grid((unsigned)((n + 255) / 256)), block(256);
+    if (type == WQ_FP32) hipLaunchKernelGGL((k_fp8_zero<float>), grid, block, 0, s, (float *)dw, rows, cols, stride, db);
+    else if (type == WQ_BF16) hipLaunchKernelGGL((k_fp8_zero<__bf16>), grid, block, 0, s, (__bf16 *)dw, rows, cols, stride, db);
+    else hipLaunchKernelGGL((k_fp8_zero<_Float16>), grid, block, 0, s, (_Float16 *)dw, rows, cols, stride, db);
+    return hipGetLastError();
+}
+
+hipError_t wq_launch_fp8_weights(const wq_fp8_weight_args &a, int type, bool load, hipStream_t s) {
+    const dim3 grid((unsigned)a.in_blocks * (unsigned)a.out_blocks), block(256);
+    if (load) hipLaunchKernelGGL((k_fp8_weights<WQ_BF16, true>), grid, block, 0, s, a);
+    else if (type == WQ_FP32) hipLaunchKernelGGL((k_fp8_weights<WQ_FP32, false>), grid, block, 0, s, a);
+    else if (type == WQ_BF16) hipLaunchKernelGGL((k_fp8_weights<WQ_BF16, false>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_fp8_weights<WQ_FP16, false>), grid, block, 0, s, a);
+    return hipGetLastError();
+}

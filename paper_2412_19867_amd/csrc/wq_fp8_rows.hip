@@ -1,0 +1,156 @@
+// The product of the linear layer in 8-bit floating point for few rows (down to one: decoding): the weights are what is read.
+#include "wq_fp8_tile.h"
+#include "wq_quantize_piece.h"
+
+namespace {
+
+struct wq_fp8_rows_grid {
+    int nO, total, per_xcd;   // tiles along the columns of y, their number, the share of each XCD
+};
+
+constexpr int kSlices = 4;   // waves that share a tile's reduction
+
+// A workgroup owns 16 columns of y (gated: and the 16 rows of `a` that go with them in the second half) x 16 NB rows; each of its four
+// waves takes a contiguous part of K for all of them and asks for D groups ahead: nothing is staged, a wave waits for its own loads
+// alone.  Codes are multiplied as bf16 numbers, x's with their power of two; a multiply-add applies the weights' scale, any fp32 number.
+template <bool GATED, int NB>
+__global__ __launch_bounds__(256) void k_fp8_rows(const wq_fp8_product a, const wq_fp8_rows_grid t) {
+    constexpr int NE = GATED ? 2 : 1, D = 4;
+    constexpr int RS = 16 * NE + 4;
+    __shared__ __attribute__((aligned(16))) float part_s[kSlices * 16 * RS];
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, q = lane >> 4;
+    const int ks = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int logical = (int)(blockIdx.x & 7u) * t.per_xcd + (int)(blockIdx.x >> 3);
+    if (logical >= t.total) return;   // the whole workgroup leaves, before any barrier
+    const int ob = logical % t.nO, p0 = logical / t.nO * 16 * NB;
+
+    const __amdgpu_buffer_rsrc_t rA = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.a.codes), 0, (int)a.a.bytes, kBufFlags);
+    const __amdgpu_buffer_rsrc_t rB = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.b.codes), 0, (int)a.b.bytes, kBufFlags);
+    const __amdgpu_buffer_rsrc_t rSB = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<float *>(a.b.scales), 0, (int)((unsigned)a.groups * (unsigned)a.b.scale_step * 4u), kBufFlags);
+    const int c_beg = ks * a.groups / kSlices, len = (ks + 1) * a.groups / kSlices - c_beg;
+    // neighbouring tiles walk their parts from different places on: from the same one they would ask for addresses a power of two
+    // apart where K is one, all in a few of the memory's channels
+    const int first = len ? ob % len : 0;
+    auto chunk = [&](int i) {   // the i-th of the wave's groups; past the last: that again
+        const int c = first + min(i, len - 1);
+        return c_beg + (c < len ? c : c - len);
+    };
+    unsigned vA[NE], vB[NB], vSB[NB];
+    const float *sA[NE];
+#pragma unroll
+    for (int e = 0; e < NE; ++e) {
+        const int row = ob * 16 + e * a.outs;
+        vA[e] = (unsigned)(row >> 4) * a.a.block + (unsigned)lane * 16u;
+        sA[e] = a.a.scales + (long)(row >> 7) * a.a.scale_step;
+    }
+#pragma unroll
+    for (int f = 0; f < NB; ++f) {
+        const int p = min(p0 + 16 * f + l16, a.rows - 1);   // (rows past the end: the last one again, not stored)
+        vB[f] = (unsigned)(p >> 4) * a.b.block + (unsigned)q * a.b.piece + (unsigned)(p & 15) * 16u;
+        vSB[f] = (unsigned)p * 4u;
+    }
+    v4i av[D][NE][2], bv[D][NB][2];
+    float sb[D][NB], sa[D][NE];
+    auto fetch = [&](int d, int i) {   // into slot d (a constant after unrolling)
+        const int c = chunk(i);
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) av[d][e][h] = __builtin_amdgcn_raw_buffer_load_b128(rA, vA[e] + h * 1024u, (unsigned)c * a.a.group, 0);
+            sa[d][e] = sA[e][c];
+        }
+#pragma unroll
+        for (int f = 0; f < NB; ++f) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                bv[d][f][h] = __builtin_amdgcn_raw_buffer_load_b128(rB, vB[f] + h * 4u * a.b.piece, (unsigned)c * a.b.group, 0);
+            sb[d][f] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rSB, vSB[f], (unsigned)c * (unsigned)a.b.scale_step * 4u, 0));
+        }
+    };
+    v4f M[NE][NB];
+#pragma unroll
+    for (int e = 0; e < NE; ++e)
+#pragma unroll
+        for (int f = 0; f < NB; ++f) M[e][f] = v4f{0.f, 0.f, 0.f, 0.f};
+    auto compute = [&](int d) {
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+            v4f P[NB];
+#pragma unroll
+            for (int f = 0; f < NB; ++f) P[f] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const v8bf x = bf16_of_codes(av[d][e][k >> 1][(k & 1) * 2], av[d][e][k >> 1][(k & 1) * 2 + 1], 1.0f);
+#pragma unroll
+                for (int f = 0; f < NB; ++f)
+                    P[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        x, bf16_of_codes(bv[d][f][k >> 1][(k & 1) * 2], bv[d][f][k >> 1][(k & 1) * 2 + 1], sb[d][f]), P[f], 0, 0, 0);
+            }
+#pragma unroll
+            for (int f = 0; f < NB; ++f)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) M[e][f][r] = __builtin_fmaf(P[f][r], sa[d][e], M[e][f][r]);
+        }
+    };
+    if (len) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            fetch(d, d);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        int i = 0;
+        for (; i + D <= len; i += D) {   // whole rounds of the ring, then the rest
+#pragma unroll
+            for (int d = 0; d < D; ++d) {
+                compute(d);
+                __builtin_amdgcn_sched_barrier(0);
+                fetch(d, i + d + D);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < D - 1; ++d)
+            if (i + d < len) compute(d);
+    }
+
+    // ---- the waves' sums through LDS, 16 rows at a time, then the epilogue ----
+    float *mine = part_s + ks * (16 * RS);
+#pragma unroll
+    for (int f = 0; f < NB; ++f) {
+        if (f) __syncthreads();   // the rows before have been read
+#pragma unroll
+        for (int e = 0; e < NE; ++e) *(v4f *)&mine[l16 * RS + 16 * e + 4 * q] = M[e][f];
+        __syncthreads();
+        const int row = tid >> 2, c = (tid & 3) * 4, p = p0 + 16 * f + row, o = ob * 16 + c;
+        if (tid >= 64 || p >= a.rows || o >= a.outs) continue;
+        const float *s = part_s + row * RS + c;
+        const v4f res[1] = {fp8_residual(a, p, o)};
+        v4f z[1] = {*(const v4f *)s + fp8_bias(a, o)}, up[1] = {};
+        if constexpr (GATED) up[0] = *(const v4f *)(s + 16) + fp8_bias(a, a.outs + o);
+#pragma unroll
+        for (int k = 1; k < kSlices; ++k) {
+            s += 16 * RS;
+            z[0] += *(const v4f *)s;
+            if constexpr (GATED) up[0] += *(const v4f *)(s + 16);
+        }
+        fp8_finish<1>(a, p, 0, o, z, up, res);
+    }
+}
+
+template <bool GATED, int NB>
+hipError_t launch(const wq_fp8_product &a, hipStream_t s) {
+    wq_fp8_rows_grid t;
+    t.nO = (a.outs + 15) / 16;
+    t.total = t.nO * ((a.rows + 16 * NB - 1) / (16 * NB));
+    t.per_xcd = (t.total + 7) / 8;
+    hipLaunchKernelGGL((k_fp8_rows<GATED, NB>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * kSlices), 0, s, a, t);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t wq_launch_fp8_rows(const wq_fp8_product &p, int row_blocks, hipStream_t s) {
+    if (p.gated) return row_blocks == 1 ? launch<true, 1>(p, s) : launch<true, 2>(p, s);
+    return row_blocks == 1 ? launch<false, 1>(p, s) : launch<false, 2>(p, s);
+}

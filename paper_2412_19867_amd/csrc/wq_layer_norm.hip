@@ -1,0 +1,481 @@
+// Layer norm: y = (h - mean) / sqrt(var + eps) gamma + beta with h = x + residual, as rows of a float type or as e4m3 codes with a
+// scale for each 128 columns; and its gradient.
+#include <float.h>
+
+#include "wq_fp8_args.h"
+#include "wq_layer_norm.h"
+#include "wq_layer_norm_args.h"
+
+namespace {
+
+// Rows in pieces of eight elements a lane, held in registers: one pass over the data.  `wpr` waves share a row of up to 512 V wpr
+// elements.
+template <int TYPE, bool CODES, int V>
+__global__ __launch_bounds__(512) void k_layer_norm(const wq_layer_norm_args a, int wpr, unsigned run) {
+    using T = typename Elem<TYPE>::type;
+    __shared__ double part[8][2];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int upw = (int)(blockDim.x >> 6) / wpr;   // rows of a workgroup
+    // an XCD takes `run` workgroups in a row: neighbouring rows' codes share lines, which its L2 puts together
+    const unsigned turn = blockIdx.x >> 3;
+    const long row = ((long)(turn / run) * 8 * run + (blockIdx.x & 7u) * run + turn % run) * upw + w / wpr;
+    const bool live = row < a.rows;
+    const long p = live ? row : a.rows - 1;   // (waves behind the last row read it again and store nothing)
+    const int c0 = (w % wpr) * 512 + lane * 8, step = 512 * wpr;
+    const T *x = (const T *)a.x + p * a.xs, *res = a.res ? (const T *)a.res + p * a.rs : nullptr;
+    float v[V][8];
+#pragma unroll
+    for (int k = 0; k < V; ++k) load8_some<T>(x + c0 + k * step, a.C - c0 - k * step, v[k]);
+    float origin = (float)x[0];
+    if (res) {
+        origin += (float)res[0];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            float t[8];
+            load8_some<T>(res + c0 + k * step, a.C - c0 - k * step, t);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[k][j] += t[j];
+        }
+    }
+    double sums[2] = {0.0, 0.0};
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const double d = c0 + k * step + j < a.C ? (double)v[k][j] - (double)origin : 0.0;
+            sums[0] += d;
+            sums[1] = __builtin_fma(d, d, sums[1]);
+        }
+    wave_sums(sums);
+    if (wpr > 1) {
+        if (lane == 0) part[w][0] = sums[0], part[w][1] = sums[1];
+        __syncthreads();
+        sums[0] = sums[1] = 0.0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {   // (a loop of wpr turns would wait for LDS in each)
+            const double *s = part[w / wpr * wpr + min(k, wpr - 1)];
+            sums[0] += k < wpr ? s[0] : 0.0;
+            sums[1] += k < wpr ? s[1] : 0.0;
+        }
+    }
+    const norm_stats st = stats_of(sums[0], sums[1], a.C, a.eps);
+    const double mean = (double)origin + st.mean;
+    const float r = (float)st.r;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int c = c0 + k * step, n = a.C - c;
+        if (a.sum && live && n > 0) store8_some<T>((T *)a.sum + p * a.ss + c, n, v[k]);
+        float y[8], gm[8], bt[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) gm[j] = 1.0f, bt[j] = 0.0f;
+        if (a.gamma) load8_some<float>(a.gamma + c, n, gm);
+        if (a.beta) load8_some<float>(a.beta + c, n, bt);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = (float)((double)v[k][j] - mean) * r * gm[j] + bt[j];
+        if constexpr (!CODES) {
+            if (live && n > 0) store8_some<T>((T *)a.y + p * a.ys + c, n, y);
+        } else {   // a group is the eight elements of 16 adjacent lanes
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (j >= n) y[j] = 0.0f;
+                top = max(top, magnitude(y[j]));
+            }
+            top = dpp_max<0xB1>(top);
+            top = dpp_max<0x4E>(top);
+            top = dpp_max<0x141>(top);
+            top = dpp_max<0x140>(top);
+            float s, inv;
+            pow2_scale(top, s, inv);
+            if (!live || c >= a.padded) continue;   // (the last group is filled up with zeros)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] *= inv;
+            *(uint2 *)(a.codes + ((size_t)(c >> 4) * a.P + p) * 16 + (c & 8)) = make_uint2(e4m3x4(y[0], y[1], y[2], y[3]), e4m3x4(y[4], y[5], y[6], y[7]));
+            if ((lane & 15) == 0) a.scales[(size_t)(c >> 7) * a.P + p] = s;
+        }
+    }
+}
+
+// Rows of any length, read three times: a workgroup of four waves to a row, a wave to a group of 128 columns at a time.
+template <int TYPE, bool CODES>
+__global__ __launch_bounds__(256) void k_layer_norm_long(const wq_layer_norm_args a) {
+    using T = typename Elem<TYPE>::type;
+    __shared__ double part[4][2];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const long p = blockIdx.x;
+    const T *x = (const T *)a.x + p * a.xs, *res = a.res ? (const T *)a.res + p * a.rs : nullptr;
+    auto load = [&](int c) { return res ? (float)x[c] + (float)res[c] : (float)x[c]; };
+    const double origin = (double)load(0);
+    __syncthreads();   // (the sum may go where x is: nobody stores before all have the first element)
+    double sums[2] = {0.0, 0.0};
+    for (int c = tid; c < a.C; c += 256) {
+        const double d = (double)load(c) - origin;
+        sums[0] += d;
+        sums[1] = __builtin_fma(d, d, sums[1]);
+    }
+    wave_sums(sums);
+    if (lane == 0) part[w][0] = sums[0], part[w][1] = sums[1];
+    __syncthreads();
+    const norm_stats st = stats_of(part[0][0] + part[1][0] + part[2][0] + part[3][0], part[0][1] + part[1][1] + part[2][1] + part[3][1], a.C, a.eps);
+    const double mean = origin + st.mean;
+    const float r = (float)st.r;
+    for (int g = w; g * kGroup < a.C; g += 4) {
+        float y[2];
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int c = g * kGroup + 2 * lane + k;
+            y[k] = 0.0f;
+            if (c >= a.C) continue;
+            const float h = load(c);
+            if (a.sum) ((T *)a.sum)[p * a.ss + c] = (T)h;
+            y[k] = (float)((double)h - mean) * r * (a.gamma ? a.gamma[c] : 1.0f) + (a.beta ? a.beta[c] : 0.0f);
+            if (!CODES) ((T *)a.y)[p * a.ys + c] = (T)y[k];
+            top = max(top, magnitude(y[k]));
+        }
+        if constexpr (CODES) {
+#pragma unroll
+            for (int m = 32; m > 0; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+            float s, inv;
+            pow2_scale(top, s, inv);
+            const uint32_t codes = e4m3x4(y[0] * inv, y[1] * inv, 0.0f, 0.0f);
+            const int c = g * kGroup + 2 * lane;
+            *(uint16_t *)(a.codes + ((size_t)(c >> 4) * a.P + p) * 16 + (c & 15)) = (uint16_t)codes;
+            if (lane == 0) a.scales[(size_t)g * a.P + p] = s;
+        }
+    }
+}
+
+template <int TYPE, bool CODES>
+void launch_norm(const wq_layer_norm_args &a, hipStream_t s) {
+    const int chunks = (a.C + 511) / 512;   // of a wave's 512 elements
+    if (chunks > 64) {
+        hipLaunchKernelGGL((k_layer_norm_long<TYPE, CODES>), dim3((unsigned)a.rows), dim3(256), 0, s, a);
+        return;
+    }
+    int wpr = 1, V = 1;
+    while (wpr < chunks && wpr < 8) wpr *= 2;
+    while (V * wpr < chunks) V *= 2;
+    const int waves = wpr < 4 ? 4 : wpr, upw = waves / wpr;
+    const long blocks = ((long)a.rows + upw - 1) / upw, share = (blocks + 7) / 8;
+    const unsigned run = (unsigned)(share > 16 ? 16 : share);
+    const dim3 grid((unsigned)((share + run - 1) / run * run * 8)), block(64 * waves);
+    if (V == 1) hipLaunchKernelGGL((k_layer_norm<TYPE, CODES, 1>), grid, block, 0, s, a, wpr, run);
+    else if (V == 2) hipLaunchKernelGGL((k_layer_norm<TYPE, CODES, 2>), grid, block, 0, s, a, wpr, run);
+    else if (V == 4) hipLaunchKernelGGL((k_layer_norm<TYPE, CODES, 4>), grid, block, 0, s, a, wpr, run);
+    else hipLaunchKernelGGL((k_layer_norm<TYPE, CODES, 8>), grid, block, 0, s, a, wpr, run);
+}
+
+// ------------------------------------------------------------ gradient
+// A workgroup's units of `wpr` waves take every units-th row; the weight's and bias's gradients of a unit's rows add up in its lanes'
+// registers and leave as one row of partial sums.
+template <int TYPE, int V>
+__global__ __launch_bounds__(512) void k_layer_norm_grad(const wq_layer_norm_grad_args a, int wpr, int units) {
+    using T = typename Elem<TYPE>::type;
+    __shared__ double part[2][8][4];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int upw = (int)(blockDim.x >> 6) / wpr;
+    const int unit = (int)blockIdx.x * upw + w / wpr;
+    const int c0 = (w % wpr) * 512 + lane * 8, step = 512 * wpr;
+    float gm[V][8], dgamma[V][8], dbeta[V][8];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) gm[k][j] = 1.0f, dgamma[k][j] = 0.0f, dbeta[k][j] = 0.0f;
+        if (a.gamma) load8_some<float>(a.gamma + c0 + k * step, a.C - c0 - k * step, gm[k]);
+    }
+    // (every unit of the workgroup makes the same number of turns: the barriers meet)
+    const int turns = (a.rows + units - 1) / units;
+    for (int i = 0; i < turns; ++i) {
+        const long row = (long)i * units + unit, p = row < a.rows ? row : a.rows - 1;
+        const bool live = row < a.rows;
+        const T *h = (const T *)a.h + p * a.hs, *dy = (const T *)a.dy + p * a.dys;
+        float hv[V][8], dv[V][8];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            load8_some<T>(h + c0 + k * step, a.C - c0 - k * step, hv[k]);
+            load8_some<T>(dy + c0 + k * step, a.C - c0 - k * step, dv[k]);
+        }
+        const double origin = (double)(float)h[0];
+        double sums[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (c0 + k * step + j >= a.C) continue;
+                const double d = (double)hv[k][j] - origin, g = (double)(dv[k][j] * gm[k][j]);
+                sums[0] += d;
+                sums[1] = __builtin_fma(d, d, sums[1]);
+                sums[2] += g;
+                sums[3] = __builtin_fma(g, d, sums[3]);
+            }
+        wave_sums(sums);
+        if (wpr > 1) {   // (two sets of sums in turn: one barrier a row)
+            double(*mine)[4] = part[i & 1];
+            if (lane < 4) mine[w][lane] = lane == 0 ? sums[0] : lane == 1 ? sums[1] : lane == 2 ? sums[2] : sums[3];
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                sums[j] = 0.0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const double s = mine[w / wpr * wpr + min(k, wpr - 1)][j];
+                    sums[j] += k < wpr ? s : 0.0;
+                }
+            }
+        }
+        const norm_stats st = stats_of(sums[0], sums[1], a.C, a.eps);
+        const double mean = origin + st.mean;
+        const float r = (float)st.r;
+        // mean of g, and of g n = g (d - mean d) r
+        const float mg = (float)(sums[2] / a.C), mgn = (float)((sums[3] - st.mean * sums[2]) * st.r / a.C);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const int c = c0 + k * step, n = a.C - c;
+            float dx[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float nn = (float)((double)hv[k][j] - mean) * r;
+                if (live) {
+                    dgamma[k][j] = __builtin_fmaf(dv[k][j], nn, dgamma[k][j]);
+                    dbeta[k][j] += dv[k][j];
+                }
+                dx[j] = r * (dv[k][j] * gm[k][j] - mg - nn * mgn);
+            }
+            if (!a.dx || !live || n <= 0) continue;
+            if (a.res) {
+                float t[8];
+                load8_some<T>((const T *)a.res + p * a.rs + c, n, t);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) dx[j] += t[j];
+            }
+            store8_some<T>((T *)a.dx + p * a.dxs + c, n, dx);
+        }
+    }
+    if (!a.part) return;
+    float *out = a.part + (size_t)unit * 2 * a.C;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int c = c0 + k * step, n = a.C - c;
+        if (n <= 0) continue;
+        store8_some<float>(out + c, n, dgamma[k]);
+        store8_some<float>(out + a.C + c, n, dbeta[k]);
+    }
+}
+
+// dgamma and dbeta of partial rows [units][2][C]: a workgroup takes 64 columns, its four waves a quarter of the rows each.
+__global__ __launch_bounds__(256) void k_layer_norm_columns(const wq_layer_norm_grad_args a, int units) {
+    __shared__ double part[4][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const long c = (long)blockIdx.x * 64 + lane, n = 2L * a.C;
+    double s = 0.0;
+    if (c < n)
+        for (int u = w; u < units; u += 4) s += (double)a.part[(size_t)u * n + c];
+    part[w][lane] = s;
+    __syncthreads();
+    if (w || c >= n) return;
+    s = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+    float *out = c < a.C ? a.dgamma : a.dbeta;
+    const long i = c < a.C ? c : c - a.C;
+    if (out) out[i] = (float)(a.accumulate ? (double)out[i] + s : s);
+}
+
+// Rows of any length: a workgroup to a row, which it reads twice; the rows' mean and factor stay in the workspace for the columns' sums.
+template <int TYPE>
+__global__ __launch_bounds__(256) void k_layer_norm_grad_long(const wq_layer_norm_grad_args a) {
+    using T = typename Elem<TYPE>::type;
+    __shared__ double part[4][4];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const long p = blockIdx.x;
+    const T *h = (const T *)a.h + p * a.hs, *dy = (const T *)a.dy + p * a.dys;
+    const double origin = (double)(float)h[0];
+    __syncthreads();   // (dx may go where h is)
+    double sums[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int c = tid; c < a.C; c += 256) {
+        const double d = (double)(float)h[c] - origin, g = (double)((float)dy[c] * (a.gamma ? a.gamma[c] : 1.0f));
+        sums[0] += d;
+        sums[1] = __builtin_fma(d, d, sums[1]);
+        sums[2] += g;
+        sums[3] = __builtin_fma(g, d, sums[3]);
+    }
+    wave_sums(sums);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (lane == 0) part[w][j] = sums[j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sums[j] = part[0][j] + part[1][j] + part[2][j] + part[3][j];
+    const norm_stats st = stats_of(sums[0], sums[1], a.C, a.eps);
+    const double mean = origin + st.mean;
+    const float r = (float)st.r;
+    if (a.stats && tid == 0) a.stats[2 * p] = mean, a.stats[2 * p + 1] = (double)r;
+    if (!a.dx) return;
+    const float mg = (float)(sums[2] / a.C), mgn = (float)((sums[3] - st.mean * sums[2]) * st.r / a.C);
+    for (int c = tid; c < a.C; c += 256) {
+        const float nn = (float)((double)(float)h[c] - mean) * r, g = (float)dy[c] * (a.gamma ? a.gamma[c] : 1.0f);
+        float dx = r * (g - mg - nn * mgn);
+        if (a.res) dx += (float)((const T *)a.res)[p * a.rs + c];
+        ((T *)a.dx)[p * a.dxs + c] = (T)dx;
+    }
+}
+// Partial sums of the columns of such rows: a workgroup takes 64 columns and one share of the rows, its waves every fourth of them.
+// It runs before dx is stored, which may go where h or dy is.
+template <int TYPE>
+__global__ __launch_bounds__(256) void k_layer_norm_columns_long(const wq_layer_norm_grad_args a, int units) {
+    using T = typename Elem<TYPE>::type;
+    __shared__ float part[2][4][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, unit = blockIdx.y;
+    const long c = (long)blockIdx.x * 64 + lane;
+    float dgamma = 0.0f, dbeta = 0.0f;
+    if (c < a.C)
+        for (long p = (long)unit + (long)w * units; p < a.rows; p += 4L * units) {
+            const float n = (float)((double)(float)((const T *)a.h)[p * a.hs + c] - a.stats[2 * p]) * (float)a.stats[2 * p + 1];
+            const float d = (float)((const T *)a.dy)[p * a.dys + c];
+            dgamma = __builtin_fmaf(d, n, dgamma);
+            dbeta += d;
+        }
+    part[0][w][lane] = dgamma;
+    part[1][w][lane] = dbeta;
+    __syncthreads();
+    if (w || c >= a.C) return;
+    float *out = a.part + (size_t)unit * 2 * a.C + c;
+    out[0] = part[0][0][lane] + part[0][1][lane] + part[0][2][lane] + part[0][3][lane];
+    out[a.C] = part[1][0][lane] + part[1][1][lane] + part[1][2][lane] + part[1][3][lane];
+}
+
+__global__ __launch_bounds__(256) void k_zero_columns(float *dgamma, float *dbeta, int C) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= C) return;
+    if (dgamma) dgamma[c] = 0.0f;
+    if (dbeta) dbeta[c] = 0.0f;
+}
+
+struct grad_form {
+    int wpr, V, waves, blocks, units;   // V = 0: rows of any length
+};
+// Sizes alone decide: the workspace is as large as the most units that so many rows or fewer make.
+grad_form choose_grad_form(int rows, int C) {
+    grad_form f = {1, 1, 4, 0, 0};
+    const int chunks = (C + 511) / 512;
+    if (chunks > 32) return {4, 0, 4, 0, rows < 64 ? rows : 64};
+    while (f.wpr < chunks && f.wpr < 8) f.wpr *= 2;
+    while (f.V * f.wpr < chunks) f.V *= 2;
+    f.waves = f.wpr < 4 ? 4 : f.wpr;
+    const int upw = f.waves / f.wpr, most = 512 * 4 / f.waves;
+    f.blocks = (rows + upw - 1) / upw < most ? (rows + upw - 1) / upw : most;
+    f.units = f.blocks * upw;
+    return f;
+}
+
+template <int TYPE>
+void launch_grad(const wq_layer_norm_grad_args &a, const grad_form &f, hipStream_t s) {
+    const unsigned columns = (unsigned)((2L * a.C + 63) / 64);
+    if (f.V == 0) {
+        if (a.part) {   // the rows' statistics, then the columns, before dx may take their place
+            wq_layer_norm_grad_args first = a;
+            first.dx = nullptr;
+            hipLaunchKernelGGL((k_layer_norm_grad_long<TYPE>), dim3((unsigned)a.rows), dim3(256), 0, s, first);
+            hipLaunchKernelGGL((k_layer_norm_columns_long<TYPE>), dim3((unsigned)((a.C + 63) / 64), (unsigned)f.units), dim3(256), 0, s, a, f.units);
+            hipLaunchKernelGGL(k_layer_norm_columns, dim3(columns), dim3(256), 0, s, a, f.units);
+        }
+        if (a.dx) {
+            wq_layer_norm_grad_args last = a;
+            last.stats = nullptr;
+            hipLaunchKernelGGL((k_layer_norm_grad_long<TYPE>), dim3((unsigned)a.rows), dim3(256), 0, s, last);
+        }
+        return;
+    }
+    const dim3 grid((unsigned)f.blocks), block(64 * f.waves);
+    if (f.V == 1) hipLaunchKernelGGL((k_layer_norm_grad<TYPE, 1>), grid, block, 0, s, a, f.wpr, f.units);
+    else if (f.V == 2) hipLaunchKernelGGL((k_layer_norm_grad<TYPE, 2>), grid, block, 0, s, a, f.wpr, f.units);
+    else hipLaunchKernelGGL((k_layer_norm_grad<TYPE, 4>), grid, block, 0, s, a, f.wpr, f.units);
+    if (a.part) hipLaunchKernelGGL(k_layer_norm_columns, dim3(columns), dim3(256), 0, s, a, f.units);
+}
+
+bool good_type(int type) { return type == WQ_FP32 || type == WQ_BF16 || type == WQ_FP16; }
+
+// A tensor [rows][cols] of the type with a row stride: aligned to its elements, rows that do not overlap.
+bool good_rows(const void *t, int64_t stride, int rows, int cols, int type) {
+    return ((uintptr_t)t % (type == WQ_FP32 ? 4 : 2)) == 0 && (rows <= 1 || (stride >= cols && stride <= INT64_MAX / 16 / rows));
+}
+
+// (offsets of columns are 32 bits wide, a launch has less than 2^32 lanes)
+bool good_size(int rows, int C) { return rows <= 1 << 25 && C <= 1 << 30; }
+
+bool good_eps(double eps) { return eps >= FLT_MIN && eps <= DBL_MAX; }
+
+}  // namespace
+
+bool wq_good_layer_norm(const wq_layer_norm_args &a, int type) {
+    auto good = [&](const void *t, long stride) { return !t || good_rows(t, stride, a.rows, a.C, type); };
+    return a.rows >= 0 && a.C >= 1 && good_type(type) && good_eps(a.eps) && (a.rows == 0 || a.x) && good(a.x, a.xs) && good(a.res, a.rs) &&
+           good(a.sum, a.ss) && good(a.y, a.ys) && !((uintptr_t)a.gamma & 3) && !((uintptr_t)a.beta & 3);
+}
+
+hipError_t wq_launch_layer_norm(const wq_layer_norm_args &a, int type, hipStream_t s) {
+    if (type == WQ_FP32) a.codes ? launch_norm<WQ_FP32, true>(a, s) : launch_norm<WQ_FP32, false>(a, s);
+    else if (type == WQ_BF16) a.codes ? launch_norm<WQ_BF16, true>(a, s) : launch_norm<WQ_BF16, false>(a, s);
+    else a.codes ? launch_norm<WQ_FP16, true>(a, s) : launch_norm<WQ_FP16, false>(a, s);
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ C ABI
+extern "C" {
+
+wq_status_t wq_layer_norm(void *stream, int rows, int C, int type, const void *x_dev, int64_t x_stride,
+                          const void *residual_dev, int64_t residual_stride, const float *gamma_dev, const float *beta_dev,
+                          double eps, void *sum_dev, int64_t sum_stride, void *y_dev, int64_t y_stride) {
+    wq_layer_norm_args a = {};
+    a.x = x_dev; a.res = residual_dev; a.sum = sum_dev; a.y = y_dev; a.gamma = gamma_dev; a.beta = beta_dev;
+    a.xs = x_stride; a.rs = residual_stride; a.ss = sum_stride; a.ys = y_stride;
+    a.rows = rows; a.C = C; a.eps = eps;
+    if (!wq_good_layer_norm(a, type) || (rows != 0 && !y_dev)) return WQ_ERR_INVALID_ARG;
+    if (!good_size(rows, C)) return WQ_ERR_UNSUPPORTED;
+    if (rows == 0) return WQ_OK;
+    return wq_launch_layer_norm(a, type, (hipStream_t)stream) == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;
+}
+
+wq_status_t wq_layer_norm_workspace(int rows, int C, uint64_t *bytes) {
+    if (rows < 0 || C < 1 || !bytes) return WQ_ERR_INVALID_ARG;
+    if (!good_size(rows, C)) return WQ_ERR_UNSUPPORTED;
+    const grad_form f = choose_grad_form(rows, C);
+    *bytes = ((uint64_t)f.units * 2 * (uint64_t)C * 4 + 255) / 256 * 256 + (f.V == 0 ? (uint64_t)rows * 16 : 0);
+    return WQ_OK;
+}
+
+wq_status_t wq_layer_norm_grad(void *stream, int rows, int C, int type, const void *dy_dev, int64_t dy_stride, const void *h_dev,
+                               int64_t h_stride, const float *gamma_dev, double eps, const void *residual_grad_dev,
+                               int64_t residual_grad_stride, void *dx_dev, int64_t dx_stride, float *dgamma_dev,
+                               float *dbeta_dev, int accumulate, void *workspace_dev, size_t workspace_bytes) {
+    if (rows < 0 || C < 1 || !good_type(type) || !good_eps(eps) || (accumulate != 0 && accumulate != 1)) return WQ_ERR_INVALID_ARG;
+    if (!workspace_dev || (uintptr_t)workspace_dev % 16 || (rows != 0 && (!dy_dev || !h_dev))) return WQ_ERR_INVALID_ARG;
+    if (!good_rows(dy_dev, dy_stride, rows, C, type) || !good_rows(h_dev, h_stride, rows, C, type) ||
+        (residual_grad_dev && !good_rows(residual_grad_dev, residual_grad_stride, rows, C, type)) ||
+        (dx_dev && !good_rows(dx_dev, dx_stride, rows, C, type)) || (((uintptr_t)gamma_dev | (uintptr_t)dgamma_dev | (uintptr_t)dbeta_dev) & 3))
+        return WQ_ERR_INVALID_ARG;
+    uint64_t need;
+    const wq_status_t st = wq_layer_norm_workspace(rows, C, &need);
+    if (st != WQ_OK) return st;
+    if (workspace_bytes < need) return WQ_ERR_WORKSPACE;
+    hipStream_t s = (hipStream_t)stream;
+    const bool columns = dgamma_dev || dbeta_dev;
+    if (rows == 0) {
+        if (!columns || accumulate) return WQ_OK;
+        hipLaunchKernelGGL(k_zero_columns, dim3((unsigned)((C + 255) / 256)), dim3(256), 0, s, dgamma_dev, dbeta_dev, C);
+        return hipGetLastError() == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;
+    }
+    if (!columns && !dx_dev) return WQ_OK;
+    const grad_form f = choose_grad_form(rows, C);
+    wq_layer_norm_grad_args a = {};
+    a.dy = dy_dev; a.h = h_dev; a.res = residual_grad_dev; a.dx = dx_dev; a.gamma = gamma_dev; a.dgamma = dgamma_dev; a.dbeta = dbeta_dev;
+    a.dys = dy_stride; a.hs = h_stride; a.rs = residual_grad_stride; a.dxs = dx_stride;
+    a.rows = rows; a.C = C; a.accumulate = accumulate; a.eps = eps;
+    a.part = columns ? (float *)workspace_dev : nullptr;
+    a.stats = (double *)((char *)workspace_dev + ((uint64_t)f.units * 2 * (uint64_t)C * 4 + 255) / 256 * 256);
+    if (type == WQ_FP32) launch_grad<WQ_FP32>(a, f, s);
+    else if (type == WQ_BF16) launch_grad<WQ_BF16>(a, f, s);
+    else launch_grad<WQ_FP16>(a, f, s);
+    return hipGetLastError() == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;
+}
+
+}  // extern "C"

@@ -29,6 +29,9 @@ EXPORTS = ["wq_standard_transforms", "wq_scaled_transforms", "wq_plan_create", "
            "wq_linear_plan_create_bits", "wq_direct_plan_destroy", "wq_direct_plan_layout",
            "wq_direct_weight_prepare", "wq_direct_quantize", "wq_direct_conv", "wq_direct_forward",
            "wq_rms_norm_quantize", "wq_linear_quantize", "wq_linear_matmul", "wq_linear_forward",
+           "wq_fp8_plan_create", "wq_fp8_plan_destroy", "wq_fp8_plan_layout", "wq_fp8_weight_prepare", "wq_fp8_weight_load",
+           "wq_fp8_quantize", "wq_fp8_layer_norm_quantize", "wq_fp8_matmul", "wq_fp8_forward", "wq_fp8_backward",
+           "wq_layer_norm", "wq_layer_norm_workspace", "wq_layer_norm_grad",
            "wq_conv_forward_debug", "wq_status_string"]
 
 
@@ -49,6 +52,15 @@ class DirectLayout(ctypes.Structure):
                 [(k, ctypes.c_uint64) for k in
                  ("blob_bytes", "blob_Wq_off", "blob_sW_off", "blob_bias_off",
                   "ws_bytes", "ws_xq_off", "ws_sx_off", "ws_part_off")])
+
+
+class Fp8Layout(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_int32) for k in
+                 ("rows", "Cin", "Cout", "in_blocks", "out_blocks", "backward", "fp32_scales", "pad")] +
+                [(k, ctypes.c_uint64) for k in
+                 ("blob_bytes", "blob_codes_off", "blob_scales_off", "blob_bias_off", "blob_codes_t_off", "blob_scales_t_off",
+                  "ws_bytes", "ws_codes_off", "ws_scales_off", "ws_dz_codes_off", "ws_dz_scales_off", "ws_xt_off", "ws_xt_scales_off",
+                  "ws_dzt_off", "ws_dzt_scales_off", "ws_db_off", "ws_part_off")])
 
 
 # wq_k2_variant_t (include/wq.h): the kernel instance of stages 2+3
@@ -113,6 +125,19 @@ def lib() -> ctypes.CDLL:
         L.wq_linear_quantize.argtypes = [vp, vp, ip, ip, vp, ll, vp, sz]
         L.wq_linear_matmul.argtypes = [vp, vp, ip, vp, sz, vp, sz, ip, ip, ip, vp, ll, vp, ll]
         L.wq_linear_forward.argtypes = [vp, vp, ip, ip, vp, ll, vp, sz, vp, sz, ip, ip, vp, ll, vp, ll]
+        L.wq_fp8_plan_create.argtypes = [ctypes.POINTER(vp), ip, ip, ip, ip, ip]
+        L.wq_fp8_plan_destroy.argtypes = [vp]
+        L.wq_fp8_plan_layout.argtypes = [vp, ctypes.POINTER(Fp8Layout)]
+        L.wq_fp8_weight_prepare.argtypes = [vp, vp, ip, vp, ll, vp, vp, sz]
+        L.wq_fp8_weight_load.argtypes = [vp, vp, vp, ll, ip, vp, vp, vp, sz]
+        L.wq_fp8_quantize.argtypes = [vp, vp, ip, ip, vp, ll, vp, sz]
+        L.wq_fp8_layer_norm_quantize.argtypes = [vp, vp, ip, ip, vp, ll, vp, ll, vp, vp, ctypes.c_double, vp, ll, vp, sz]
+        L.wq_fp8_matmul.argtypes = [vp, vp, ip, vp, sz, vp, sz, ip, ip, ip, vp, ll, vp, ll, vp, ll]
+        L.wq_fp8_forward.argtypes = [vp, vp, ip, ip, vp, ll, vp, sz, vp, sz, ip, ip, vp, ll, vp, ll, vp, ll]
+        L.wq_fp8_backward.argtypes = [vp, vp, ip, ip, vp, ll, vp, ll, vp, ll, vp, sz, vp, sz, ip, ip, vp, ll, ip, vp, ll, vp, ip]
+        L.wq_layer_norm.argtypes = [vp, ip, ip, ip, vp, ll, vp, ll, vp, vp, ctypes.c_double, vp, ll, vp, ll]
+        L.wq_layer_norm_workspace.argtypes = [ip, ip, ctypes.POINTER(ctypes.c_uint64)]
+        L.wq_layer_norm_grad.argtypes = [vp, ip, ip, ip, vp, ll, vp, ll, vp, ctypes.c_double, vp, ll, vp, ll, vp, vp, ip, vp, sz]
         L.wq_status_string.argtypes = [ip]
         L.wq_status_string.restype = ctypes.c_char_p
         for name in EXPORTS:
@@ -505,18 +530,11 @@ class DirectPlan:
                "wq_direct_forward")
 
 
-class LinearPlan(DirectPlan):
-    """A group-wise quantized linear layer of up to `rows` rows, with what a transformer block puts
-    around it: the root-mean-square norm with the residual's addition in front of it, bias, activation,
-    gate and residual behind it.  x, residual and outputs are [n][columns] tensors of one float type
-    (fp32, bf16, fp16) with adjacent columns and any row stride, n <= rows; blob and workspace are
-    DirectPlan's.  quantize, conv and forward are the older calls, for all rows in contiguous fp32 without an epilogue: their
-    sums are partly in fp64, linear's in fp32, which takes as long or less for most layers.  All tensors are on the current device, which is the stream's."""
+class _RowCalls:
+    """What calls on rows of tensors check: [n][columns] tensors of one float type with adjacent columns, n <= self._rows."""
 
-    def __init__(self, rows, Cin, Cout, group_size, weight_bits: int = 8):
+    def _look_up(self):
         import torch
-        super().__init__(rows, 1, 1, Cin, Cout, group_size, linear=True, weight_bits=weight_bits)
-        self._rows, self._cin, self._cout = self.layout.P, self.layout.Cin, self.layout.Cout
         # a decoding step makes hundreds of these calls: what they look up is looked up once
         self._tensor_type, self._uint8, self._fp32, self._cuda = torch.Tensor, torch.uint8, torch.float32, torch.cuda
         self._types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -541,8 +559,8 @@ class LinearPlan(DirectPlan):
             raise ValueError(f"{what}: expected a tensor on the device of the others")
         return t.data_ptr(), t.numel()
 
-    def _first(self, t, cols, what):
-        """(rows, dtype, its code, device, address, row stride) of a call's first tensor."""
+    def _first(self, t, cols, what, limit=None):
+        """(rows, dtype, its code, device, address, row stride) of a call's first tensor, of up to `limit` rows (the plan's)."""
         if not isinstance(t, self._tensor_type) or not t.is_cuda:
             raise TypeError(f"{what}: expected a device tensor")
         dtype = t.dtype
@@ -550,8 +568,10 @@ class LinearPlan(DirectPlan):
         if code is None:
             raise TypeError(f"{what}: expected fp32, bf16 or fp16")
         shape = t.shape
-        if len(shape) != 2 or shape[1] != cols or shape[0] > self._rows:
-            raise ValueError(f"{what}: expected shape [up to {self._rows}][{cols}], got {tuple(shape)}")
+        if limit is None:
+            limit = self._rows
+        if len(shape) != 2 or shape[1] != cols or shape[0] > limit:
+            raise ValueError(f"{what}: expected shape [up to {limit}][{cols}], got {tuple(shape)}")
         stride = t.stride()
         if stride[1] != 1 and cols > 1:
             raise ValueError(f"{what}: expected adjacent columns")
@@ -575,6 +595,30 @@ class LinearPlan(DirectPlan):
             raise ValueError(f"{what}: expected a tensor on the device of the others")
         return t.data_ptr(), stride[0]
 
+    def _vector(self, t, cols, device, what):
+        """Address of a contiguous fp32 vector; None of None."""
+        if t is None:
+            return None
+        if not isinstance(t, self._tensor_type) or not t.is_cuda or t.dtype != self._fp32 or not t.is_contiguous():
+            raise TypeError(f"{what}: expected a contiguous fp32 device tensor")
+        if t.numel() != cols or t.get_device() != device:
+            raise ValueError(f"{what}: expected {cols} elements on the device of the others")
+        return t.data_ptr()
+
+
+class LinearPlan(_RowCalls, DirectPlan):
+    """A group-wise quantized linear layer of up to `rows` rows, with what a transformer block puts
+    around it: the root-mean-square norm with the residual's addition in front of it, bias, activation,
+    gate and residual behind it.  x, residual and outputs are [n][columns] tensors of one float type
+    (fp32, bf16, fp16) with adjacent columns and any row stride, n <= rows; blob and workspace are
+    DirectPlan's.  quantize, conv and forward are the older calls, for all rows in contiguous fp32 without an epilogue: their
+    sums are partly in fp64, linear's in fp32, which takes as long or less for most layers.  All tensors are on the current device, which is the stream's."""
+
+    def __init__(self, rows, Cin, Cout, group_size, weight_bits: int = 8):
+        super().__init__(rows, 1, 1, Cin, Cout, group_size, linear=True, weight_bits=weight_bits)
+        self._rows, self._cin, self._cout = self.layout.P, self.layout.Cin, self.layout.Cout
+        self._look_up()
+
     def _epilogue(self, activation, gated):
         act = ACTIVATIONS.get(activation)
         if act is None:
@@ -589,13 +633,7 @@ class LinearPlan(DirectPlan):
         rp, rs = self._other(residual, n, cin, dtype, dev, "residual")
         op, os_ = self._other(out, n, cin, dtype, dev, "out")
         wp, wn = self._buffer(ws, dev, "workspace")
-        gp = None
-        if gamma is not None:
-            if not isinstance(gamma, self._tensor_type) or not gamma.is_cuda or gamma.dtype != self._fp32 or not gamma.is_contiguous():
-                raise TypeError("gamma: expected a contiguous fp32 device tensor")
-            if gamma.numel() != cin or gamma.get_device() != dev:
-                raise ValueError(f"gamma: expected {cin} elements on the device of the others")
-            gp = gamma.data_ptr()
+        gp = self._vector(gamma, cin, dev, "gamma")
         _check(self._lib.wq_rms_norm_quantize(self._h, self._stream(stream, dev), n, code, xp, xs, rp, rs, gp, eps, op, os_, wp,
                                               wn), "wq_rms_norm_quantize")
 
@@ -628,3 +666,201 @@ class LinearPlan(DirectPlan):
         bp, bn = self._buffer(blob, dev, "blob")
         _check(self._lib.wq_linear_forward(self._h, self._stream(stream, dev), n, code, xp, xs, bp, bn, wp, wn, act,
                                            1 if gated else 0, rp, rs, yp, ys), "wq_linear_forward")
+
+
+class Fp8LinearPlan(_RowCalls):
+    """A linear layer of up to `rows` rows in 8-bit floating point (e4m3): a scale for each 128 columns of a row of x and for each
+    block of 128 x 128 of the weights, powers of two unless the plan takes a checkpoint's (`fp32_scales`).  x, residual, preactivation
+    and outputs are [n][columns] tensors of one float type (fp32, bf16, fp16) with adjacent columns and any row stride, n <= rows.  `backward` makes room for the gradients' calls in blob and workspace.  All tensors are on
+    the current device, which is the stream's."""
+
+    def __init__(self, rows, Cin, Cout, backward: bool = False, fp32_scales: bool = False):
+        self._h = ctypes.c_void_p()
+        _check(lib().wq_fp8_plan_create(ctypes.byref(self._h), rows, Cin, Cout, 1 if backward else 0, 1 if fp32_scales else 0),
+               "wq_fp8_plan_create")
+        self.layout = Fp8Layout()
+        _check(lib().wq_fp8_plan_layout(self._h, ctypes.byref(self.layout)), "wq_fp8_plan_layout")
+        self._rows, self._cin, self._cout = rows, Cin, Cout
+        self._look_up()
+
+    def __del__(self):
+        h = getattr(self, "_h", None)
+        if h and _lib is not None:
+            _lib.wq_fp8_plan_destroy(h)
+            self._h = None
+
+    def alloc_blob(self, device="cuda"):
+        import torch
+        return torch.empty(self.layout.blob_bytes, dtype=torch.uint8, device=device)
+
+    def alloc_workspace(self, device="cuda"):
+        import torch
+        return torch.empty(self.layout.ws_bytes, dtype=torch.uint8, device=device)
+
+    # ---- views of the library's formats: pure index permutations ----
+    def workspace_views(self, ws):
+        """(codes [rows][in_blocks 128] e4m3, scales [rows][in_blocks] fp32) of x"""
+        import torch
+        L = self.layout
+        codes = ws[L.ws_codes_off:L.ws_codes_off + L.rows * L.in_blocks * 128].view(torch.float8_e4m3fn)
+        codes = codes.view(L.in_blocks * 8, L.rows, 16).permute(1, 0, 2).reshape(L.rows, -1)
+        scales = ws[L.ws_scales_off:L.ws_scales_off + L.rows * L.in_blocks * 4].view(torch.float32).view(L.in_blocks, L.rows)
+        return codes, scales.t().contiguous()
+
+    def blob_views(self, blob):
+        """(codes [Cout][Cin] e4m3, scales [out_blocks][in_blocks] fp32, bias [Cout])"""
+        import torch
+        L = self.layout
+        R, B = (L.Cout + 15) // 16 * 16, L.in_blocks
+        codes = blob[L.blob_codes_off:L.blob_codes_off + R * B * 128].view(torch.float8_e4m3fn)
+        codes = codes.view(R // 16, B * 8, 16, 16).permute(0, 2, 1, 3).reshape(R, B * 128)[:L.Cout, :L.Cin]
+        scales = blob[L.blob_scales_off:L.blob_scales_off + L.out_blocks * B * 4].view(torch.float32).view(L.out_blocks, B)
+        return codes, scales, blob[L.blob_bias_off:L.blob_bias_off + L.Cout * 4].view(torch.float32)
+
+    def _bias(self, bias, device):
+        return self._vector(bias, self._cout, device, "bias")
+
+    def weight_prepare(self, w, bias, blob, stream=None):
+        """Weights of any float type [Cout][Cin] (any row stride), quantized in blocks into the blob."""
+        n, _, code, dev, wp, ws = self._first(w, self._cin, "w", self._cout)
+        if n != self._cout:
+            raise ValueError(f"w: expected shape [{self._cout}][{self._cin}], got {tuple(w.shape)}")
+        bp, bn = self._buffer(blob, dev, "blob")
+        _check(self._lib.wq_fp8_weight_prepare(self._h, self._stream(stream, dev), code, wp, ws, self._bias(bias, dev), bp, bn),
+               "wq_fp8_weight_prepare")
+
+    def weight_load(self, codes, scales, bias, blob, stream=None):
+        """A checkpoint's weights: codes [Cout][Cin] (float8_e4m3fn, any row stride), scales [out_blocks][in_blocks], fp32 (for plans
+        with fp32_scales) or float8_e8m0fnu, contiguous."""
+        import torch
+        L = self.layout
+        for t, what in ((codes, "codes"), (scales, "scales")):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda:
+                raise TypeError(f"{what}: expected a device tensor")
+        dev = codes.get_device()
+        if codes.dtype != torch.float8_e4m3fn or tuple(codes.shape) != (L.Cout, L.Cin) or (codes.stride(1) != 1 and L.Cin > 1):
+            raise TypeError(f"codes: expected float8_e4m3fn [{L.Cout}][{L.Cin}] with adjacent columns")
+        kind = 0 if scales.dtype == torch.float32 else 1 if scales.dtype == torch.float8_e8m0fnu else None
+        if kind is None or tuple(scales.shape) != (L.out_blocks, L.in_blocks) or not scales.is_contiguous():
+            raise TypeError(f"scales: expected contiguous fp32 or float8_e8m0fnu [{L.out_blocks}][{L.in_blocks}]")
+        if scales.get_device() != dev:
+            raise ValueError("scales: expected a tensor on the device of the others")
+        bp, bn = self._buffer(blob, dev, "blob")
+        _check(self._lib.wq_fp8_weight_load(self._h, self._stream(stream, dev), codes.data_ptr(), codes.stride(0), kind, scales.data_ptr(),
+                                            self._bias(bias, dev), bp, bn), "wq_fp8_weight_load")
+
+    def quantize_rows(self, x, ws, stream=None):
+        """Codes and scales of x into the workspace."""
+        n, _, code, dev, xp, xs = self._first(x, self._cin, "x")
+        wp, wn = self._buffer(ws, dev, "workspace")
+        _check(self._lib.wq_fp8_quantize(self._h, self._stream(stream, dev), n, code, xp, xs, wp, wn), "wq_fp8_quantize")
+
+    def layer_norm_quantize(self, x, ws, residual=None, gamma=None, beta=None, eps=1e-5, out=None, stream=None):
+        """Codes and scales of the layer norm of x + residual into the workspace; `out` (may be x or residual itself) gets
+        x + residual.  gamma, beta: fp32 [Cin]."""
+        cin = self._cin
+        n, dtype, code, dev, xp, xs = self._first(x, cin, "x")
+        rp, rs = self._other(residual, n, cin, dtype, dev, "residual")
+        op, os_ = self._other(out, n, cin, dtype, dev, "out")
+        gp, bp = self._vector(gamma, cin, dev, "gamma"), self._vector(beta, cin, dev, "beta")
+        wp, wn = self._buffer(ws, dev, "workspace")
+        _check(self._lib.wq_fp8_layer_norm_quantize(self._h, self._stream(stream, dev), n, code, xp, xs, rp, rs, gp, bp, eps, op, os_,
+                                                    wp, wn), "wq_fp8_layer_norm_quantize")
+
+    def _epilogue(self, activation, gated):
+        act = ACTIVATIONS.get(activation)
+        if act is None:
+            raise ValueError(f"activation: expected one of {', '.join(ACTIVATIONS)}")
+        return act, self._cout // 2 if gated else self._cout
+
+    def matmul(self, ws, blob, y, activation="none", gated=False, residual=None, preactivation=None, stream=None):
+        """y = act(z) + residual, or act(gate) * up + residual, z the product of the workspace's first len(y) rows with the
+        weights, plus bias; `preactivation` [n][Cout] gets z, which the backward pass needs."""
+        act, outs = self._epilogue(activation, gated)
+        n, dtype, code, dev, yp, ys = self._first(y, outs, "y")
+        rp, rs = self._other(residual, n, outs, dtype, dev, "residual")
+        pp, ps = self._other(preactivation, n, self._cout, dtype, dev, "preactivation")
+        wp, wn = self._buffer(ws, dev, "workspace")
+        bp, bn = self._buffer(blob, dev, "blob")
+        _check(self._lib.wq_fp8_matmul(self._h, self._stream(stream, dev), n, wp, wn, bp, bn, act, 1 if gated else 0, code, rp, rs, pp, ps,
+                                       yp, ys), "wq_fp8_matmul")
+
+    def linear(self, x, blob, ws, y, activation="none", gated=False, residual=None, preactivation=None, stream=None):
+        """quantize_rows followed by matmul; what the workspace holds afterwards is unspecified."""
+        act, outs = self._epilogue(activation, gated)
+        n, dtype, code, dev, xp, xs = self._first(x, self._cin, "x")
+        if y is None:
+            raise TypeError("y: expected a device tensor")
+        yp, ys = self._other(y, n, outs, dtype, dev, "y")
+        rp, rs = self._other(residual, n, outs, dtype, dev, "residual")
+        pp, ps = self._other(preactivation, n, self._cout, dtype, dev, "preactivation")
+        wp, wn = self._buffer(ws, dev, "workspace")
+        bp, bn = self._buffer(blob, dev, "blob")
+        _check(self._lib.wq_fp8_forward(self._h, self._stream(stream, dev), n, code, xp, xs, bp, bn, wp, wn, act, 1 if gated else 0, rp, rs,
+                                        pp, ps, yp, ys), "wq_fp8_forward")
+
+    def backward(self, x, dy, blob, ws, dx=None, dw=None, db=None, preactivation=None, activation="none", gated=False,
+                 accumulate=False, stream=None):
+        """Gradients of linear() from dy, the gradient of y: dx [n][Cin], dw [Cout][Cin] (dy's type or fp32), db fp32 [Cout], those
+        that are given (dw and db added to what they hold with `accumulate`).  preactivation: what linear() kept, needed with an
+        activation or a gate.  x may be None without dw, blob without dx.  The residual's gradient is dy itself."""
+        act, outs = self._epilogue(activation, gated)
+        n, dtype, code, dev, yp, ys = self._first(dy, outs, "dy")
+        xp, xs = self._other(x, n, self._cin, dtype, dev, "x")
+        pp, ps = self._other(preactivation, n, self._cout, dtype, dev, "preactivation")
+        dxp, dxs = self._other(dx, n, self._cin, dtype, dev, "dx")
+        wide = dw is not None and isinstance(dw, self._tensor_type) and dw.dtype == self._fp32
+        dwp, dws = self._other(dw, self._cout, self._cin, self._fp32 if wide else dtype, dev, "dw")
+        dbp = self._vector(db, self._cout, dev, "db")
+        wp, wn = self._buffer(ws, dev, "workspace")
+        bp, bn = self._buffer(blob, dev, "blob") if blob is not None else (None, 0)
+        _check(self._lib.wq_fp8_backward(self._h, self._stream(stream, dev), n, code, xp, xs, yp, ys, pp, ps, bp, bn, wp, wn, act,
+                                         1 if gated else 0, dxp, dxs, 0 if wide else code, dwp, dws, dbp, 1 if accumulate else 0),
+               "wq_fp8_backward")
+
+
+class LayerNormPlan(_RowCalls):
+    """Layer norm of up to `rows` rows of C columns, with its gradient.  Rows are [n][C] tensors of one float type (fp32, bf16,
+    fp16) with adjacent columns and any row stride, n <= rows; gamma, beta and their gradients fp32 [C].  backward needs a workspace,
+    forward none.  All tensors are on the current device, which is the stream's."""
+
+    def __init__(self, rows, C):
+        self._look_up()
+        size = ctypes.c_uint64()
+        _check(self._lib.wq_layer_norm_workspace(rows, C, ctypes.byref(size)), "wq_layer_norm_workspace")
+        self._rows, self._cols, self.ws_bytes = rows, C, size.value
+
+    def alloc_workspace(self, device="cuda"):
+        import torch
+        return torch.empty(max(16, self.ws_bytes), dtype=torch.uint8, device=device)
+
+    def forward(self, x, y, gamma=None, beta=None, eps=1e-5, residual=None, out=None, stream=None):
+        """y = the layer norm of h = x + residual (y may be x or residual itself); `out` gets h, which the backward pass needs."""
+        C = self._cols
+        n, dtype, code, dev, xp, xs = self._first(x, C, "x")
+        if y is None:
+            raise TypeError("y: expected a device tensor")
+        yp, ys = self._other(y, n, C, dtype, dev, "y")
+        rp, rs = self._other(residual, n, C, dtype, dev, "residual")
+        op, os_ = self._other(out, n, C, dtype, dev, "out")
+        gp, bp = self._vector(gamma, C, dev, "gamma"), self._vector(beta, C, dev, "beta")
+        _check(self._lib.wq_layer_norm(self._stream(stream, dev), n, C, code, xp, xs, rp, rs, gp, bp, eps, op, os_, yp, ys),
+               "wq_layer_norm")
+
+    def backward(self, dy, h, ws, dx=None, gamma=None, eps=1e-5, residual_grad=None, dgamma=None, dbeta=None, accumulate=False,
+                 stream=None):
+        """Gradients of forward() from dy, the gradient of y, and h, what was normalized: dx (the gradient of h, and so of x and of
+        the residual; may be dy or h itself) with `residual_grad` added, dgamma and dbeta, those that are given (the latter added
+        to what they hold with `accumulate`)."""
+        C = self._cols
+        n, dtype, code, dev, yp, ys = self._first(dy, C, "dy")
+        if h is None:
+            raise TypeError("h: expected a device tensor")
+        hp, hs = self._other(h, n, C, dtype, dev, "h")
+        rp, rs = self._other(residual_grad, n, C, dtype, dev, "residual_grad")
+        dxp, dxs = self._other(dx, n, C, dtype, dev, "dx")
+        gp = self._vector(gamma, C, dev, "gamma")
+        dgp, dbp = self._vector(dgamma, C, dev, "dgamma"), self._vector(dbeta, C, dev, "dbeta")
+        wp, wn = self._buffer(ws, dev, "workspace")
+        _check(self._lib.wq_layer_norm_grad(self._stream(stream, dev), n, C, code, yp, ys, hp, hs, gp, eps, rp, rs, dxp, dxs, dgp, dbp,
+                                            1 if accumulate else 0, wp, wn), "wq_layer_norm_grad")
