@@ -22,10 +22,10 @@ bool good_rows(const void *t, int64_t stride, int rows, int cols, int type) {
 
 wq_status_t status(hipError_t e) { return e == hipSuccess ? WQ_OK : WQ_ERR_DEVICE; }
 
-// An operand in planes of a piece of all R rows.
-wq_fp8_operand planes(const uint8_t *codes, const float *scales, int rows, int R, int groups) {
+// An operand in planes of a piece of all R rows: codes in `groups` groups of 128, or values in twice as many of 64.
+wq_fp8_operand planes(const void *data, const float *scales, int rows, int R, int groups, bool values) {
     const unsigned piece = 16u * (unsigned)R;
-    return {codes, scales, (unsigned)groups * 8u * piece, 256u, 8u * piece, piece, rows, R};
+    return {(const uint8_t *)data, scales, (unsigned)groups * (values ? 16u : 8u) * piece, 256u, 8u * piece, piece, rows, R};
 }
 // Weights in 16-row blocks.
 wq_fp8_operand blocks(const uint8_t *codes, const float *scales, int rows16, int groups, int scale_step) {
@@ -64,10 +64,31 @@ void set_wide(wq_fp8_product &p) {
 // exact: sums that keep 24 bits (a kernel for few rows, which reads weights all the while, has no others)
 wq_status_t run_product(const wq_fp8_plan *plan, wq_fp8_product &p, bool exact, hipStream_t s) {
     set_wide(p);
-    const wq_fp8_form form = wq_fp8_choose_form(p.rows, p.outs, p.cols, p.groups);
+    const wq_fp8_form form = wq_fp8_choose_form(p.rows, p.outs, p.gated, p.groups, exact);
     if (form.row_blocks) return status(wq_launch_fp8_rows(p, form.row_blocks, s));
     const int mode = exact ? plan->fp32_scales ? WQ_FP8_EXACT_FP32 : WQ_FP8_EXACT : plan->fp32_scales ? WQ_FP8_DIRECT_FP32 : WQ_FP8_DIRECT;
     return status(wq_launch_fp8_tile(p, mode, form.tile, 1, nullptr, s));
+}
+
+bool is_captured(hipStream_t s) {
+    hipStreamCaptureStatus status;
+    if (hipStreamIsCapturing(s, &status) == hipSuccess) return status != hipStreamCaptureStatusNone;
+    (void)hipGetLastError();   // (the question's own: the launch that follows has its answer checked)
+    return false;
+}
+
+// Whether the product takes the rows of x as they are: few of them, and apart from what some workgroups write while others still
+// read x.
+bool quantizes_itself(const wq_fp8_product &p, const void *x, int64_t xs, int Cin, hipStream_t s) {
+    const wq_fp8_form form = wq_fp8_choose_form(p.rows, p.outs, p.gated, p.groups, true);
+    if (!wq_fp8_takes_rows(form, p.rows, Cin, false) || (!wq_fp8_takes_rows(form, p.rows, Cin, true) && is_captured(s))) return false;
+    const int64_t e = type_size(p.type), last = p.rows - 1;
+    const char *x0 = (const char *)x, *x1 = x0 + (last * xs + Cin) * e;
+    auto apart = [&](const void *t, int64_t stride, int cols) {
+        const char *t0 = (const char *)t, *t1 = t0 + (last * stride + cols) * e;
+        return !t || x1 <= t0 || t1 <= x0;
+    };
+    return apart(p.y, p.ys, p.outs) && apart(p.pre, p.ps, p.cols);
 }
 
 wq_fp8_product forward_product(const wq_fp8_plan *plan, int rows, const void *workspace, const void *blob, int activation, int gated, int type,
@@ -76,7 +97,7 @@ wq_fp8_product forward_product(const wq_fp8_plan *plan, int rows, const void *wo
     const wq_fp8_layout_t &L = plan->lay;
     wq_fp8_product p = {};
     p.a = blocks((const uint8_t *)(b + L.blob_codes_off), (const float *)(b + L.blob_scales_off), plan->Cout16, plan->in_blocks, plan->in_blocks);
-    p.b = planes((const uint8_t *)(ws + L.ws_codes_off), (const float *)(ws + L.ws_scales_off), rows, plan->P, plan->in_blocks);
+    p.b = planes((const uint8_t *)(ws + L.ws_codes_off), (const float *)(ws + L.ws_scales_off), rows, plan->P, plan->in_blocks, false);
     p.groups = plan->in_blocks;
     p.bias = (const float *)(b + L.blob_bias_off);
     p.res = res; p.y = y; p.pre = pre; p.rs = res_stride; p.ys = y_stride; p.ps = pre_stride;
@@ -144,7 +165,7 @@ wq_status_t wq_fp8_plan_create(wq_fp8_plan_t **out, int rows, int Cin, int Cout,
     take(L.ws_dzt_off, TB * 256 * Cout16);
     take(L.ws_dzt_scales_off, TB * Cout16 * 4);
     take(L.ws_db_off, TB * (uint64_t)Cout * 4);
-    const int most_slices = wq_fp8_choose_grad_form(Cout, Cin, (int)(2 * TB)).slices;
+    const int most_slices = wq_fp8_choose_grad_form(Cout, Cin, (int)TB).slices;
     take(L.ws_part_off, most_slices > 1 ? (uint64_t)most_slices * Cout * Cin * 4 : 0);
     L.ws_bytes = at;
     p->prepared.store(0);
@@ -244,8 +265,12 @@ wq_status_t wq_fp8_forward(const wq_fp8_plan_t *plan, void *stream, int rows, in
     if (rows == 0) return WQ_OK;
     wq_fp8_product p = forward_product(plan, rows, workspace_dev, weight_blob_dev, activation, gated, type, residual_dev, residual_stride,
                                        pre_dev, pre_stride, y_dev, y_stride);
-    st = wq_fp8_quantize(plan, stream, rows, type, x_dev, x_stride, workspace_dev, workspace_bytes);
-    if (st != WQ_OK) return st;
+    if (quantizes_itself(p, x_dev, x_stride, plan->Cin, (hipStream_t)stream)) {
+        p.x = x_dev; p.xs = x_stride; p.xcols = plan->Cin;
+    } else {
+        st = wq_fp8_quantize(plan, stream, rows, type, x_dev, x_stride, workspace_dev, workspace_bytes);
+        if (st != WQ_OK) return st;
+    }
     return run_product(plan, p, true, (hipStream_t)stream);
 }
 
@@ -279,35 +304,34 @@ wq_status_t wq_fp8_backward(const wq_fp8_plan_t *plan, void *stream, int rows, i
     char *ws = (char *)workspace_dev;
     const int TB = (rows + kGroup - 1) / kGroup;
     const bool wide_values = dw_dev && dw_type == WQ_FP32;   // sums for an fp32 result are of bf16 values
-    const int along = !dw_dev ? 0 : wide_values ? 2 : 1, groups = wide_values ? 2 * TB : TB;
+    const int along = !dw_dev ? 0 : wide_values ? 2 : 1;
     hipError_t e;
 
-    wq_fp8_both_args q = {};
-    q.rows = rows; q.P = plan->P;
-    if (dw_dev) {   // x along the rows
-        q.v = x_dev; q.vs = x_stride; q.cols = plan->Cin; q.colsT = plan->Cin16; q.groups = plan->in_blocks;
-        q.codesT = (uint8_t *)(ws + L.ws_xt_off); q.scalesT = (float *)(ws + L.ws_xt_scales_off);
-        if ((e = wq_launch_fp8_both(q, type, along, s)) != hipSuccess) return status(e);
+    wq_fp8_both_args x = {}, q = {};
+    x.rows = q.rows = rows; x.P = q.P = plan->P;
+    if (dw_dev) {   // along the rows
+        x.v = x_dev; x.vs = x_stride; x.cols = plan->Cin; x.colsT = plan->Cin16; x.groups = plan->in_blocks;
+        x.codesT = (uint8_t *)(ws + L.ws_xt_off); x.scalesT = (float *)(ws + L.ws_xt_scales_off);
     }
     q.v = dy_dev; q.vs = dy_stride; q.pre = through ? pre_dev : nullptr; q.ps = pre_stride; q.act = activation; q.gated = gated;
     q.cols = plan->Cout; q.colsT = plan->Cout16; q.groups = plan->out_blocks;
     q.codesT = (uint8_t *)(ws + L.ws_dzt_off); q.scalesT = (float *)(ws + L.ws_dzt_scales_off);
     q.codes = dx_dev ? (uint8_t *)(ws + L.ws_dz_codes_off) : nullptr; q.scales = (float *)(ws + L.ws_dz_scales_off);
     q.db = db_dev ? (float *)(ws + L.ws_db_off) : nullptr;
-    if ((e = wq_launch_fp8_both(q, type, along, s)) != hipSuccess) return status(e);
+    if ((e = wq_launch_fp8_both(x, q, type, along, s)) != hipSuccess) return status(e);
     if (db_dev && (e = wq_launch_fp8_db(q.db, TB, plan->Cout, db_dev, accumulate, s)) != hipSuccess) return status(e);
 
     if (dw_dev) {   // columns of dw are rows of `a`, x's columns
-        const wq_fp8_form form = wq_fp8_choose_grad_form(plan->Cout, plan->Cin, groups);
+        const wq_fp8_form form = wq_fp8_choose_grad_form(plan->Cout, plan->Cin, TB);
         float *part = (float *)(ws + L.ws_part_off);
         wq_fp8_product p = {};
-        p.a = planes((const uint8_t *)(ws + L.ws_xt_off), (const float *)(ws + L.ws_xt_scales_off), plan->Cin16, plan->Cin16, groups);
-        p.b = planes((const uint8_t *)(ws + L.ws_dzt_off), (const float *)(ws + L.ws_dzt_scales_off), plan->Cout16, plan->Cout16, groups);
-        p.groups = groups;
+        p.a = planes((const uint8_t *)(ws + L.ws_xt_off), (const float *)(ws + L.ws_xt_scales_off), plan->Cin16, plan->Cin16, TB, wide_values);
+        p.b = planes((const uint8_t *)(ws + L.ws_dzt_off), (const float *)(ws + L.ws_dzt_scales_off), plan->Cout16, plan->Cout16, TB, wide_values);
+        p.groups = TB;
         p.y = dw_dev; p.ys = dw_stride; p.rows = plan->Cout; p.outs = p.cols = plan->Cin; p.type = dw_type;
         if (accumulate) p.res = dw_dev, p.rs = dw_stride;
         set_wide(p);
-        if ((e = wq_launch_fp8_tile(p, wide_values ? WQ_FP8_BF16 : WQ_FP8_DIRECT_ROWS, form.tile, form.slices, part, s)) != hipSuccess) return status(e);
+        if ((e = wq_launch_fp8_tile(p, wide_values ? WQ_FP8_VALUES : WQ_FP8_DIRECT_ROWS, form.tile, form.slices, part, s)) != hipSuccess) return status(e);
         if (form.slices > 1 &&
             (e = wq_launch_fp8_join(part, form.slices, plan->Cout, plan->Cin, dw_dev, dw_stride, dw_type, accumulate, s)) != hipSuccess)
             return status(e);
@@ -316,7 +340,7 @@ wq_status_t wq_fp8_backward(const wq_fp8_plan_t *plan, void *stream, int rows, i
         const char *b = (const char *)weight_blob_dev;
         wq_fp8_product p = {};
         p.a = blocks((const uint8_t *)(b + L.blob_codes_t_off), (const float *)(b + L.blob_scales_t_off), plan->Cin16, plan->out_blocks, plan->out_blocks);
-        p.b = planes((const uint8_t *)(ws + L.ws_dz_codes_off), (const float *)(ws + L.ws_dz_scales_off), rows, plan->P, plan->out_blocks);
+        p.b = planes((const uint8_t *)(ws + L.ws_dz_codes_off), (const float *)(ws + L.ws_dz_scales_off), rows, plan->P, plan->out_blocks, false);
         p.groups = plan->out_blocks;
         p.y = dx_dev; p.ys = dx_stride; p.rows = rows; p.outs = p.cols = plan->Cin; p.type = type;
         return run_product(plan, p, type == WQ_FP32, s);

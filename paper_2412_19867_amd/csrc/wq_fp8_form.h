@@ -2,22 +2,62 @@
 // that runs on the host.
 #pragma once
 
+// Workgroup tiles: weight rows x rows of x, and teams of waves that share their K.
+enum wq_fp8_tile_form {
+    WQ_FP8_TILE_256 = 0,
+    WQ_FP8_TILE_128 = 1,
+    WQ_FP8_TILE_128x64 = 2,
+    WQ_FP8_TILE_64 = 3,
+    WQ_FP8_TILE_64_2 = 4,   // two teams
+    WQ_FP8_TILE_64_4 = 5    // four
+};
+
 struct wq_fp8_form {
     int row_blocks;   // few rows: 16-row blocks of a workgroup, 1 or 2; 0: tiles
-    int tile;
+    int tile;         // a wq_fp8_tile_form
     int slices;       // of K, joined by a second kernel (the weights' gradient)
 };
 
-// y [rows][outs] from K in `groups` groups; cols: rows of the weights
-inline wq_fp8_form wq_fp8_choose_form(int rows, int outs, int cols, int groups) {
-    if (rows <= 32) return {rows <= 16 ? 1 : 2, 0, 1};
-    return {0, 0, 1};
+inline long wq_fp8_tiles(int outs, int rows, int across, int down) {
+    return (long)((outs + across - 1) / across) * ((rows + down - 1) / down);
 }
 
-// dw [Cout][Cin] from groups of rows
+// y [rows][outs] from K in `groups` groups of 128; gated: outs columns from twice as many weight rows, so tiles are half as wide.
+// exact: bf16 sums, else codes (half the time in the matrix core).  Over 104 drawn layers of 33 to 8192 rows the rules are 1.5 % (1.1 % where
+// not exact) from the best of the tiles in the geometric mean, 18 % at most.  us on either side of each line, 4096x.. for rows x K -> columns:
+//   rows: up to 128 of them while there are at most 900 blocks of 16 x 16 (64x6592->1728 7.4, tiles 18.0; 80x1792->2048 6.5, 8.7;
+//     52x7744->9152, 2288 blocks: 27.8, 20.7); one block of rows a workgroup up to 16 rows or 256 blocks, else two
+//   256: reductions from 2048 on where the last round of 256 of them wastes less than they gain over 128 (a fifth):
+//     4096x4096->2x8192 393, 443; 2472x4608->2x2912 104, 121; 1000x1280->2x5120 38.5, 35
+//   128: the same from 384 of them (512x4096->2x8192 59, of 128x64 70; 512x8192->4096, 128 of them: 80, 42 with two teams)
+//   128x64 from 384, 64 x 64 from 192 (512), two teams from 40 (192) tiles of 64, else four: CUs with enough waves
+inline wq_fp8_form wq_fp8_choose_form(int rows, int outs, bool gated, int groups, bool exact) {
+    const int half = gated ? 2 : 1;
+    const long blocks = wq_fp8_tiles(outs, rows, 16, 16);
+    if (rows <= 128 && blocks <= 900) return {rows <= 16 || blocks <= 256 ? 1 : 2, 0, 1};
+    const long n256 = wq_fp8_tiles(outs, rows, 256 / half, 256), n128 = wq_fp8_tiles(outs, rows, 128 / half, 128);
+    const long n64 = wq_fp8_tiles(outs, rows, 64 / half, 64);
+    if (groups >= 16 && (n256 + 255) / 256 * 256 <= 0.3 * n128) return {0, WQ_FP8_TILE_256, 1};
+    if (groups >= 16 && n128 >= 384) return {0, WQ_FP8_TILE_128, 1};
+    if (wq_fp8_tiles(outs, rows, 128 / half, 64) >= 384) return {0, WQ_FP8_TILE_128x64, 1};
+    return {0, n64 >= (exact ? 192 : 512) ? WQ_FP8_TILE_64 : n64 >= (exact ? 40 : 192) ? WQ_FP8_TILE_64_2 : WQ_FP8_TILE_64_4, 1};
+}
+
+// dw [Cout][Cin] from groups of 128 rows.
 inline wq_fp8_form wq_fp8_choose_grad_form(int Cout, int Cin, int groups) {
-    const long tiles = (long)((Cout + 127) / 128) * ((Cin + 127) / 128);
-    long slices = tiles ? 256 / tiles : 1;
-    if (slices > groups / 4) slices = groups / 4;
-    return {0, 0, slices < 1 ? 1 : (int)slices};
+    const long n256 = wq_fp8_tiles(Cin, Cout, 256, 256), n128 = wq_fp8_tiles(Cin, Cout, 128, 128), n64 = wq_fp8_tiles(Cin, Cout, 64, 64);
+    if (groups >= 7 && (n256 + 255) / 256 * 256 <= 0.3 * n128) return {0, WQ_FP8_TILE_256, 1};
+    if (groups >= 7 && n128 >= 270) return {0, WQ_FP8_TILE_128, 1};
+    if (groups < 4 || n64 >= 512) return {0, WQ_FP8_TILE_64, 1};
+    return {0, n64 >= 192 ? WQ_FP8_TILE_64_2 : WQ_FP8_TILE_64_4, 1};
+}
+
+// Whether the product for few rows may take rows of x as they are, as far as sizes go: up to 16384 elements of a workgroup's 16 rows,
+// every workgroup quantizing its own (12288 in a stream that is being captured, which has the card's time to save but not the host's).
+inline bool wq_fp8_takes_rows(const wq_fp8_form &form, int rows, int Cin, bool captured) {
+    return form.row_blocks == 1 && (rows < 16 ? rows : 16) * (long)Cin <= (captured ? 12288 : 16384);
+}
+// Waves to such a workgroup: four multiply, four more help to quantize where that counts and all workgroups are on the card at once.
+inline int wq_fp8_row_waves(int rows, int Cin, long blocks) {
+    return (rows < 16 ? rows : 16) * (long)Cin >= (blocks <= 512 ? 2048 : 10240 + 8 * (blocks - 512)) ? 8 : 4;
 }

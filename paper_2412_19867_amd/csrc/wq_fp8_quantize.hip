@@ -1,5 +1,6 @@
 // Rows into e4m3 codes with power-of-two scales: along the rows' columns, along the rows (for the weights' gradient), weights in blocks; the
 // gradient through activation and gate on the way.
+#include "wq_column_sums.h"
 #include "wq_fp8_quantize.h"
 #include "wq_layer_norm.h"
 
@@ -105,15 +106,18 @@ __device__ __forceinline__ void activation_slope(const float (&z)[N], int act, f
 // the groups along the columns are 16 lanes', those along the rows a lane's eight and its counterparts' in the other 15 sixteenths of
 // the workgroup.  Codes leave through LDS, where they lie as in memory.
 //   ALONG: 0 no codes along the rows, 1 codes, 2 values in bf16.
+//   Two tensors in one launch: the first `blocks` workgroups take the first.
 template <int TYPE, int ALONG>
-__global__ __launch_bounds__(256) void k_fp8_both(const wq_fp8_both_args a) {
+__global__ __launch_bounds__(256, ALONG == 0 ? 4 : 3) void k_fp8_both(const wq_fp8_both_args first, const wq_fp8_both_args second, unsigned blocks) {
     using T = typename Elem<TYPE>::type;
     constexpr int STRIDE = 16 * 128 + 16 * 16;   // bytes of a plane of 128 columns' pieces in LDS, 16 of them between each eight columns
-    __shared__ __attribute__((aligned(16))) char image[16 * STRIDE];
+    __shared__ __attribute__((aligned(16))) char image[(ALONG == 2 ? 16 : 8) * STRIDE];
+    const wq_fp8_both_args a = blockIdx.x < blocks ? first : second;
+    const unsigned id = blockIdx.x < blocks ? blockIdx.x : blockIdx.x - blocks;
     __shared__ uint32_t top_s[4][128];
     __shared__ float sum_s[4][128];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, octet = lane & 15, sub = tid >> 4;
-    const int g = blockIdx.x % a.groups, tb = blockIdx.x / a.groups;
+    const int g = id % a.groups, tb = id / a.groups;
     const int c = g * kGroup + octet * 8, p0 = tb * kGroup + sub * 8;
     const int outs = a.gated ? a.cols / 2 : a.cols;
     const bool up = a.gated && c >= outs;   // (outs is a multiple of 32: all eight columns are of one half)
@@ -234,15 +238,14 @@ __global__ __launch_bounds__(256) void k_fp8_both(const wq_fp8_both_args a) {
     }
 }
 
-// db of partial sums [blocks][cols], or the weights' gradient of K's slices [blocks][rows cols]: one value a lane, in the slices' order.
-__global__ __launch_bounds__(256) void k_fp8_db(const float *part, int blocks, int cols, float *db, int accumulate) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= cols) return;
-    double s = accumulate ? (double)db[c] : 0.0;
-    for (int b = 0; b < blocks; ++b) s += (double)part[(size_t)b * cols + c];
-    db[c] = (float)s;
+// db of partial sums [blocks][cols].
+__global__ __launch_bounds__(1024) void k_fp8_db(const float *part, int blocks, int cols, float *db, int accumulate) {
+    const long c = (long)blockIdx.x * 64 + (threadIdx.x & 63);
+    const double s = column_sum(part, blocks, cols, c, c < cols);
+    if (threadIdx.x < 64 && c < cols) db[c] = (float)(accumulate ? (double)db[c] + s : s);
 }
 
+// The weights' gradient of K's slices [slices][rows cols], in the slices' order.
 template <typename T>
 __global__ __launch_bounds__(256) void k_fp8_join(const float *part, int slices, int rows, int cols, T *dw, long stride, int accumulate) {
     const long i = (long)blockIdx.x * 256 + threadIdx.x, n = (long)rows * cols;
@@ -349,11 +352,12 @@ __global__ __launch_bounds__(256) void k_fp8_weights(const wq_fp8_weight_args a)
 }
 
 template <int TYPE>
-void launch_both(const wq_fp8_both_args &a, int along, hipStream_t s) {
-    const dim3 grid((unsigned)a.groups * (unsigned)((a.rows + kGroup - 1) / kGroup)), block(256);
-    if (along == 0) hipLaunchKernelGGL((k_fp8_both<TYPE, 0>), grid, block, 0, s, a);
-    else if (along == 1) hipLaunchKernelGGL((k_fp8_both<TYPE, 1>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((k_fp8_both<TYPE, 2>), grid, block, 0, s, a);
+void launch_both(const wq_fp8_both_args &x, const wq_fp8_both_args &dy, int along, hipStream_t s) {
+    const unsigned bands = (unsigned)((dy.rows + kGroup - 1) / kGroup), blocks = x.v ? (unsigned)x.groups * bands : 0u;
+    const dim3 grid(blocks + (unsigned)dy.groups * bands), block(256);
+    if (along == 0) hipLaunchKernelGGL((k_fp8_both<TYPE, 0>), grid, block, 0, s, x, dy, blocks);
+    else if (along == 1) hipLaunchKernelGGL((k_fp8_both<TYPE, 1>), grid, block, 0, s, x, dy, blocks);
+    else hipLaunchKernelGGL((k_fp8_both<TYPE, 2>), grid, block, 0, s, x, dy, blocks);
 }
 
 }  // namespace
@@ -367,15 +371,15 @@ hipError_t wq_launch_fp8_quantize(const wq_fp8_rows_args &a, int type, hipStream
     return hipGetLastError();
 }
 
-hipError_t wq_launch_fp8_both(const wq_fp8_both_args &a, int type, int along, hipStream_t s) {
-    if (type == WQ_FP32) launch_both<WQ_FP32>(a, along, s);
-    else if (type == WQ_BF16) launch_both<WQ_BF16>(a, along, s);
-    else launch_both<WQ_FP16>(a, along, s);
+hipError_t wq_launch_fp8_both(const wq_fp8_both_args &x, const wq_fp8_both_args &dy, int type, int along, hipStream_t s) {
+    if (type == WQ_FP32) launch_both<WQ_FP32>(x, dy, along, s);
+    else if (type == WQ_BF16) launch_both<WQ_BF16>(x, dy, along, s);
+    else launch_both<WQ_FP16>(x, dy, along, s);
     return hipGetLastError();
 }
 
 hipError_t wq_launch_fp8_db(const float *part, int blocks, int cols, float *db, int accumulate, hipStream_t s) {
-    hipLaunchKernelGGL(k_fp8_db, dim3((unsigned)((cols + 255) / 256)), dim3(256), 0, s, part, blocks, cols, db, accumulate);
+    hipLaunchKernelGGL(k_fp8_db, dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, s, part, blocks, cols, db, accumulate);
     return hipGetLastError();
 }
 

@@ -1,34 +1,37 @@
 // The product of the linear layer in 8-bit floating point for few rows (down to one: decoding): the weights are what is read.
 #include "wq_fp8_tile.h"
-#include "wq_quantize_piece.h"
+#include "wq_layer_norm.h"
 
 namespace {
 
 struct wq_fp8_rows_grid {
-    int nO, total, per_xcd;   // tiles along the columns of y, their number, the share of each XCD
+    int waves, nO, total, per_xcd;   // waves to a workgroup, tiles along the columns of y, their number, the share of each XCD
 };
 
-constexpr int kSlices = 4;   // waves that share a tile's reduction
+constexpr int kSlices = 4;   // waves that share a tile's reduction (others only help to quantize x)
 
 // A workgroup owns 16 columns of y (gated: and the 16 rows of `a` that go with them in the second half) x 16 NB rows; each of its four
 // waves takes a contiguous part of K for all of them and asks for D groups ahead: nothing is staged, a wave waits for its own loads
 // alone.  Codes are multiplied as bf16 numbers, x's with their power of two; a multiply-add applies the weights' scale, any fp32 number.
-template <bool GATED, int NB>
-__global__ __launch_bounds__(256) void k_fp8_rows(const wq_fp8_product a, const wq_fp8_rows_grid t) {
+// FUSED: the workgroup quantizes the rows of x itself, into LDS, while its first weights are on their way: a launch less, with the
+// bits of two.
+template <bool GATED, int NB, bool FUSED>
+__global__ __launch_bounds__(FUSED ? 512 : 256) void k_fp8_rows(const wq_fp8_product a, const wq_fp8_rows_grid t) {
     constexpr int NE = GATED ? 2 : 1, D = 4;
     constexpr int RS = 16 * NE + 4;
-    __shared__ __attribute__((aligned(16))) float part_s[kSlices * 16 * RS];
+    constexpr int XOFF = kSlices * 16 * RS * 4;   // FUSED: bytes of LDS before the codes of x
+    extern __shared__ __attribute__((aligned(16))) float part_s[];   // [kSlices][16][RS]
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, q = lane >> 4;
     const int ks = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int logical = (int)(blockIdx.x & 7u) * t.per_xcd + (int)(blockIdx.x >> 3);
     if (logical >= t.total) return;   // the whole workgroup leaves, before any barrier
     const int ob = logical % t.nO, p0 = logical / t.nO * 16 * NB;
 
-    const __amdgpu_buffer_rsrc_t rA = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.a.codes), 0, (int)a.a.bytes, kBufFlags);
-    const __amdgpu_buffer_rsrc_t rB = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.b.codes), 0, (int)a.b.bytes, kBufFlags);
+    const __amdgpu_buffer_rsrc_t rA = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.a.data), 0, (int)a.a.bytes, kBufFlags);
+    const __amdgpu_buffer_rsrc_t rB = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.b.data), 0, (int)a.b.bytes, kBufFlags);
     const __amdgpu_buffer_rsrc_t rSB = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<float *>(a.b.scales), 0, (int)((unsigned)a.groups * (unsigned)a.b.scale_step * 4u), kBufFlags);
-    const int c_beg = ks * a.groups / kSlices, len = (ks + 1) * a.groups / kSlices - c_beg;
+    const int c_beg = min(ks, kSlices) * a.groups / kSlices, len = min(ks + 1, kSlices) * a.groups / kSlices - c_beg;
     // neighbouring tiles walk their parts from different places on: from the same one they would ask for addresses a power of two
     // apart where K is one, all in a few of the memory's channels
     const int first = len ? ob % len : 0;
@@ -50,8 +53,13 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const wq_fp8_product a, const 
         vB[f] = (unsigned)(p >> 4) * a.b.block + (unsigned)q * a.b.piece + (unsigned)(p & 15) * 16u;
         vSB[f] = (unsigned)p * 4u;
     }
-    v4i av[D][NE][2], bv[D][NB][2];
-    float sb[D][NB], sa[D][NE];
+    // FUSED: codes [groups][8 pieces][rows][16] and scales [groups][rows] of the workgroup's rows of x in LDS
+    const int x_rows = min(16, a.rows - p0), lrow = min(l16, x_rows - 1);
+    char *codes_s = (char *)part_s + XOFF;
+    float *scales_s = (float *)(codes_s + x_rows * a.groups * kGroup);
+    constexpr int DB = FUSED ? 1 : D;
+    v4i av[D][NE][2], bv[DB][NB][2];
+    float sb[DB][NB], sa[D][NE];
     auto fetch = [&](int d, int i) {   // into slot d (a constant after unrolling)
         const int c = chunk(i);
 #pragma unroll
@@ -61,7 +69,7 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const wq_fp8_product a, const 
             sa[d][e] = sA[e][c];
         }
 #pragma unroll
-        for (int f = 0; f < NB; ++f) {
+        for (int f = 0; f < (FUSED ? 0 : NB); ++f) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 bv[d][f][h] = __builtin_amdgcn_raw_buffer_load_b128(rB, vB[f] + h * 4u * a.b.piece, (unsigned)c * a.b.group, 0);
@@ -73,7 +81,14 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const wq_fp8_product a, const 
     for (int e = 0; e < NE; ++e)
 #pragma unroll
         for (int f = 0; f < NB; ++f) M[e][f] = v4f{0.f, 0.f, 0.f, 0.f};
-    auto compute = [&](int d) {
+    auto compute = [&](int d, int i) {
+        const int xd = FUSED ? 0 : d;
+        if constexpr (FUSED) {
+            const int c = chunk(i);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) bv[0][0][h] = *(const v4i *)(codes_s + ((c * 8 + h * 4 + q) * x_rows + lrow) * 16);
+            sb[0][0] = scales_s[c * x_rows + lrow];
+        }
 #pragma unroll
         for (int e = 0; e < NE; ++e) {
             v4f P[NB];
@@ -85,7 +100,7 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const wq_fp8_product a, const 
 #pragma unroll
                 for (int f = 0; f < NB; ++f)
                     P[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        x, bf16_of_codes(bv[d][f][k >> 1][(k & 1) * 2], bv[d][f][k >> 1][(k & 1) * 2 + 1], sb[d][f]), P[f], 0, 0, 0);
+                        x, bf16_of_codes(bv[xd][f][k >> 1][(k & 1) * 2], bv[xd][f][k >> 1][(k & 1) * 2 + 1], sb[xd][f]), P[f], 0, 0, 0);
             }
 #pragma unroll
             for (int f = 0; f < NB; ++f)
@@ -93,17 +108,54 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const wq_fp8_product a, const 
                 for (int r = 0; r < 4; ++r) M[e][f][r] = __builtin_fmaf(P[f][r], sa[d][e], M[e][f][r]);
         }
     };
+    // x: pieces of 512 elements of a row, a wave's first one asked for ahead of the weights (loads come back in order)
+    const int chunks = (a.xcols + 511) / 512, pieces = FUSED ? x_rows * chunks : 0;
+    float v[8];
+    auto load_piece = [&](int i) {
+        const int c = i % chunks * 512 + lane * 8, n = i < pieces ? a.xcols - c : 0;
+        const long at = (p0 + (long)(i / chunks)) * a.xs + c;
+        if (a.type == WQ_FP32) load8_some((const float *)a.x + at, n, v);
+        else if (a.type == WQ_BF16) load8_some((const __bf16 *)a.x + at, n, v);
+        else load8_some((const _Float16 *)a.x + at, n, v);
+    };
+    if constexpr (FUSED) {
+        load_piece(ks);
+        __builtin_amdgcn_sched_barrier(0);
+    }
     if (len) {
 #pragma unroll
         for (int d = 0; d < D; ++d) {
             fetch(d, d);
             __builtin_amdgcn_sched_barrier(0);
         }
+    }
+    if constexpr (FUSED) {
+        for (int i = ks; i < pieces; i += t.waves) {
+            if (i != ks) load_piece(i);
+            const int row = i / chunks, c = i % chunks * 512 + lane * 8;
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[j]));
+            top = dpp_max<0xB1>(top);
+            top = dpp_max<0x4E>(top);
+            top = dpp_max<0x141>(top);
+            top = dpp_max<0x140>(top);
+            float s, r;
+            pow2_scale(top, s, r);
+            if (c >= a.groups * kGroup) continue;   // (the last group is filled up with zeros)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= r;
+            *(uint2 *)(codes_s + ((c >> 4) * x_rows + row) * 16 + (c & 8)) = make_uint2(e4m3x4(v[0], v[1], v[2], v[3]), e4m3x4(v[4], v[5], v[6], v[7]));
+            if ((c & (kGroup - 1)) == 0) scales_s[(c >> 7) * x_rows + row] = s;
+        }
+        __syncthreads();
+    }
+    if (len) {
         int i = 0;
         for (; i + D <= len; i += D) {   // whole rounds of the ring, then the rest
 #pragma unroll
             for (int d = 0; d < D; ++d) {
-                compute(d);
+                compute(d, i + d);
                 __builtin_amdgcn_sched_barrier(0);
                 fetch(d, i + d + D);
                 __builtin_amdgcn_sched_barrier(0);
@@ -111,7 +163,7 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const wq_fp8_product a, const 
         }
 #pragma unroll
         for (int d = 0; d < D - 1; ++d)
-            if (i + d < len) compute(d);
+            if (i + d < len) compute(d, i + d);
     }
 
     // ---- the waves' sums through LDS, 16 rows at a time, then the epilogue ----
@@ -120,7 +172,8 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const wq_fp8_product a, const 
     for (int f = 0; f < NB; ++f) {
         if (f) __syncthreads();   // the rows before have been read
 #pragma unroll
-        for (int e = 0; e < NE; ++e) *(v4f *)&mine[l16 * RS + 16 * e + 4 * q] = M[e][f];
+        for (int e = 0; e < NE; ++e)
+            if (!FUSED || ks < kSlices) *(v4f *)&mine[l16 * RS + 16 * e + 4 * q] = M[e][f];
         __syncthreads();
         const int row = tid >> 2, c = (tid & 3) * 4, p = p0 + 16 * f + row, o = ob * 16 + c;
         if (tid >= 64 || p >= a.rows || o >= a.outs) continue;
@@ -138,19 +191,26 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const wq_fp8_product a, const 
     }
 }
 
-template <bool GATED, int NB>
+template <bool GATED, int NB, bool FUSED>
 hipError_t launch(const wq_fp8_product &a, hipStream_t s) {
     wq_fp8_rows_grid t;
     t.nO = (a.outs + 15) / 16;
     t.total = t.nO * ((a.rows + 16 * NB - 1) / (16 * NB));
     t.per_xcd = (t.total + 7) / 8;
-    hipLaunchKernelGGL((k_fp8_rows<GATED, NB>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * kSlices), 0, s, a, t);
+    t.waves = FUSED ? wq_fp8_row_waves(a.rows, a.xcols, t.total) : kSlices;
+    const size_t lds = kSlices * 16 * (16 * (GATED ? 2 : 1) + 4) * 4 + (FUSED ? (size_t)min(a.rows, 16) * a.groups * (kGroup + 4) : 0);
+    hipLaunchKernelGGL((k_fp8_rows<GATED, NB, FUSED>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * t.waves), lds, s, a, t);
     return hipGetLastError();
+}
+
+template <bool GATED>
+hipError_t launch_blocks(const wq_fp8_product &a, int row_blocks, hipStream_t s) {
+    if (a.x) return launch<GATED, 1, true>(a, s);
+    return row_blocks == 1 ? launch<GATED, 1, false>(a, s) : launch<GATED, 2, false>(a, s);
 }
 
 }  // namespace
 
 hipError_t wq_launch_fp8_rows(const wq_fp8_product &p, int row_blocks, hipStream_t s) {
-    if (p.gated) return row_blocks == 1 ? launch<true, 1>(p, s) : launch<true, 2>(p, s);
-    return row_blocks == 1 ? launch<false, 1>(p, s) : launch<false, 2>(p, s);
+    return p.gated ? launch_blocks<true>(p, row_blocks, s) : launch_blocks<false>(p, row_blocks, s);
 }

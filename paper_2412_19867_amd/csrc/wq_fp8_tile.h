@@ -2,6 +2,7 @@
 #pragma once
 
 #include "wq_fp8_args.h"
+#include "wq_fp8_form.h"
 #include "wq_linear_args.h"
 
 namespace {
@@ -12,9 +13,12 @@ __device__ __forceinline__ void lds_load4(__amdgpu_buffer_rsrc_t r, char *lds, u
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, WQ_LDS_PTR(lds), 4, voff, soff, 0, 0);
 }
 
-// Until the wave's loads and LDS reads are done, then the workgroup's barrier.
+// Until at most VM of the wave's loads are outstanding (they complete in order) and its LDS reads are done, then the
+// workgroup's barrier.
+template <int VM>
 __device__ __forceinline__ void wait_and_barrier() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    static_assert(VM >= 0 && VM < 64, "vmcnt is a 6-bit counter");
+    asm volatile("s_waitcnt %0\n\ts_barrier" ::"n"(0x0070 | (VM & 0xf) | ((VM >> 4) << 14)) : "memory");
 }
 
 struct wq_fp8_grid {
@@ -56,22 +60,24 @@ __device__ __forceinline__ v4f fp8_residual(const wq_fp8_product &a, long p, int
 // (the bias is padded to whole blocks, a column's own four always lie in it)
 __device__ __forceinline__ v4f fp8_bias(const wq_fp8_product &a, int o) { return a.bias ? *(const v4f *)(a.bias + o) : v4f{}; }
 
-// WA x WB waves, each with NA x NB blocks of 16 x 16 (a's rows x b's).  A stage is one K-group of 128 bytes: the operands' pieces
-// go straight into LDS with the scales of the rows, in the matrix core's order, into one of two halves of it while the other
-// is multiplied.
-template <int MODE, int NA, int NB, int WA, int WB>
-__global__ __launch_bounds__(64 * WA * WB, 2) void k_fp8_tile(const wq_fp8_product a, const wq_fp8_grid t) {
+// WA x WB waves, each with NA x NB blocks of 16 x 16 (a's rows x b's); KS such teams share a tile's reduction, each a contiguous part of K.
+// A stage is 64 H of K: the operands' pieces go straight into LDS with the scales of the rows, in the order in which lanes read them, into
+// a ring of NST stages per team, NST - 1 of them in flight.
+template <int MODE, int NA, int NB, int WA, int WB, int KS, int H, int NST>
+__global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_product a, const wq_fp8_grid t) {
     constexpr int W = WA * WB, OA = NA * WA, OB = NB * WB;   // blocks of the workgroup tile
-    constexpr bool ROWS = MODE == WQ_FP8_DIRECT_ROWS, SCALED = MODE != WQ_FP8_BF16;
-    constexpr bool EXACT = MODE == WQ_FP8_EXACT || MODE == WQ_FP8_EXACT_FP32, MADD = MODE == WQ_FP8_EXACT_FP32 || MODE == WQ_FP8_DIRECT_FP32;
-    constexpr int QB = SCALED ? (OB + 3) / 4 : 0, QA = ROWS ? (OA + 3) / 4 : 0;   // loads of rows' scales, 64 of one group each
-    constexpr int BOFF = OA * 2048, SBOFF = BOFF + OB * 2048, SAOFF = SBOFF + QB * 256, STAGE = SAOFF + QA * 256;
+    constexpr bool EXACT = MODE == WQ_FP8_EXACT || MODE == WQ_FP8_EXACT_FP32, ROWS = MODE == WQ_FP8_DIRECT_ROWS, VALUES = MODE == WQ_FP8_VALUES;
+    constexpr bool DIRECT = !EXACT && !VALUES, MADD = MODE == WQ_FP8_EXACT_FP32 || MODE == WQ_FP8_DIRECT_FP32;
+    static_assert(H == 2 || (H == 1 && !DIRECT), "the direct product takes a whole group");
+    constexpr int UA = VALUES ? 2 * H : H, UB = UA;   // KiB of a 16-row block in a stage
+    constexpr int QB = VALUES ? 0 : (OB + 3) / 4, QA = ROWS ? (OA + 3) / 4 : VALUES ? 0 : 1;   // loads of scales, 64 of one group each
+    constexpr int BOFF = OA * UA * 1024, SBOFF = BOFF + OB * UB * 1024, SAOFF = SBOFF + QB * 256, STAGE = SAOFF + QA * 256;
     constexpr int RS = 16 * NA + 4, PART = 16 * RS;   // epilogue: floats of a row and of a wave's 16 rows
-    constexpr int BYTES = 2 * STAGE > W * PART * 4 ? 2 * STAGE : W * PART * 4;
-    __shared__ __attribute__((aligned(16))) char lds[BYTES];
+    constexpr int BYTES = NST * STAGE > W * PART * 4 ? NST * STAGE : W * PART * 4;
+    __shared__ __attribute__((aligned(16))) char lds[KS * BYTES];
 
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, q = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wa = wave % WA, wb = wave / WA;
+    const int wave_id = __builtin_amdgcn_readfirstlane(tid >> 6), wave = wave_id % W, team = wave_id / W, wa = wave % WA, wb = wave / WA;
     // workgroup ids go round-robin over the XCDs: each takes a contiguous share of the tile order, in which 8 tiles along b share
     // a's tile before the next follows
     const int logical = (int)(blockIdx.x & 7u) * t.per_xcd + (int)(blockIdx.x >> 3);
@@ -79,7 +85,12 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void k_fp8_tile(const wq_fp8_produ
     const int slice = logical / t.tiles, tile = logical - slice * t.tiles;
     const int band = tile / (8 * t.nA), in_band = tile - band * 8 * t.nA, high = min(8, t.nB - band * 8);
     const int pa = in_band / high, pb = band * 8 + in_band % high;
-    const int s_beg = (int)((long)slice * a.groups / t.slices), s_end = (int)((long)(slice + 1) * a.groups / t.slices);
+    // the team's stages; all teams make the same number of turns
+    const int part = slice * KS + team, parts = t.slices * KS;
+    constexpr int PER = 2 / H;   // stages of a group
+    const int s_beg = (int)((long)part * a.groups / parts) * PER, s_end = (int)((long)(part + 1) * a.groups / parts) * PER,
+              turns = (a.groups + parts - 1) / parts * PER;
+    char *const stages = lds + team * BYTES;
 
     // the first row of a's block j of the tile.  Gated: the first half of a wave's blocks are the gate's, the second the same columns
     // of what it multiplies
@@ -89,44 +100,52 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void k_fp8_tile(const wq_fp8_produ
     };
     const int b0 = pb * OB * 16;
 
-    const __amdgpu_buffer_rsrc_t rA = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.a.codes), 0, (int)a.a.bytes, kBufFlags);
-    const __amdgpu_buffer_rsrc_t rB = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.b.codes), 0, (int)a.b.bytes, kBufFlags);
+    const __amdgpu_buffer_rsrc_t rA = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.a.data), 0, (int)a.a.bytes, kBufFlags);
+    const __amdgpu_buffer_rsrc_t rB = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.b.data), 0, (int)a.b.bytes, kBufFlags);
 
     // ---- the loader ---- (rows past the end read the last one again, whose sums are not stored)
-    constexpr int LA = 2 * OA / W, LB = 2 * OB / W;   // loads of 1 KiB of a wave: half a block each
-    static_assert(LA * W == 2 * OA && LB * W == 2 * OB, "the waves share the loads evenly");
+    constexpr int LA = OA * UA / W, LB = OB * UB / W;   // loads of 1 KiB of a wave: half a group of a block each
+    static_assert(LA * W == OA * UA && LB * W == OB * UB, "the waves share the loads evenly");
     unsigned vA[LA], vB[LB];
-    auto place = [&](const wq_fp8_operand &o, int row, int half) {
+    auto place = [&](const wq_fp8_operand &o, int row, int u) {
         const int r = min(row + l16, o.rows - 1);
-        return (unsigned)(r >> 4) * o.block + (unsigned)(half * 4 + q) * o.piece + (unsigned)(r & 15) * 16u;
+        const unsigned group = VALUES ? (unsigned)(u >> 1) * o.group : 0u;
+        return (unsigned)(r >> 4) * o.block + group + ((unsigned)(u & 1) * 4u + q) * o.piece + (unsigned)(r & 15) * 16u;
     };
 #pragma unroll
-    for (int u = 0; u < LA; ++u) vA[u] = place(a.a, row_of((wave * LA + u) >> 1), (wave * LA + u) & 1);
+    for (int u = 0; u < LA; ++u) vA[u] = place(a.a, row_of((wave * LA + u) / UA), (wave * LA + u) % UA);
 #pragma unroll
-    for (int u = 0; u < LB; ++u) vB[u] = place(a.b, b0 + ((wave * LB + u) >> 1) * 16, (wave * LB + u) & 1);
-    constexpr int LS = (QA + QB + W - 1) / W;   // loads of scales, b's and then a's, are dealt to the waves in turn
+    for (int u = 0; u < LB; ++u) vB[u] = place(a.b, b0 + (wave * LB + u) / UB * 16, (wave * LB + u) % UB);
+    // loads of scales, b's and then a's, are dealt to the waves in turn (a wave without one of its own repeats another's)
+    const unsigned vSA = (unsigned)(min(row_of(min(lane, OA - 1)), a.a.rows - 1) >> 7) * (unsigned)a.a.scale_step * 4u;
+    constexpr int NS = QA + QB, LS = (NS + W - 1) / W, LPS = LA + LB + LS;
     auto issue = [&](int s, int slot) {
-        char *const to = lds + slot * STAGE;
-        const unsigned oA = (unsigned)s * a.a.group, oB = (unsigned)s * a.b.group;
+        char *const to = stages + slot * STAGE;
+        const int g = s / PER;
+        const unsigned half = H == 1 ? (unsigned)(s & 1) * 4u : 0u;   // half a group of codes: pieces of its first or second half
+        const unsigned oA = VALUES ? (unsigned)(s * H) * a.a.group : (unsigned)g * a.a.group + half * a.a.piece;
+        const unsigned oB = VALUES ? (unsigned)(s * H) * a.b.group : (unsigned)g * a.b.group + half * a.b.piece;
 #pragma unroll
         for (int u = 0; u < LA; ++u) lds_load16(rA, to + (wave * LA + u) * 1024, vA[u], oA);
 #pragma unroll
         for (int u = 0; u < LB; ++u) lds_load16(rB, to + BOFF + (wave * LB + u) * 1024, vB[u], oB);
-        if constexpr (SCALED) {
 #pragma unroll
-            for (int u = 0; u < LS; ++u) {
-                const int i = wave + u * W;
-                if (i < QB) {
-                    const __amdgpu_buffer_rsrc_t rS = __builtin_amdgcn_make_buffer_rsrc(
-                        const_cast<float *>(a.b.scales), 0, (int)((unsigned)a.groups * (unsigned)a.b.scale_step * 4u), kBufFlags);
-                    lds_load4(rS, to + SBOFF + i * 256, (unsigned)min(b0 + i * 64 + lane, a.b.rows - 1) * 4u, (unsigned)s * (unsigned)a.b.scale_step * 4u);
-                } else if (i < QB + QA) {
-                    const __amdgpu_buffer_rsrc_t rS = __builtin_amdgcn_make_buffer_rsrc(
-                        const_cast<float *>(a.a.scales), 0, (int)((unsigned)a.groups * (unsigned)a.a.scale_step * 4u), kBufFlags);
-                    const int j = (i - QB) * 4 + q;
-                    lds_load4(rS, to + SAOFF + (i - QB) * 256, (unsigned)min(row_of(min(j, OA - 1)) + l16, a.a.rows - 1) * 4u,
-                              (unsigned)s * (unsigned)a.a.scale_step * 4u);
-                }
+        for (int u = 0; u < LS; ++u) {
+            const int i = (wave + u * W) % (NS ? NS : 1);
+            if (i < QB) {
+                const __amdgpu_buffer_rsrc_t rS = __builtin_amdgcn_make_buffer_rsrc(
+                    const_cast<float *>(a.b.scales), 0, (int)((unsigned)a.groups * (unsigned)a.b.scale_step * 4u), kBufFlags);
+                lds_load4(rS, to + SBOFF + i * 256, (unsigned)min(b0 + i * 64 + lane, a.b.rows - 1) * 4u, (unsigned)g * (unsigned)a.b.scale_step * 4u);
+            } else if constexpr (ROWS) {
+                const __amdgpu_buffer_rsrc_t rS = __builtin_amdgcn_make_buffer_rsrc(
+                    const_cast<float *>(a.a.scales), 0, (int)((unsigned)a.groups * (unsigned)a.a.scale_step * 4u), kBufFlags);
+                const int j = (i - QB) * 4 + q;
+                lds_load4(rS, to + SAOFF + (i - QB) * 256, (unsigned)min(row_of(min(j, OA - 1)) + l16, a.a.rows - 1) * 4u,
+                          (unsigned)g * (unsigned)a.a.scale_step * 4u);
+            } else {   // one for each block (they go through LDS too: a load into a register would wait for those into LDS)
+                const __amdgpu_buffer_rsrc_t rS = __builtin_amdgcn_make_buffer_rsrc(
+                    const_cast<float *>(a.a.scales), 0, (int)((unsigned)((a.a.rows + 127) >> 7) * (unsigned)a.a.scale_step * 4u), kBufFlags);
+                lds_load4(rS, to + SAOFF, vSA, (unsigned)g * 4u);
             }
         }
     };
@@ -137,90 +156,107 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void k_fp8_tile(const wq_fp8_produ
 #pragma unroll
         for (int f = 0; f < NB; ++f) M[e][f] = v4f{0.f, 0.f, 0.f, 0.f};
 
-    // a's scale of one in 128 rows: the wave's blocks in runs that share one (the halves of a gated layer are multiples of 32)
-    constexpr int RUN = NA >= 4 ? 2 : 1, NR = NA / RUN;
-    const float *runs[NR];
-#pragma unroll
-    for (int r = 0; r < NR; ++r)
-        runs[r] = SCALED && !ROWS ? a.a.scales + (long)(min(row_of(wa * NA + r * RUN), a.a.rows - 1) >> 7) * a.a.scale_step : nullptr;
-
-    const char *const atA = lds + wa * NA * 2048 + lane * 16, *const atB = lds + BOFF + wb * NB * 2048 + lane * 16;
-    const char *const atSB = lds + SBOFF + wb * NB * 64 + l16 * 4, *const atSA = lds + SAOFF + wa * NA * 64 + l16 * 4;
-    auto read = [&](const char *p) {
-        const v4i lo = *(const v4i *)p, hi = *(const v4i *)(p + 1024);
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
-    constexpr int NQ = EXACT ? 4 : 2;   // products of 32 bf16 numbers in a group
-    struct Operand {
-        v8i codes;
-        v8bf values[NQ];
-    };
-    auto take = [&](const char *p, float scale, Operand &o) {
-        o.codes = read(p);
-        if constexpr (EXACT) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) o.values[k] = bf16_of_codes(o.codes[2 * k], o.codes[2 * k + 1], scale);
-        } else if constexpr (MODE == WQ_FP8_BF16) {
-            o.values[0] = __builtin_bit_cast(v8bf, __builtin_shufflevector(o.codes, o.codes, 0, 1, 2, 3));
-            o.values[1] = __builtin_bit_cast(v8bf, __builtin_shufflevector(o.codes, o.codes, 4, 5, 6, 7));
-        }
-    };
+    const char *const atA = stages + wa * NA * UA * 1024 + lane * 16, *const atB = stages + BOFF + wb * NB * UB * 1024 + lane * 16;
+    const char *const atSB = stages + SBOFF + wb * NB * 64 + l16 * 4, *const atSA = stages + SAOFF + (ROWS ? wa * NA * 64 + l16 * 4 : wa * NA * 4);
     auto compute = [&](int s, int slot) {
-        Operand bv[NB];
-        float sb[NB], sa[NR];
-        if constexpr (SCALED && !ROWS) {
+        const char *const pA = atA + slot * STAGE, *const pB = atB + slot * STAGE;
+        float sa[NA];
+        if constexpr (!VALUES) {
 #pragma unroll
-            for (int r = 0; r < NR; ++r) sa[r] = runs[r][s];
+            for (int e = 0; e < NA; ++e) sa[e] = *(const float *)(atSA + slot * STAGE + e * (ROWS ? 64 : 4));
         }
-#pragma unroll
-        for (int f = 0; f < NB; ++f) {
-            sb[f] = SCALED ? *(const float *)(atSB + slot * STAGE + f * 64) : 1.0f;
-            take(atB + slot * STAGE + f * 2048, sb[f], bv[f]);
-        }
-#pragma unroll
-        for (int e = 0; e < NA; ++e) {
-            Operand av;
-            const float scale = ROWS ? *(const float *)(atSA + slot * STAGE + e * 64) : SCALED && !MADD ? sa[e / RUN] : 1.0f;
-            take(atA + slot * STAGE + e * 2048, scale, av);
-            v4f P[NB];
-#pragma unroll
-            for (int f = 0; f < NB; ++f) P[f] = MADD ? v4f{0.f, 0.f, 0.f, 0.f} : M[e][f];
-            if constexpr (EXACT || MODE == WQ_FP8_BF16) {
-#pragma unroll
-                for (int k = 0; k < NQ; ++k)
-#pragma unroll
-                    for (int f = 0; f < NB; ++f) P[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av.values[k], bv[f].values[k], P[f], 0, 0, 0);
-            } else {   // an e8m0 scale is a power of two's exponent field
-#pragma unroll
-                for (int f = 0; f < NB; ++f)
-                    P[f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av.codes, bv[f].codes, P[f], 0, 0, 0, __float_as_int(scale) >> 23, 0,
-                                                                            __float_as_int(sb[f]) >> 23);
-            }
+        if constexpr (DIRECT) {
+            auto read = [&](const char *p) {
+                const v4i lo = *(const v4i *)p, hi = *(const v4i *)(p + 1024);
+                return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            };
+            v8i bv[NB];
+            int sb[NB];
 #pragma unroll
             for (int f = 0; f < NB; ++f) {
-                if constexpr (MADD) {
+                bv[f] = read(pB + f * 2048);
+                sb[f] = *(const int *)(atSB + slot * STAGE + f * 64) >> 23;   // a power of two's exponent field: an e8m0 scale
+            }
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) M[e][f][r] = __builtin_fmaf(P[f][r], sa[e / RUN], M[e][f][r]);
+            for (int e = 0; e < NA; ++e) {
+                const v8i av = read(pA + e * 2048);
+                const int ea = MADD ? 127 : __float_as_int(sa[e]) >> 23;
+#pragma unroll
+                for (int f = 0; f < NB; ++f) {
+                    const v4f P = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv[f], MADD ? v4f{0.f, 0.f, 0.f, 0.f} : M[e][f], 0, 0, 0, ea, 0, sb[f]);
+                    if constexpr (MADD) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) M[e][f][r] = __builtin_fmaf(P[r], sa[e], M[e][f][r]);
+                    } else {
+                        M[e][f] = P;
+                    }
+                }
+            }
+        } else {
+            float sb[NB];
+            if constexpr (EXACT) {
+#pragma unroll
+                for (int f = 0; f < NB; ++f) sb[f] = *(const float *)(atSB + slot * STAGE + f * 64);
+            }
+            auto read = [&](const char *p, float scale, v8bf (&v)[2]) {   // 64 of K: two products of 32
+                if constexpr (VALUES) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) v[k] = *(const v8bf *)(p + k * 1024);
                 } else {
-                    M[e][f] = P[f];
+                    const v4i c = *(const v4i *)p;
+                    v[0] = bf16_of_codes(c.x, c.y, scale);
+                    v[1] = bf16_of_codes(c.z, c.w, scale);
+                }
+            };
+            constexpr int STEP = UA / H * 1024, NK = 2 * H;
+            v8bf bv[NB][H][2];
+#pragma unroll
+            for (int f = 0; f < NB; ++f)
+#pragma unroll
+                for (int h = 0; h < H; ++h) read(pB + (f * H + h) * STEP, sb[f], bv[f][h]);
+#pragma unroll
+            for (int e = 0; e < NA; ++e) {
+                v8bf av[H][2];
+#pragma unroll
+                for (int h = 0; h < H; ++h) read(pA + (e * H + h) * STEP, MADD || VALUES ? 1.0f : sa[e], av[h]);
+                v4f P[NB];
+#pragma unroll
+                for (int f = 0; f < NB; ++f) P[f] = MADD ? v4f{0.f, 0.f, 0.f, 0.f} : M[e][f];
+#pragma unroll
+                for (int k = 0; k < NK; ++k)
+#pragma unroll
+                    for (int f = 0; f < NB; ++f) P[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[k / 2][k % 2], bv[f][k / 2][k % 2], P[f], 0, 0, 0);
+#pragma unroll
+                for (int f = 0; f < NB; ++f) {
+                    if constexpr (MADD) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) M[e][f][r] = __builtin_fmaf(P[f][r], sa[e], M[e][f][r]);
+                    } else {
+                        M[e][f] = P[f];
+                    }
                 }
             }
         }
     };
 
-    if (s_beg < s_end) issue(s_beg, 0);
-    for (int s = s_beg; s < s_end; s += 2) {
 #pragma unroll
-        for (int slot = 0; slot < 2; ++slot) {   // (a constant: so are the addresses in LDS)
-            if (s + slot >= s_end) break;
-            wait_and_barrier();   // the stage has landed, every wave's loads, and the other half has been read by all
-            if (s + slot + 1 < s_end) issue(s + slot + 1, slot ^ 1);
-            compute(s + slot, slot);
+    for (int d = 0; d < NST - 1; ++d)
+        if (s_beg + d < s_end) issue(s_beg + d, d);
+    for (int i = 0; i < turns; i += NST) {
+#pragma unroll
+        for (int slot = 0; slot < NST; ++slot) {   // (a constant: so are the addresses in LDS)
+            if (i + slot >= turns) break;
+            const int s = s_beg + i + slot;
+            // the stage's loads have landed, every wave's, and the slot of the stage before has been read by all
+            if (NST > 2 && s + NST - 1 <= s_end) wait_and_barrier<(NST - 2) * LPS>();
+            else wait_and_barrier<0>();
+            if (s + NST - 1 < s_end) issue(s + NST - 1, (slot + NST - 1) % NST);
+            if (s < s_end) compute(s, slot);
         }
     }
 
     // ---- epilogue ---- through LDS, 16 rows of a wave at a time: its lanes then hold whole runs of columns of a row
-    float *mine = (float *)lds + wave * PART;
+    float *mine = (float *)stages + wave * PART;
     wq_fp8_product out = a;
     if (t.slices > 1) {   // a slice's sums as they are
         out.y = t.partial + (long)slice * a.rows * a.cols;
@@ -238,18 +274,25 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void k_fp8_tile(const wq_fp8_produ
     __syncthreads();   // the last stage has been read by all
 #pragma unroll
     for (int f = 0; f < NB; ++f) {
+        if (KS > 1 && f) __syncthreads();   // the rows before have been read by all teams
 #pragma unroll
         for (int e = 0; e < NA; ++e) *(v4f *)&mine[l16 * RS + 16 * e + 4 * q] = M[e][f];
-        __builtin_amdgcn_wave_barrier();
+        if (KS > 1) __syncthreads();
+        else __builtin_amdgcn_wave_barrier();
         if (o < a.outs) {
 #pragma unroll 1
-            for (int row = lane >> shift; row < 16; row += row_step) {
+            for (int row = (team * 64 + lane) >> shift; row < 16; row += row_step * KS) {   // (the teams share the rows)
                 const int p = b0 + (wb * NB + f) * 16 + row;
                 if (p >= a.rows) break;
                 const v4f res[1] = {fp8_residual(out, p, o)};
-                const v4f z[1] = {bias + *(const v4f *)(mine + row * RS + c)};
-                v4f up[1] = {};
-                if (a.gated) up[0] = bias_up + *(const v4f *)(mine + row * RS + 8 * NA + c);
+                const float *sums = (const float *)lds + wave * PART + row * RS + c;
+                v4f z[1] = {bias + *(const v4f *)sums}, up[1] = {};
+                if (a.gated) up[0] = bias_up + *(const v4f *)(sums + 8 * NA);
+#pragma unroll
+                for (int k = 1; k < KS; ++k) {
+                    z[0] += *(const v4f *)(sums + k * (BYTES / 4));
+                    if (a.gated) up[0] += *(const v4f *)(sums + k * (BYTES / 4) + 8 * NA);
+                }
                 fp8_finish<1>(out, p, 0, o, z, up, res);
             }
         }
@@ -257,7 +300,7 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void k_fp8_tile(const wq_fp8_produ
     }
 }
 
-template <int MODE, int NA, int NB, int WA, int WB>
+template <int MODE, int NA, int NB, int WA, int WB, int KS, int H, int NST>
 hipError_t launch_fp8_tile(const wq_fp8_product &a, int slices, float *partial, hipStream_t s) {
     wq_fp8_grid t;
     const int across = a.gated ? 8 * NA * WA : 16 * NA * WA;   // columns of y in a tile
@@ -268,13 +311,21 @@ hipError_t launch_fp8_tile(const wq_fp8_product &a, int slices, float *partial, 
     t.per_xcd = (t.total + 7) / 8;
     t.partial = partial;
     t.slices = slices;
-    hipLaunchKernelGGL((k_fp8_tile<MODE, NA, NB, WA, WB>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * WA * WB), 0, s, a, t);
+    hipLaunchKernelGGL((k_fp8_tile<MODE, NA, NB, WA, WB, KS, H, NST>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * WA * WB * KS), 0, s, a, t);
     return hipGetLastError();
 }
 
 template <int MODE>
 hipError_t launch_fp8_form(const wq_fp8_product &a, int form, int slices, float *partial, hipStream_t s) {
-    return launch_fp8_tile<MODE, 4, 4, 2, 2>(a, slices, partial, s);
+    constexpr int H = MODE == WQ_FP8_VALUES ? 1 : 2;
+    switch (form) {
+        case WQ_FP8_TILE_256: return launch_fp8_tile<MODE, 8, 4, 2, 4, 1, H, 2>(a, slices, partial, s);
+        case WQ_FP8_TILE_128: return launch_fp8_tile<MODE, 4, 4, 2, 2, 1, H, 2>(a, slices, partial, s);
+        case WQ_FP8_TILE_128x64: return launch_fp8_tile<MODE, 4, 2, 2, 2, 1, H, 2>(a, slices, partial, s);
+        case WQ_FP8_TILE_64: return launch_fp8_tile<MODE, 2, 2, 2, 2, 1, H, 2>(a, slices, partial, s);
+        case WQ_FP8_TILE_64_2: return launch_fp8_tile<MODE, 2, 2, 2, 2, 2, H, 2>(a, slices, partial, s);
+        default: return launch_fp8_tile<MODE, 2, 2, 2, 2, 4, H, 2>(a, slices, partial, s);
+    }
 }
 
 }  // namespace

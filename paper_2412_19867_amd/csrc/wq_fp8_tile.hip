@@ -8,6 +8,6 @@ hipError_t wq_launch_fp8_tile(const wq_fp8_product &p, int mode, int form, int s
         case WQ_FP8_DIRECT: return launch_fp8_form<WQ_FP8_DIRECT>(p, form, slices, partial, s);
         case WQ_FP8_DIRECT_FP32: return launch_fp8_form<WQ_FP8_DIRECT_FP32>(p, form, slices, partial, s);
         case WQ_FP8_DIRECT_ROWS: return launch_fp8_form<WQ_FP8_DIRECT_ROWS>(p, form, slices, partial, s);
-        default: return launch_fp8_form<WQ_FP8_BF16>(p, form, slices, partial, s);
+        default: return launch_fp8_form<WQ_FP8_VALUES>(p, form, slices, partial, s);
     }
 }

@@ -2,6 +2,7 @@
 // scale for each 128 columns; and its gradient.
 #include <float.h>
 
+#include "wq_column_sums.h"
 #include "wq_fp8_args.h"
 #include "wq_layer_norm.h"
 #include "wq_layer_norm_args.h"
@@ -170,20 +171,33 @@ void launch_norm(const wq_layer_norm_args &a, hipStream_t s) {
 // A workgroup's units of `wpr` waves take every units-th row; the weight's and bias's gradients of a unit's rows add up in its lanes'
 // registers and leave as one row of partial sums.
 template <int TYPE, int V>
-__global__ __launch_bounds__(512) void k_layer_norm_grad(const wq_layer_norm_grad_args a, int wpr, int units) {
+__global__ __launch_bounds__(512, V <= 2 ? 4 : 2) void k_layer_norm_grad(const wq_layer_norm_grad_args a, int wpr, int units) {
     using T = typename Elem<TYPE>::type;
     __shared__ double part[2][8][4];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int upw = (int)(blockDim.x >> 6) / wpr;
     const int unit = (int)blockIdx.x * upw + w / wpr;
     const int c0 = (w % wpr) * 512 + lane * 8, step = 512 * wpr;
-    float gm[V][8], dgamma[V][8], dbeta[V][8];
+    float dgamma[V][8], dbeta[V][8], kept[8];
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
+    for (int k = 0; k < V; ++k)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) gm[k][j] = 1.0f, dgamma[k][j] = 0.0f, dbeta[k][j] = 0.0f;
-        if (a.gamma) load8_some<float>(a.gamma + c0 + k * step, a.C - c0 - k * step, gm[k]);
-    }
+        for (int j = 0; j < 8; ++j) dgamma[k][j] = 0.0f, dbeta[k][j] = 0.0f;
+    // gamma of more pieces than one is loaded where it is used, from the caches: there are no registers for it
+    auto load_gamma = [&](int k, float (&gm)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) gm[j] = 1.0f;
+        if (a.gamma) load8_some<float>(a.gamma + c0 + k * step, a.C - c0 - k * step, gm);
+    };
+    load_gamma(0, kept);
+    auto gamma_of = [&](int k, float (&gm)[8]) {
+        if constexpr (V > 1) {
+            load_gamma(k, gm);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) gm[j] = kept[j];
+        }
+    };
     // (every unit of the workgroup makes the same number of turns: the barriers meet)
     const int turns = (a.rows + units - 1) / units;
     for (int i = 0; i < turns; ++i) {
@@ -199,16 +213,19 @@ __global__ __launch_bounds__(512) void k_layer_norm_grad(const wq_layer_norm_gra
         const double origin = (double)(float)h[0];
         double sums[4] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
-        for (int k = 0; k < V; ++k)
+        for (int k = 0; k < V; ++k) {
+            float gm[8];
+            gamma_of(k, gm);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 if (c0 + k * step + j >= a.C) continue;
-                const double d = (double)hv[k][j] - origin, g = (double)(dv[k][j] * gm[k][j]);
+                const double d = (double)hv[k][j] - origin, g = (double)(dv[k][j] * gm[j]);
                 sums[0] += d;
                 sums[1] = __builtin_fma(d, d, sums[1]);
                 sums[2] += g;
                 sums[3] = __builtin_fma(g, d, sums[3]);
             }
+        }
         wave_sums(sums);
         if (wpr > 1) {   // (two sets of sums in turn: one barrier a row)
             double(*mine)[4] = part[i & 1];
@@ -227,12 +244,18 @@ __global__ __launch_bounds__(512) void k_layer_norm_grad(const wq_layer_norm_gra
         const norm_stats st = stats_of(sums[0], sums[1], a.C, a.eps);
         const double mean = origin + st.mean;
         const float r = (float)st.r;
+        // (as if loaded anew: what the sums converted to 64 bits would be kept, in more registers than two workgroups a CU have)
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) asm("" : "+v"(hv[k][j]), "+v"(dv[k][j]));
         // mean of g, and of g n = g (d - mean d) r
         const float mg = (float)(sums[2] / a.C), mgn = (float)((sums[3] - st.mean * sums[2]) * st.r / a.C);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             const int c = c0 + k * step, n = a.C - c;
-            float dx[8];
+            float dx[8], gm[8];
+            gamma_of(k, gm);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float nn = (float)((double)hv[k][j] - mean) * r;
@@ -240,7 +263,7 @@ __global__ __launch_bounds__(512) void k_layer_norm_grad(const wq_layer_norm_gra
                     dgamma[k][j] = __builtin_fmaf(dv[k][j], nn, dgamma[k][j]);
                     dbeta[k][j] += dv[k][j];
                 }
-                dx[j] = r * (dv[k][j] * gm[k][j] - mg - nn * mgn);
+                dx[j] = r * (dv[k][j] * gm[j] - mg - nn * mgn);
             }
             if (!a.dx || !live || n <= 0) continue;
             if (a.res) {
@@ -263,18 +286,11 @@ __global__ __launch_bounds__(512) void k_layer_norm_grad(const wq_layer_norm_gra
     }
 }
 
-// dgamma and dbeta of partial rows [units][2][C]: a workgroup takes 64 columns, its four waves a quarter of the rows each.
-__global__ __launch_bounds__(256) void k_layer_norm_columns(const wq_layer_norm_grad_args a, int units) {
-    __shared__ double part[4][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const long c = (long)blockIdx.x * 64 + lane, n = 2L * a.C;
-    double s = 0.0;
-    if (c < n)
-        for (int u = w; u < units; u += 4) s += (double)a.part[(size_t)u * n + c];
-    part[w][lane] = s;
-    __syncthreads();
-    if (w || c >= n) return;
-    s = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+// dgamma and dbeta of partial rows [units][2][C].
+__global__ __launch_bounds__(1024) void k_layer_norm_columns(const wq_layer_norm_grad_args a, int units) {
+    const long c = (long)blockIdx.x * 64 + (threadIdx.x & 63), n = 2L * a.C;
+    const double s = column_sum(a.part, units, n, c, c < n);
+    if (threadIdx.x >= 64 || c >= n) return;
     float *out = c < a.C ? a.dgamma : a.dbeta;
     const long i = c < a.C ? c : c - a.C;
     if (out) out[i] = (float)(a.accumulate ? (double)out[i] + s : s);
@@ -361,7 +377,7 @@ grad_form choose_grad_form(int rows, int C) {
     while (f.wpr < chunks && f.wpr < 8) f.wpr *= 2;
     while (f.V * f.wpr < chunks) f.V *= 2;
     f.waves = f.wpr < 4 ? 4 : f.wpr;
-    const int upw = f.waves / f.wpr, most = 512 * 4 / f.waves;
+    const int upw = f.waves / f.wpr, most = (f.V <= 2 ? 1024 : 512) * 4 / f.waves;
     f.blocks = (rows + upw - 1) / upw < most ? (rows + upw - 1) / upw : most;
     f.units = f.blocks * upw;
     return f;
@@ -376,7 +392,7 @@ void launch_grad(const wq_layer_norm_grad_args &a, const grad_form &f, hipStream
             first.dx = nullptr;
             hipLaunchKernelGGL((k_layer_norm_grad_long<TYPE>), dim3((unsigned)a.rows), dim3(256), 0, s, first);
             hipLaunchKernelGGL((k_layer_norm_columns_long<TYPE>), dim3((unsigned)((a.C + 63) / 64), (unsigned)f.units), dim3(256), 0, s, a, f.units);
-            hipLaunchKernelGGL(k_layer_norm_columns, dim3(columns), dim3(256), 0, s, a, f.units);
+            hipLaunchKernelGGL(k_layer_norm_columns, dim3(columns), dim3(1024), 0, s, a, f.units);
         }
         if (a.dx) {
             wq_layer_norm_grad_args last = a;
@@ -389,7 +405,7 @@ void launch_grad(const wq_layer_norm_grad_args &a, const grad_form &f, hipStream
     if (f.V == 1) hipLaunchKernelGGL((k_layer_norm_grad<TYPE, 1>), grid, block, 0, s, a, f.wpr, f.units);
     else if (f.V == 2) hipLaunchKernelGGL((k_layer_norm_grad<TYPE, 2>), grid, block, 0, s, a, f.wpr, f.units);
     else hipLaunchKernelGGL((k_layer_norm_grad<TYPE, 4>), grid, block, 0, s, a, f.wpr, f.units);
-    if (a.part) hipLaunchKernelGGL(k_layer_norm_columns, dim3(columns), dim3(256), 0, s, a, f.units);
+    if (a.part) hipLaunchKernelGGL(k_layer_norm_columns, dim3(columns), dim3(1024), 0, s, a, f.units);
 }
 
 bool good_type(int type) { return type == WQ_FP32 || type == WQ_BF16 || type == WQ_FP16; }
