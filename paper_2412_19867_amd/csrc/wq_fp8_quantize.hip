@@ -60,9 +60,16 @@ __global__ __launch_bounds__(256) void k_fp8_quantize(const wq_fp8_rows_args a) 
 }
 
 // ------------------------------------------------------------ along the rows, and the gradient through the epilogue
-// Slope and value of the activation at N values (act'(z), act(z)), in fp32.
+// Slope and value of the activation at N values (act'(z), act(z)), in fp32.  An infinite z has the limits' slope: products with what
+// vanishes there take a z of at most 2^60 in size.
 template <int N>
 __device__ __forceinline__ void activation_slope(const float (&z)[N], int act, float (&slope)[N], float (&value)[N]) {
+    float b[N], v[N];   // (the minimum and maximum that keep a NaN)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        v[i] = __builtin_elementwise_maximum(z[i], -0x1p60f);
+        b[i] = __builtin_elementwise_minimum(v[i], 0x1p60f);
+    }
     switch (act) {
         case WQ_ACT_RELU:
 #pragma unroll
@@ -74,26 +81,27 @@ __device__ __forceinline__ void activation_slope(const float (&z)[N], int act, f
         case WQ_ACT_SILU:   // s (1 + z (1 - s)), s = 1 / (1 + e^-z)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float s = logistic(z[i] * -1.44269504f), c = logistic(z[i] * 1.44269504f);
-                value[i] = z[i] * s;
-                slope[i] = __builtin_fmaf(value[i], c, s);
+                const float s = logistic(b[i] * -1.44269504f), c = logistic(b[i] * 1.44269504f);
+                value[i] = v[i] * s;
+                slope[i] = __builtin_fmaf(b[i] * s, c, s);
             }
             break;
         case WQ_ACT_GELU:   // Phi(z) + z phi(z)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float cdf = 0.5f * erfcf(z[i] * -0.707106781f), pdf = 0.398942280f * __expf(-0.5f * z[i] * z[i]);
-                value[i] = z[i] * cdf;
-                slope[i] = __builtin_fmaf(z[i], pdf, cdf);
+                const float x = fabsf(b[i]), e = __builtin_amdgcn_exp2f(x * x * -0.721347520f), tail = e * gelu_tail(x);
+                const float cdf = b[i] < 0.0f ? tail : 1.0f - tail;
+                value[i] = v[i] * cdf;
+                slope[i] = __builtin_fmaf(b[i], 0.398942280f * e, cdf);
             }
             break;
         case WQ_ACT_GELU_TANH:   // s + z s (1 - s) 2 u', s = 1 / (1 + e^-2u), u = sqrt(2 / pi) (z + 0.044715 z^3)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float z2 = z[i] * z[i], e2 = z[i] * __builtin_fmaf(-0.102943240f, z2, -2.30220820f);
+                const float z2 = b[i] * b[i], e2 = b[i] * __builtin_fmaf(-0.102943240f, z2, -2.30220820f);
                 const float s = logistic(e2), c = logistic(-e2);
-                value[i] = z[i] * s;
-                slope[i] = __builtin_fmaf(value[i] * c, __builtin_fmaf(0.214064488f, z2, 1.59576912f), s);
+                value[i] = v[i] * s;
+                slope[i] = __builtin_fmaf(b[i] * s * c, __builtin_fmaf(0.214064488f, z2, 1.59576912f), s);
             }
             break;
         default:
@@ -117,7 +125,13 @@ __global__ __launch_bounds__(256, ALONG == 0 ? 4 : 3) void k_fp8_both(const wq_f
     __shared__ uint32_t top_s[4][128];
     __shared__ float sum_s[4][128];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, octet = lane & 15, sub = tid >> 4;
-    const int g = id % a.groups, tb = id / a.groups;
+    int g = id % a.groups;
+    const int tb = id / a.groups;
+    if (a.gated) {   // the gate's columns and those that it multiplies read the same: they go to one XCD, eight workgroups apart
+        const int pairs = a.groups / 2 / 8 * 8;
+        if (g < 2 * pairs) g = (g >> 4) * 8 + (g & 7) + ((g & 8) ? a.groups / 2 : 0);
+        else g -= g < 2 * pairs + (a.groups / 2 - pairs) ? pairs : 0;
+    }
     const int c = g * kGroup + octet * 8, p0 = tb * kGroup + sub * 8;
     const int outs = a.gated ? a.cols / 2 : a.cols;
     const bool up = a.gated && c >= outs;   // (outs is a multiple of 32: all eight columns are of one half)

@@ -32,12 +32,12 @@ __device__ __forceinline__ float logistic(float e2) { return __builtin_amdgcn_rc
 
 // The division, exponential and error function of the math library, correctly rounded or nearly, take 40 (silu) to 100 (gelu)
 // instructions a value in place of 5 to 20: an eighth of the vector instructions of the product 4096 x 4096 -> 2 x 8192, g 128.
-__device__ __forceinline__ float gelu(float z) {
-    // z Phi(z) = max(z, 0) - |z| e^(-z^2 / 2) G(|z|), G(x) = e^(x^2 / 2) erfc(x / sqrt 2) / 2 as a polynomial in
-    // t = 1 / (1 + x / 4) that is 1/2 at x = 0: a fit by reweighted least squares of its relative error, 7e-8 up to x = 6, 8e-7 at 10.
-    // The negative tail keeps its digits so (a fit of one degree less, to the error of gelu itself, was 5e-7 off near 0 and 2e-5 at -5;
-    // 2048x640->5120 g 64 W8 bf16 29.8 us with it, 30.5 so).
-    const float x = fabsf(z), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.25f, x, 1.0f));
+// G(x) = e^(x^2 / 2) erfc(x / sqrt 2) / 2 at x >= 0, so that Phi(-x) = e^(-x^2 / 2) G(x)
+__device__ __forceinline__ float gelu_tail(float x) {
+    // a polynomial in t = 1 / (1 + x / 4) that is 1/2 at x = 0: a fit by reweighted least squares of its relative error, 7e-8 up to x = 6,
+    // 8e-7 at 10.  The negative tail keeps its digits so (a fit of one degree less, to the error of gelu itself, was 5e-7 off near 0 and
+    // 2e-5 at -5; 2048x640->5120 g 64 W8 bf16 29.8 us with it, 30.5 so).
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.25f, x, 1.0f));
     float G = -0.0996275544f;
     G = __builtin_fmaf(G, t, 0.380040318f);
     G = __builtin_fmaf(G, t, -0.343892276f);
@@ -45,7 +45,11 @@ __device__ __forceinline__ float gelu(float z) {
     G = __builtin_fmaf(G, t, -0.0272250343f);
     G = __builtin_fmaf(G, t, 0.131000191f);
     G = __builtin_fmaf(G, t, 0.0952150896f);
-    G = __builtin_fmaf(G, t, 0.000279937405f);
+    return __builtin_fmaf(G, t, 0.000279937405f);
+}
+__device__ __forceinline__ float gelu(float z) {
+    // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
+    const float x = fabsf(z), G = gelu_tail(x);
     // (bounded from above: infinity times 0 would be NaN)
     const float b = fabsf(__builtin_elementwise_minimum(z, 0x1p60f));
     return __builtin_fmaf(-b, __builtin_amdgcn_exp2f(x * x * -0.721347520f) * G, fmaxf(z, 0.0f));

@@ -573,3 +573,33 @@ def test_binding_refusals(wq):
         plan.backward(x, y, blob, ws, dx=x, activation="silu")   # without the values before the activation
     with pytest.raises(wq.WqError):
         plan.backward(x, y, None, ws, dx=x)
+
+
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu", "gelu_tanh"])
+def test_slopes_by_place(wq, act):
+    """The bias's gradient of one row is dz itself: slopes and values over the whole range, at infinities and NaN."""
+    z = np.concatenate([np.linspace(-14, 14, 3001), [-300.0, -40.0, 0.0, -0.0, 300.0, 6e4, np.inf, -np.inf, np.nan] * 8, np.zeros(63)])
+    z = z[:len(z) // 64 * 64].astype(np.float32)
+    n = len(z)
+    lim = np.where(np.isinf(z), np.sign(z) * 1e4, z).astype(np.float64)
+    slope, value = fb.slope(lim, act), fb.activation(lim, act)
+    plan = wq.Fp8LinearPlan(1, 8, n, backward=True)
+    ws = plan.alloc_workspace()
+    db = torch.empty(n, device="cuda")
+    plan.backward(None, torch.ones((1, n), device="cuda"), None, ws, db=db, preactivation=torch.from_numpy(z).cuda()[None], activation=act)
+    nan = np.isnan(z)
+    got = f64(db)
+    # s and 1 - s, or the tail and the density, are each off by a few units relative to themselves and are added after a product with z
+    tol = 16 * U * (1 + np.abs(lim) * (np.abs(lim) < 20))
+    assert (np.abs(got - slope)[~nan] <= tol[~nan]).all() and np.isnan(got[nan]).all()
+    # gated: the second half's gradient is the value of the first
+    plan = wq.Fp8LinearPlan(1, 8, 2 * n, backward=True)
+    ws = plan.alloc_workspace()
+    db = torch.empty(2 * n, device="cuda")
+    pre = torch.cat([torch.from_numpy(z), torch.full((n,), 0.5)])[None].cuda()
+    plan.backward(None, torch.ones((1, n), device="cuda"), None, ws, db=db, preactivation=pre, activation=act, gated=True)
+    got = f64(db)
+    assert (np.abs(got[:n] - 0.5 * slope)[~nan] <= tol[~nan]).all()
+    fine = np.isfinite(z)
+    assert (np.abs(got[n:] - value)[fine] <= 16 * U * (np.abs(value) + 1)[fine]).all()
+    assert (got[n:][z == np.inf] == np.inf).all() and not got[n:][z == -np.inf].any() and np.isnan(got[n:][nan]).all()
