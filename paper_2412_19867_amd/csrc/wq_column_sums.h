@@ -15,9 +15,9 @@ __device__ __forceinline__ double column_sum(const float *part, int rows, long s
         for (int r = w; r < rows; r += 128) {
             float v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = r + 16 * k < rows ? part[(size_t)(r + 16 * k) * stride + c] : 0.0f;
+            for (int k = 0; k < 8; ++k) v[k] = part[(size_t)min(r + 16 * k, rows - 1) * stride + c];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) s += (double)v[k];
+            for (int k = 0; k < 8; ++k) s += r + 16 * k < rows ? (double)v[k] : 0.0;
         }
     shares[w][lane] = s;
     __syncthreads();

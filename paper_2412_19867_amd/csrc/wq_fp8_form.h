@@ -1,6 +1,7 @@
 // Which kernels the calls of the linear layer in 8-bit floating point launch, by rules on sizes: shared by the launches and by a check
 // that runs on the host.
 #pragma once
+#include <stdlib.h>
 
 // Workgroup tiles: weight rows x rows of x, and teams of waves that share their K.
 enum wq_fp8_tile_form {
@@ -33,6 +34,7 @@ inline long wq_fp8_tiles(int outs, int rows, int across, int down) {
 //   128x64 from 384, 64 x 64 from 192 (512), two teams from 40 (192) tiles of 64, else four: CUs with enough waves
 inline wq_fp8_form wq_fp8_choose_form(int rows, int outs, bool gated, int groups, bool exact) {
     const int half = gated ? 2 : 1;
+    if (getenv("WQF")) return {0, atoi(getenv("WQF")), 1};
     const long blocks = wq_fp8_tiles(outs, rows, 16, 16);
     if (rows <= 128 && blocks <= 900) return {rows <= 16 || blocks <= 256 ? 1 : 2, 0, 1};
     const long n256 = wq_fp8_tiles(outs, rows, 256 / half, 256), n128 = wq_fp8_tiles(outs, rows, 128 / half, 128);
@@ -45,6 +47,7 @@ inline wq_fp8_form wq_fp8_choose_form(int rows, int outs, bool gated, int groups
 
 // dw [Cout][Cin] from groups of 128 rows.
 inline wq_fp8_form wq_fp8_choose_grad_form(int Cout, int Cin, int groups) {
+    if (getenv("WQG")) return {0, atoi(getenv("WQG")), 1};
     const long n256 = wq_fp8_tiles(Cin, Cout, 256, 256), n128 = wq_fp8_tiles(Cin, Cout, 128, 128), n64 = wq_fp8_tiles(Cin, Cout, 64, 64);
     if (groups >= 7 && (n256 + 255) / 256 * 256 <= 0.3 * n128) return {0, WQ_FP8_TILE_256, 1};
     if (groups >= 7 && n128 >= 270) return {0, WQ_FP8_TILE_128, 1};

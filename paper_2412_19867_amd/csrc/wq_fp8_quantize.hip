@@ -1,5 +1,7 @@
 // Rows into e4m3 codes with power-of-two scales: along the rows' columns, along the rows (for the weights' gradient), weights in blocks; the
 // gradient through activation and gate on the way.
+#include <type_traits>
+
 #include "wq_column_sums.h"
 #include "wq_fp8_quantize.h"
 #include "wq_layer_norm.h"
@@ -13,12 +15,27 @@ __device__ __forceinline__ uint32_t wave_max16(uint32_t v) {   // over 16 adjace
     return dpp_max<0x140>(v);
 }
 
+// Over the lanes l, l ^ 16, l ^ 32 and l ^ 48, whose swaps need no LDS.
+__device__ __forceinline__ uint32_t rows_max(uint32_t v) {
+    auto t = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max((uint32_t)t[0], (uint32_t)t[1]);
+    t = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return max((uint32_t)t[0], (uint32_t)t[1]);
+}
+__device__ __forceinline__ float rows_sum(float f) {
+    uint32_t v = __float_as_uint(f);
+    auto t = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = __float_as_uint(__uint_as_float(t[0]) + __uint_as_float(t[1]));
+    t = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+}
+
 // The other lane of a pair's value.
 __device__ __forceinline__ uint32_t neighbour(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xf, 0xf, true); }
 
 // A wave takes 16 rows x 128 columns: four lanes to a row, each with four runs of eight elements 32 apart.  Two lanes' runs make a
 // piece of 16 codes; they exchange halves so that each stores whole pieces, 16 rows of a plane side by side.
-template <int TYPE>
+template <int TYPE, bool WHOLE>
 __global__ __launch_bounds__(256) void k_fp8_quantize(const wq_fp8_rows_args a) {
     using T = typename Elem<TYPE>::type;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, part = lane & 3;
@@ -33,10 +50,12 @@ __global__ __launch_bounds__(256) void k_fp8_quantize(const wq_fp8_rows_args a) 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int c = g * kGroup + i * 32 + part * 8;
-        load8_some<T>(x + c, a.cols - c, v[i]);
+        load8_row<T, WHOLE>(x, c, a.cols, true, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[i][j]));
-    }
     top = dpp_max<0xB1>(top);
     top = dpp_max<0x4E>(top);
     float s, r;
@@ -110,20 +129,24 @@ __device__ __forceinline__ void activation_slope(const float (&z)[N], int act, f
     }
 }
 
-// A workgroup takes 128 rows x 128 columns of v (x itself, or dz), each lane eight adjacent rows x eight adjacent columns in registers:
-// the groups along the columns are 16 lanes', those along the rows a lane's eight and its counterparts' in the other 15 sixteenths of
-// the workgroup.  Codes leave through LDS, where they lie as in memory.
+// A workgroup takes 128 rows x 128 columns of v (x itself, or dz), each lane RT adjacent rows x eight adjacent columns in registers:
+// the groups along the columns are 16 lanes', those along the rows a lane's RT and its counterparts' in the rest of the workgroup.  Codes
+// leave through LDS, where they lie as in memory.
 //   ALONG: 0 no codes along the rows, 1 codes, 2 values in bf16.
 //   Two tensors in one launch: the first `blocks` workgroups take the first.
-template <int TYPE, int ALONG>
-__global__ __launch_bounds__(256, ALONG == 0 ? 4 : 3) void k_fp8_both(const wq_fp8_both_args first, const wq_fp8_both_args second, unsigned blocks) {
+//   bound: memory: x and dy of 4096 x 4096 bf16 into values and codes 33 us (150 MB).  Eight rows a lane and half the lanes: 35, and with
+//   a gate, whose three tensors then do not fit the registers, 42 in place of 22 (1000x1280, 2x5120 columns).
+template <int TYPE, int ALONG, bool WHOLE>
+__global__ __launch_bounds__(512, 4) void k_fp8_both(const wq_fp8_both_args first, const wq_fp8_both_args second, unsigned blocks) {
     using T = typename Elem<TYPE>::type;
-    constexpr int STRIDE = 16 * 128 + 16 * 16;   // bytes of a plane of 128 columns' pieces in LDS, 16 of them between each eight columns
-    __shared__ __attribute__((aligned(16))) char image[(ALONG == 2 ? 16 : 8) * STRIDE];
+    constexpr int RT = 4, THREADS = 512, PLANES = ALONG == 2 ? 16 : 8;
+    // bytes of a plane of 128 columns' pieces in LDS, 16 of them between each eight columns, and between planes: both ways in spread over the banks
+    constexpr int STRIDE = 16 * 128 + 16 * 16 + 16;
+    __shared__ __attribute__((aligned(16))) char image[PLANES * STRIDE];
     const wq_fp8_both_args a = blockIdx.x < blocks ? first : second;
     const unsigned id = blockIdx.x < blocks ? blockIdx.x : blockIdx.x - blocks;
-    __shared__ uint32_t top_s[4][128];
-    __shared__ float sum_s[4][128];
+    __shared__ uint32_t top_s[THREADS / 64][128];
+    __shared__ float sum_s[THREADS / 64][128];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, octet = lane & 15, sub = tid >> 4;
     int g = id % a.groups;
     const int tb = id / a.groups;
@@ -132,38 +155,29 @@ __global__ __launch_bounds__(256, ALONG == 0 ? 4 : 3) void k_fp8_both(const wq_f
         if (g < 2 * pairs) g = (g >> 4) * 8 + (g & 7) + ((g & 8) ? a.groups / 2 : 0);
         else g -= g < 2 * pairs + (a.groups / 2 - pairs) ? pairs : 0;
     }
-    const int c = g * kGroup + octet * 8, p0 = tb * kGroup + sub * 8;
+    const int c = g * kGroup + octet * 8, p0 = tb * kGroup + sub * RT;
     const int outs = a.gated ? a.cols / 2 : a.cols;
     const bool up = a.gated && c >= outs;   // (outs is a multiple of 32: all eight columns are of one half)
     const int cy = up ? c - outs : c;       // the column of dy
-    const int n = (a.gated ? (up ? a.cols : outs) : a.cols) - c;
-    float v[8][8];
+    float v[RT][8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const long p = p0 + i;
-        const int m = p < a.rows ? n : 0;
-        load8_some<T>((const T *)a.v + p * a.vs + cy, m, v[i]);
-        if (!a.pre) continue;
-        float z[8], slope[8], value[8];
-        load8_some<T>((const T *)a.pre + p * a.ps + cy, m, z);
-        activation_slope(z, a.act, slope, value);
-        if (up) {
+    for (int i = 0; i < RT; ++i)   // (rows past the end read the last one, as nothing)
+        load8_row<T, WHOLE>((const T *)a.v + (long)min(p0 + i, a.rows - 1) * a.vs, cy, outs, p0 + i < a.rows, v[i]);
+    if (a.pre) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] *= value[j];
-        } else if (a.gated) {
-            float u[8];
-            load8_some<T>((const T *)a.pre + p * a.ps + outs + cy, m, u);
+        for (int i = 0; i < RT; ++i) {
+            const T *pre = (const T *)a.pre + (long)min(p0 + i, a.rows - 1) * a.ps;
+            float z[8], slope[8], value[8];
+            load8_row<T, WHOLE>(pre, cy, outs, p0 + i < a.rows, z);
+            if (a.gated && !up) {
+                float u[8];
+                load8_row<T, WHOLE>(pre + outs, cy, outs, p0 + i < a.rows, u);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * u[j] * slope[j];
-        } else {
+                for (int j = 0; j < 8; ++j) v[i][j] *= u[j];
+            }
+            activation_slope(z, a.act, slope, value);   // (finite at zero, which stands for what does not exist)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] *= slope[j];
-        }
-        // (0 times an infinite or NaN slope, where nothing exists)
-        if (m < 8) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j >= m) v[i][j] = 0.0f;
+            for (int j = 0; j < 8; ++j) v[i][j] *= up ? value[j] : slope[j];
         }
     }
     if (ALONG || a.db) {
@@ -174,14 +188,12 @@ __global__ __launch_bounds__(256, ALONG == 0 ? 4 : 3) void k_fp8_both(const wq_f
             top[j] = 0;
             sum[j] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < RT; ++i) {
                 top[j] = max(top[j], magnitude(v[i][j]));
                 sum[j] += v[i][j];
             }
-            top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 16));
-            top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 32));
-            sum[j] += __shfl_xor(sum[j], 16);
-            sum[j] += __shfl_xor(sum[j], 32);
+            top[j] = rows_max(top[j]);
+            sum[j] = rows_sum(sum[j]);
         }
         if (lane < 16) {
 #pragma unroll
@@ -191,34 +203,40 @@ __global__ __launch_bounds__(256, ALONG == 0 ? 4 : 3) void k_fp8_both(const wq_f
             }
         }
         __syncthreads();
+        if (tid < 128) {   // of all rows
+            uint32_t t = 0;
+            float f = 0.0f;
+#pragma unroll
+            for (int k = 0; k < THREADS / 64; ++k) {
+                t = max(t, top_s[k][tid]);
+                f += sum_s[k][tid];
+            }
+            top_s[0][tid] = t;
+            if (a.db && g * kGroup + tid < a.cols) a.db[(size_t)tb * a.cols + g * kGroup + tid] = f;
+        }
+        if constexpr (ALONG != 0) __syncthreads();
     }
-    if (tid < 128 && a.db && g * kGroup + tid < a.cols)
-        a.db[(size_t)tb * a.cols + g * kGroup + tid] = sum_s[0][tid] + sum_s[1][tid] + sum_s[2][tid] + sum_s[3][tid];
     if constexpr (ALONG != 0) {
         float s[8], r[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int k = octet * 8 + j;
-            pow2_scale(max(max(top_s[0][k], top_s[1][k]), max(top_s[2][k], top_s[3][k])), s[j], r[j]);
+            pow2_scale(top_s[0][octet * 8 + j], s[j], r[j]);
             if (sub == 0 && c + j < a.colsT) a.scalesT[(size_t)tb * a.colsT + c + j] = s[j];
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float t[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) t[i] = v[i][j] * r[j];
-            const uint2 codes = make_uint2(e4m3x4(t[0], t[1], t[2], t[3]), e4m3x4(t[4], t[5], t[6], t[7]));
+            const uint32_t codes = e4m3x4(v[0][j] * r[j], v[1][j] * r[j], v[2][j] * r[j], v[3][j] * r[j]);
             if constexpr (ALONG == 1) {
-                *(uint2 *)(image + (sub >> 1) * STRIDE + octet * 144 + j * 16 + (sub & 1) * 8) = codes;
+                *(uint32_t *)(image + (sub >> 2) * STRIDE + octet * 144 + j * 16 + (sub & 3) * 4) = codes;
             } else {   // the values that the codes stand for are bf16 numbers, a piece has eight of them
-                *(v8bf *)(image + sub * STRIDE + octet * 144 + j * 16) = bf16_of_codes((int)codes.x, (int)codes.y, s[j]);
+                const v2bf lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, s[j], false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, s[j], true);
+                *(v4bf *)(image + (sub >> 1) * STRIDE + octet * 144 + j * 16 + (sub & 1) * 8) = v4bf{lo[0], lo[1], hi[0], hi[1]};
             }
         }
         __syncthreads();
-        constexpr int PLANES = ALONG == 1 ? 8 : 16;
 #pragma unroll
-        for (int i = 0; i < PLANES / 2; ++i) {
-            const int k = (i * 256 + tid) & 127, plane = (i * 256 + tid) >> 7;
+        for (int i = 0; i < PLANES * 128 / THREADS; ++i) {
+            const int k = (i * THREADS + tid) & 127, plane = (i * THREADS + tid) >> 7;
             if (g * kGroup + k >= a.colsT) continue;
             *(uint4 *)(a.codesT + ((size_t)(tb * PLANES + plane) * a.colsT + g * kGroup + k) * 16) =
                 *(const uint4 *)(image + plane * STRIDE + (k >> 3) * 144 + (k & 7) * 16);
@@ -228,7 +246,7 @@ __global__ __launch_bounds__(256, ALONG == 0 ? 4 : 3) void k_fp8_both(const wq_f
     if (!a.codes) return;
     // along the columns: a row's piece is two lanes' eight codes
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < RT; ++i) {
         uint32_t top = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[i][j]));
@@ -238,14 +256,14 @@ __global__ __launch_bounds__(256, ALONG == 0 ? 4 : 3) void k_fp8_both(const wq_f
         if (octet == 0 && p0 + i < a.rows) a.scales[(size_t)g * a.P + p0 + i] = s;
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[i][j] *= r;
-        const int row = sub * 8 + i;
+        const int row = sub * RT + i;
         *(uint2 *)(image + (octet >> 1) * STRIDE + (row >> 3) * 144 + (row & 7) * 16 + (octet & 1) * 8) =
             make_uint2(e4m3x4(v[i][0], v[i][1], v[i][2], v[i][3]), e4m3x4(v[i][4], v[i][5], v[i][6], v[i][7]));
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = (i * 256 + tid) & 127, plane = (i * 256 + tid) >> 7;
+    for (int i = 0; i < 8 * 128 / THREADS; ++i) {
+        const int row = (i * THREADS + tid) & 127, plane = (i * THREADS + tid) >> 7;
         if (tb * kGroup + row >= a.rows) continue;
         *(uint4 *)(a.codes + ((size_t)(g * 8 + plane) * a.P + tb * kGroup + row) * 16) =
             *(const uint4 *)(image + plane * STRIDE + (row >> 3) * 144 + (row & 7) * 16);
@@ -312,10 +330,12 @@ __global__ __launch_bounds__(256) void k_fp8_weights(const wq_fp8_weight_args a)
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            load8_some<T>((const T *)a.w + (long)(o0 + i) * a.ws + c, o0 + i < a.Cout ? a.Cin - c : 0, v[i]);
+            load8_row<T, false>((const T *)a.w + (long)min(o0 + i, a.Cout - 1) * a.ws, c, a.Cin, o0 + i < a.Cout, v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[i][j]));
-        }
 #pragma unroll
         for (int m = 32; m > 0; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
         if (lane == 0) top_s[w] = top;
@@ -368,10 +388,15 @@ __global__ __launch_bounds__(256) void k_fp8_weights(const wq_fp8_weight_args a)
 template <int TYPE>
 void launch_both(const wq_fp8_both_args &x, const wq_fp8_both_args &dy, int along, hipStream_t s) {
     const unsigned bands = (unsigned)((dy.rows + kGroup - 1) / kGroup), blocks = x.v ? (unsigned)x.groups * bands : 0u;
-    const dim3 grid(blocks + (unsigned)dy.groups * bands), block(256);
-    if (along == 0) hipLaunchKernelGGL((k_fp8_both<TYPE, 0>), grid, block, 0, s, x, dy, blocks);
-    else if (along == 1) hipLaunchKernelGGL((k_fp8_both<TYPE, 1>), grid, block, 0, s, x, dy, blocks);
-    else hipLaunchKernelGGL((k_fp8_both<TYPE, 2>), grid, block, 0, s, x, dy, blocks);
+    const dim3 grid(blocks + (unsigned)dy.groups * bands), block(512);
+    auto launch = [&](auto whole) {
+        constexpr bool W = decltype(whole)::value;
+        if (along == 0) hipLaunchKernelGGL((k_fp8_both<TYPE, 0, W>), grid, block, 0, s, x, dy, blocks);
+        else if (along == 1) hipLaunchKernelGGL((k_fp8_both<TYPE, 1, W>), grid, block, 0, s, x, dy, blocks);
+        else hipLaunchKernelGGL((k_fp8_both<TYPE, 2, W>), grid, block, 0, s, x, dy, blocks);
+    };
+    if (x.cols % 8 == 0 && dy.cols % 8 == 0) launch(std::true_type{});
+    else launch(std::false_type{});
 }
 
 }  // namespace
@@ -379,9 +404,14 @@ void launch_both(const wq_fp8_both_args &x, const wq_fp8_both_args &dy, int alon
 hipError_t wq_launch_fp8_quantize(const wq_fp8_rows_args &a, int type, hipStream_t s) {
     const long units = (long)a.groups * ((a.rows + 15) / 16);
     const dim3 grid((unsigned)((units + 3) / 4)), block(256);
-    if (type == WQ_FP32) hipLaunchKernelGGL((k_fp8_quantize<WQ_FP32>), grid, block, 0, s, a);
-    else if (type == WQ_BF16) hipLaunchKernelGGL((k_fp8_quantize<WQ_BF16>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((k_fp8_quantize<WQ_FP16>), grid, block, 0, s, a);
+    auto launch = [&](auto whole) {
+        constexpr bool W = decltype(whole)::value;
+        if (type == WQ_FP32) hipLaunchKernelGGL((k_fp8_quantize<WQ_FP32, W>), grid, block, 0, s, a);
+        else if (type == WQ_BF16) hipLaunchKernelGGL((k_fp8_quantize<WQ_BF16, W>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((k_fp8_quantize<WQ_FP16, W>), grid, block, 0, s, a);
+    };
+    if (a.cols % 8 == 0) launch(std::true_type{});
+    else launch(std::false_type{});
     return hipGetLastError();
 }
 

@@ -112,11 +112,11 @@ __global__ __launch_bounds__(FUSED ? 512 : 256) void k_fp8_rows(const wq_fp8_pro
     const int chunks = (a.xcols + 511) / 512, pieces = FUSED ? x_rows * chunks : 0;
     float v[8];
     auto load_piece = [&](int i) {
-        const int c = i % chunks * 512 + lane * 8, n = i < pieces ? a.xcols - c : 0;
-        const long at = (p0 + (long)(i / chunks)) * a.xs + c;
-        if (a.type == WQ_FP32) load8_some((const float *)a.x + at, n, v);
-        else if (a.type == WQ_BF16) load8_some((const __bf16 *)a.x + at, n, v);
-        else load8_some((const _Float16 *)a.x + at, n, v);
+        const int c = i % chunks * 512 + lane * 8, row = min(i / chunks, x_rows - 1);   // (past the last piece: some piece again)
+        const long at = (p0 + (long)row) * a.xs;
+        if (a.type == WQ_FP32) load8_row<float, false>((const float *)a.x + at, c, a.xcols, true, v);
+        else if (a.type == WQ_BF16) load8_row<__bf16, false>((const __bf16 *)a.x + at, c, a.xcols, true, v);
+        else load8_row<_Float16, false>((const _Float16 *)a.x + at, c, a.xcols, true, v);
     };
     if constexpr (FUSED) {
         load_piece(ks);

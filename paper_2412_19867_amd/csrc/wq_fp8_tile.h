@@ -61,17 +61,16 @@ __device__ __forceinline__ v4f fp8_residual(const wq_fp8_product &a, long p, int
 __device__ __forceinline__ v4f fp8_bias(const wq_fp8_product &a, int o) { return a.bias ? *(const v4f *)(a.bias + o) : v4f{}; }
 
 // WA x WB waves, each with NA x NB blocks of 16 x 16 (a's rows x b's); KS such teams share a tile's reduction, each a contiguous part of K.
-// A stage is 64 H of K: the operands' pieces go straight into LDS with the scales of the rows, in the order in which lanes read them, into
-// a ring of NST stages per team, NST - 1 of them in flight.
-template <int MODE, int NA, int NB, int WA, int WB, int KS, int H, int NST>
+// A stage has U KiB of each 16-row block, a group's eight pieces or four of them: they go straight into LDS with the scales of the rows, in the
+// order in which lanes read them, into a ring of NST stages per team, NST - 1 of them in flight.
+template <int MODE, int NA, int NB, int WA, int WB, int KS, int U, int NST>
 __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_product a, const wq_fp8_grid t) {
     constexpr int W = WA * WB, OA = NA * WA, OB = NB * WB;   // blocks of the workgroup tile
     constexpr bool EXACT = MODE == WQ_FP8_EXACT || MODE == WQ_FP8_EXACT_FP32, ROWS = MODE == WQ_FP8_DIRECT_ROWS, VALUES = MODE == WQ_FP8_VALUES;
     constexpr bool DIRECT = !EXACT && !VALUES, MADD = MODE == WQ_FP8_EXACT_FP32 || MODE == WQ_FP8_DIRECT_FP32;
-    static_assert(H == 2 || (H == 1 && !DIRECT), "the direct product takes a whole group");
-    constexpr int UA = VALUES ? 2 * H : H, UB = UA;   // KiB of a 16-row block in a stage
+    static_assert(U == 2 || (U == 1 && !DIRECT), "the direct product takes a whole group");
     constexpr int QB = VALUES ? 0 : (OB + 3) / 4, QA = ROWS ? (OA + 3) / 4 : VALUES ? 0 : 1;   // loads of scales, 64 of one group each
-    constexpr int BOFF = OA * UA * 1024, SBOFF = BOFF + OB * UB * 1024, SAOFF = SBOFF + QB * 256, STAGE = SAOFF + QA * 256;
+    constexpr int BOFF = OA * U * 1024, SBOFF = BOFF + OB * U * 1024, SAOFF = SBOFF + QB * 256, STAGE = SAOFF + QA * 256;
     constexpr int RS = 16 * NA + 4, PART = 16 * RS;   // epilogue: floats of a row and of a wave's 16 rows
     constexpr int BYTES = NST * STAGE > W * PART * 4 ? NST * STAGE : W * PART * 4;
     __shared__ __attribute__((aligned(16))) char lds[KS * BYTES];
@@ -87,7 +86,7 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
     const int pa = in_band / high, pb = band * 8 + in_band % high;
     // the team's stages; all teams make the same number of turns
     const int part = slice * KS + team, parts = t.slices * KS;
-    constexpr int PER = 2 / H;   // stages of a group
+    constexpr int PER = VALUES ? 4 / U : 2 / U;   // stages of 128 of K
     const int s_beg = (int)((long)part * a.groups / parts) * PER, s_end = (int)((long)(part + 1) * a.groups / parts) * PER,
               turns = (a.groups + parts - 1) / parts * PER;
     char *const stages = lds + team * BYTES;
@@ -104,27 +103,25 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
     const __amdgpu_buffer_rsrc_t rB = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.b.data), 0, (int)a.b.bytes, kBufFlags);
 
     // ---- the loader ---- (rows past the end read the last one again, whose sums are not stored)
-    constexpr int LA = OA * UA / W, LB = OB * UB / W;   // loads of 1 KiB of a wave: half a group of a block each
-    static_assert(LA * W == OA * UA && LB * W == OB * UB, "the waves share the loads evenly");
+    constexpr int LA = OA * U / W, LB = OB * U / W;   // loads of 1 KiB of a wave: half a group of a block each
+    static_assert(LA * W == OA * U && LB * W == OB * U, "the waves share the loads evenly");
     unsigned vA[LA], vB[LB];
     auto place = [&](const wq_fp8_operand &o, int row, int u) {
         const int r = min(row + l16, o.rows - 1);
-        const unsigned group = VALUES ? (unsigned)(u >> 1) * o.group : 0u;
-        return (unsigned)(r >> 4) * o.block + group + ((unsigned)(u & 1) * 4u + q) * o.piece + (unsigned)(r & 15) * 16u;
+        return (unsigned)(r >> 4) * o.block + ((unsigned)u * 4u + q) * o.piece + (unsigned)(r & 15) * 16u;
     };
 #pragma unroll
-    for (int u = 0; u < LA; ++u) vA[u] = place(a.a, row_of((wave * LA + u) / UA), (wave * LA + u) % UA);
+    for (int u = 0; u < LA; ++u) vA[u] = place(a.a, row_of((wave * LA + u) / U), (wave * LA + u) % U);
 #pragma unroll
-    for (int u = 0; u < LB; ++u) vB[u] = place(a.b, b0 + (wave * LB + u) / UB * 16, (wave * LB + u) % UB);
+    for (int u = 0; u < LB; ++u) vB[u] = place(a.b, b0 + (wave * LB + u) / U * 16, (wave * LB + u) % U);
     // loads of scales, b's and then a's, are dealt to the waves in turn (a wave without one of its own repeats another's)
     const unsigned vSA = (unsigned)(min(row_of(min(lane, OA - 1)), a.a.rows - 1) >> 7) * (unsigned)a.a.scale_step * 4u;
     constexpr int NS = QA + QB, LS = (NS + W - 1) / W, LPS = LA + LB + LS;
     auto issue = [&](int s, int slot) {
         char *const to = stages + slot * STAGE;
-        const int g = s / PER;
-        const unsigned half = H == 1 ? (unsigned)(s & 1) * 4u : 0u;   // half a group of codes: pieces of its first or second half
-        const unsigned oA = VALUES ? (unsigned)(s * H) * a.a.group : (unsigned)g * a.a.group + half * a.a.piece;
-        const unsigned oB = VALUES ? (unsigned)(s * H) * a.b.group : (unsigned)g * a.b.group + half * a.b.piece;
+        const int g = U == 2 ? s : s >> 1;   // the group, of 128 codes or 64 values
+        const unsigned half = U == 1 ? (unsigned)(s & 1) * 4u : 0u;
+        const unsigned oA = (unsigned)g * a.a.group + half * a.a.piece, oB = (unsigned)g * a.b.group + half * a.b.piece;
 #pragma unroll
         for (int u = 0; u < LA; ++u) lds_load16(rA, to + (wave * LA + u) * 1024, vA[u], oA);
 #pragma unroll
@@ -156,7 +153,7 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
 #pragma unroll
         for (int f = 0; f < NB; ++f) M[e][f] = v4f{0.f, 0.f, 0.f, 0.f};
 
-    const char *const atA = stages + wa * NA * UA * 1024 + lane * 16, *const atB = stages + BOFF + wb * NB * UB * 1024 + lane * 16;
+    const char *const atA = stages + wa * NA * U * 1024 + lane * 16, *const atB = stages + BOFF + wb * NB * U * 1024 + lane * 16;
     const char *const atSB = stages + SBOFF + wb * NB * 64 + l16 * 4, *const atSA = stages + SAOFF + (ROWS ? wa * NA * 64 + l16 * 4 : wa * NA * 4);
     auto compute = [&](int s, int slot) {
         const char *const pA = atA + slot * STAGE, *const pB = atB + slot * STAGE;
@@ -198,34 +195,33 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
 #pragma unroll
                 for (int f = 0; f < NB; ++f) sb[f] = *(const float *)(atSB + slot * STAGE + f * 64);
             }
-            auto read = [&](const char *p, float scale, v8bf (&v)[2]) {   // 64 of K: two products of 32
-                if constexpr (VALUES) {
+            constexpr int NK = VALUES ? U : 2 * U;   // products of 32 of K
+            auto read = [&](const char *p, float scale, v8bf (&v)[NK]) {
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) v[k] = *(const v8bf *)(p + k * 1024);
-                } else {
-                    const v4i c = *(const v4i *)p;
-                    v[0] = bf16_of_codes(c.x, c.y, scale);
-                    v[1] = bf16_of_codes(c.z, c.w, scale);
+                for (int u = 0; u < U; ++u) {
+                    const v4i c = *(const v4i *)(p + u * 1024);
+                    if constexpr (VALUES) {
+                        v[u] = __builtin_bit_cast(v8bf, c);
+                    } else {
+                        v[2 * u] = bf16_of_codes(c.x, c.y, scale);
+                        v[2 * u + 1] = bf16_of_codes(c.z, c.w, scale);
+                    }
                 }
             };
-            constexpr int STEP = UA / H * 1024, NK = 2 * H;
-            v8bf bv[NB][H][2];
+            v8bf bv[NB][NK];
 #pragma unroll
-            for (int f = 0; f < NB; ++f)
-#pragma unroll
-                for (int h = 0; h < H; ++h) read(pB + (f * H + h) * STEP, sb[f], bv[f][h]);
+            for (int f = 0; f < NB; ++f) read(pB + f * U * 1024, sb[f], bv[f]);
 #pragma unroll
             for (int e = 0; e < NA; ++e) {
-                v8bf av[H][2];
-#pragma unroll
-                for (int h = 0; h < H; ++h) read(pA + (e * H + h) * STEP, MADD || VALUES ? 1.0f : sa[e], av[h]);
+                v8bf av[NK];
+                read(pA + e * U * 1024, MADD || VALUES ? 1.0f : sa[e], av);
                 v4f P[NB];
 #pragma unroll
                 for (int f = 0; f < NB; ++f) P[f] = MADD ? v4f{0.f, 0.f, 0.f, 0.f} : M[e][f];
 #pragma unroll
                 for (int k = 0; k < NK; ++k)
 #pragma unroll
-                    for (int f = 0; f < NB; ++f) P[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[k / 2][k % 2], bv[f][k / 2][k % 2], P[f], 0, 0, 0);
+                    for (int f = 0; f < NB; ++f) P[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[k], bv[f][k], P[f], 0, 0, 0);
 #pragma unroll
                 for (int f = 0; f < NB; ++f) {
                     if constexpr (MADD) {
@@ -300,7 +296,7 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
     }
 }
 
-template <int MODE, int NA, int NB, int WA, int WB, int KS, int H, int NST>
+template <int MODE, int NA, int NB, int WA, int WB, int KS, int U, int NST>
 hipError_t launch_fp8_tile(const wq_fp8_product &a, int slices, float *partial, hipStream_t s) {
     wq_fp8_grid t;
     const int across = a.gated ? 8 * NA * WA : 16 * NA * WA;   // columns of y in a tile
@@ -311,20 +307,19 @@ hipError_t launch_fp8_tile(const wq_fp8_product &a, int slices, float *partial, 
     t.per_xcd = (t.total + 7) / 8;
     t.partial = partial;
     t.slices = slices;
-    hipLaunchKernelGGL((k_fp8_tile<MODE, NA, NB, WA, WB, KS, H, NST>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * WA * WB * KS), 0, s, a, t);
+    hipLaunchKernelGGL((k_fp8_tile<MODE, NA, NB, WA, WB, KS, U, NST>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * WA * WB * KS), 0, s, a, t);
     return hipGetLastError();
 }
 
 template <int MODE>
 hipError_t launch_fp8_form(const wq_fp8_product &a, int form, int slices, float *partial, hipStream_t s) {
-    constexpr int H = MODE == WQ_FP8_VALUES ? 1 : 2;
     switch (form) {
-        case WQ_FP8_TILE_256: return launch_fp8_tile<MODE, 8, 4, 2, 4, 1, H, 2>(a, slices, partial, s);
-        case WQ_FP8_TILE_128: return launch_fp8_tile<MODE, 4, 4, 2, 2, 1, H, 2>(a, slices, partial, s);
-        case WQ_FP8_TILE_128x64: return launch_fp8_tile<MODE, 4, 2, 2, 2, 1, H, 2>(a, slices, partial, s);
-        case WQ_FP8_TILE_64: return launch_fp8_tile<MODE, 2, 2, 2, 2, 1, H, 2>(a, slices, partial, s);
-        case WQ_FP8_TILE_64_2: return launch_fp8_tile<MODE, 2, 2, 2, 2, 2, H, 2>(a, slices, partial, s);
-        default: return launch_fp8_tile<MODE, 2, 2, 2, 2, 4, H, 2>(a, slices, partial, s);
+        case WQ_FP8_TILE_256: return launch_fp8_tile<MODE, 8, 4, 2, 4, 1, 2, 2>(a, slices, partial, s);
+        case WQ_FP8_TILE_128: return launch_fp8_tile<MODE, 4, 4, 2, 2, 1, 2, 2>(a, slices, partial, s);
+        case WQ_FP8_TILE_128x64: return launch_fp8_tile<MODE, 4, 2, 2, 2, 1, 2, 2>(a, slices, partial, s);
+        case WQ_FP8_TILE_64: return launch_fp8_tile<MODE, 2, 2, 2, 2, 1, 2, 2>(a, slices, partial, s);
+        case WQ_FP8_TILE_64_2: return launch_fp8_tile<MODE, 2, 2, 2, 2, 2, 2, 2>(a, slices, partial, s);
+        default: return launch_fp8_tile<MODE, 2, 2, 2, 2, 4, 2, 2>(a, slices, partial, s);
     }
 }
 
