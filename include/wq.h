@@ -459,7 +459,7 @@ typedef struct {
     uint64_t ws_dz_codes_off, ws_dz_scales_off;       /* backward: codes of dz as those of x, [O][8][rows][16], [O][rows] */
     uint64_t ws_xt_off, ws_xt_scales_off;             /* of x along the rows: codes, or bf16 values, and scales */
     uint64_t ws_dzt_off, ws_dzt_scales_off;           /* of dz along the rows */
-    uint64_t ws_db_off, ws_part_off;                  /* partial sums of the bias's and the weights' gradients */
+    uint64_t ws_db_off;                               /* partial sums of the bias's gradient */
 } wq_fp8_layout_t;
 
 wq_status_t wq_fp8_plan_create(wq_fp8_plan_t **out, int rows, int Cin, int Cout, int backward, int fp32_scales);

@@ -67,7 +67,7 @@ wq_status_t run_product(const wq_fp8_plan *plan, wq_fp8_product &p, bool exact, 
     const wq_fp8_form form = wq_fp8_choose_form(p.rows, p.outs, p.gated, p.groups, exact);
     if (form.row_blocks) return status(wq_launch_fp8_rows(p, form.row_blocks, s));
     const int mode = exact ? plan->fp32_scales ? WQ_FP8_EXACT_FP32 : WQ_FP8_EXACT : plan->fp32_scales ? WQ_FP8_DIRECT_FP32 : WQ_FP8_DIRECT;
-    return status(wq_launch_fp8_tile(p, mode, form.tile, 1, nullptr, s));
+    return status(wq_launch_fp8_tile(p, mode, form.tile, s));
 }
 
 bool is_captured(hipStream_t s) {
@@ -165,8 +165,6 @@ wq_status_t wq_fp8_plan_create(wq_fp8_plan_t **out, int rows, int Cin, int Cout,
     take(L.ws_dzt_off, TB * 256 * Cout16);
     take(L.ws_dzt_scales_off, TB * Cout16 * 4);
     take(L.ws_db_off, TB * (uint64_t)Cout * 4);
-    const int most_slices = wq_fp8_choose_grad_form(Cout, Cin, (int)TB).slices;
-    take(L.ws_part_off, most_slices > 1 ? (uint64_t)most_slices * Cout * Cin * 4 : 0);
     L.ws_bytes = at;
     p->prepared.store(0);
     *out = p;
@@ -323,7 +321,6 @@ wq_status_t wq_fp8_backward(const wq_fp8_plan_t *plan, void *stream, int rows, i
 
     if (dw_dev) {   // columns of dw are rows of `a`, x's columns
         const wq_fp8_form form = wq_fp8_choose_grad_form(plan->Cout, plan->Cin, TB);
-        float *part = (float *)(ws + L.ws_part_off);
         wq_fp8_product p = {};
         p.a = planes((const uint8_t *)(ws + L.ws_xt_off), (const float *)(ws + L.ws_xt_scales_off), plan->Cin16, plan->Cin16, TB, wide_values);
         p.b = planes((const uint8_t *)(ws + L.ws_dzt_off), (const float *)(ws + L.ws_dzt_scales_off), plan->Cout16, plan->Cout16, TB, wide_values);
@@ -331,10 +328,7 @@ wq_status_t wq_fp8_backward(const wq_fp8_plan_t *plan, void *stream, int rows, i
         p.y = dw_dev; p.ys = dw_stride; p.rows = plan->Cout; p.outs = p.cols = plan->Cin; p.type = dw_type;
         if (accumulate) p.res = dw_dev, p.rs = dw_stride;
         set_wide(p);
-        if ((e = wq_launch_fp8_tile(p, wide_values ? WQ_FP8_VALUES : WQ_FP8_DIRECT_ROWS, form.tile, form.slices, part, s)) != hipSuccess) return status(e);
-        if (form.slices > 1 &&
-            (e = wq_launch_fp8_join(part, form.slices, plan->Cout, plan->Cin, dw_dev, dw_stride, dw_type, accumulate, s)) != hipSuccess)
-            return status(e);
+        if ((e = wq_launch_fp8_tile(p, wide_values ? WQ_FP8_VALUES : WQ_FP8_DIRECT_ROWS, form.tile, s)) != hipSuccess) return status(e);
     }
     if (dx_dev) {
         const char *b = (const char *)weight_blob_dev;

@@ -55,7 +55,7 @@ enum wq_fp8_mode {
     WQ_FP8_VALUES = 5       // the operands hold values, no scales
 };
 
-hipError_t wq_launch_fp8_tile(const wq_fp8_product &p, int mode, int form, int slices, float *partial, hipStream_t s);
+hipError_t wq_launch_fp8_tile(const wq_fp8_product &p, int mode, int form, hipStream_t s);   // a wq_fp8_tile_form
 hipError_t wq_launch_fp8_rows(const wq_fp8_product &p, int row_blocks, hipStream_t s);
 
 namespace {   // every including file has its own

@@ -38,6 +38,5 @@ hipError_t wq_launch_fp8_quantize(const wq_fp8_rows_args &a, int type, hipStream
 // x (x.v null: not wanted) and dy in one launch; along: 0 no codes along the rows, 1 codes, 2 values in bf16
 hipError_t wq_launch_fp8_both(const wq_fp8_both_args &x, const wq_fp8_both_args &dy, int type, int along, hipStream_t s);
 hipError_t wq_launch_fp8_db(const float *part, int blocks, int cols, float *db, int accumulate, hipStream_t s);
-hipError_t wq_launch_fp8_join(const float *part, int slices, int rows, int cols, void *dw, long stride, int type, int accumulate, hipStream_t s);
 hipError_t wq_launch_fp8_zero(void *dw, int rows, int cols, long stride, int type, float *db, hipStream_t s);
 hipError_t wq_launch_fp8_weights(const wq_fp8_weight_args &a, int type, bool load, hipStream_t s);

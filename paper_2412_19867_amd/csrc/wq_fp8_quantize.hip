@@ -277,17 +277,6 @@ __global__ __launch_bounds__(1024) void k_fp8_db(const float *part, int blocks, 
     if (threadIdx.x < 64 && c < cols) db[c] = (float)(accumulate ? (double)db[c] + s : s);
 }
 
-// The weights' gradient of K's slices [slices][rows cols], in the slices' order.
-template <typename T>
-__global__ __launch_bounds__(256) void k_fp8_join(const float *part, int slices, int rows, int cols, T *dw, long stride, int accumulate) {
-    const long i = (long)blockIdx.x * 256 + threadIdx.x, n = (long)rows * cols;
-    if (i >= n) return;
-    float s = 0.0f;
-    for (int k = 0; k < slices; ++k) s += part[(size_t)k * n + i];
-    T *at = dw + i / cols * stride + i % cols;
-    *at = (T)(accumulate ? s + (float)*at : s);
-}
-
 template <typename T>
 __global__ __launch_bounds__(256) void k_fp8_zero(T *dw, int rows, int cols, long stride, float *db) {
     const long i = (long)blockIdx.x * 256 + threadIdx.x;
@@ -424,14 +413,6 @@ hipError_t wq_launch_fp8_both(const wq_fp8_both_args &x, const wq_fp8_both_args 
 
 hipError_t wq_launch_fp8_db(const float *part, int blocks, int cols, float *db, int accumulate, hipStream_t s) {
     hipLaunchKernelGGL(k_fp8_db, dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, s, part, blocks, cols, db, accumulate);
-    return hipGetLastError();
-}
-
-hipError_t wq_launch_fp8_join(const float *part, int slices, int rows, int cols, void *dw, long stride, int type, int accumulate, hipStream_t s) {
-    const dim3 grid((unsigned)(((long)rows * cols + 255) / 256)), block(256);
-    if (type == WQ_FP32) hipLaunchKernelGGL((k_fp8_join<float>), grid, block, 0, s, part, slices, rows, cols, (float *)dw, stride, accumulate);
-    else if (type == WQ_BF16) hipLaunchKernelGGL((k_fp8_join<__bf16>), grid, block, 0, s, part, slices, rows, cols, (__bf16 *)dw, stride, accumulate);
-    else hipLaunchKernelGGL((k_fp8_join<_Float16>), grid, block, 0, s, part, slices, rows, cols, (_Float16 *)dw, stride, accumulate);
     return hipGetLastError();
 }
 

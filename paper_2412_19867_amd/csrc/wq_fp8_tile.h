@@ -22,9 +22,7 @@ __device__ __forceinline__ void wait_and_barrier() {
 }
 
 struct wq_fp8_grid {
-    int nA, nB, tiles, total, per_xcd;   // tiles along a and b, their number, with K's slices, the share of each XCD
-    float *partial;                      // slices > 1: their sums, [slice][rows][cols]
-    int slices;
+    int nA, nB, total, per_xcd;   // tiles along a and b, their number, the share of each XCD
 };
 
 // The epilogue of columns o .. o + 3 of rows p, p + step, .. (R of them) from their sums with the bias (gated: up, those of the other
@@ -81,14 +79,11 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
     // a's tile before the next follows
     const int logical = (int)(blockIdx.x & 7u) * t.per_xcd + (int)(blockIdx.x >> 3);
     if (logical >= t.total) return;   // the whole workgroup leaves, before any barrier
-    const int slice = logical / t.tiles, tile = logical - slice * t.tiles;
-    const int band = tile / (8 * t.nA), in_band = tile - band * 8 * t.nA, high = min(8, t.nB - band * 8);
+    const int band = logical / (8 * t.nA), in_band = logical - band * 8 * t.nA, high = min(8, t.nB - band * 8);
     const int pa = in_band / high, pb = band * 8 + in_band % high;
     // the team's stages; all teams make the same number of turns
-    const int part = slice * KS + team, parts = t.slices * KS;
     constexpr int PER = VALUES ? 4 / U : 2 / U;   // stages of 128 of K
-    const int s_beg = (int)((long)part * a.groups / parts) * PER, s_end = (int)((long)(part + 1) * a.groups / parts) * PER,
-              turns = (a.groups + parts - 1) / parts * PER;
+    const int s_beg = team * a.groups / KS * PER, s_end = (team + 1) * a.groups / KS * PER, turns = (a.groups + KS - 1) / KS * PER;
     char *const stages = lds + team * BYTES;
 
     // the first row of a's block j of the tile.  Gated: the first half of a wave's blocks are the gate's, the second the same columns
@@ -253,19 +248,13 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
 
     // ---- epilogue ---- through LDS, 16 rows of a wave at a time: its lanes then hold whole runs of columns of a row
     float *mine = (float *)stages + wave * PART;
-    wq_fp8_product out = a;
-    if (t.slices > 1) {   // a slice's sums as they are
-        out.y = t.partial + (long)slice * a.rows * a.cols;
-        out.ys = a.cols; out.type = WQ_FP32; out.res = nullptr; out.bias = nullptr; out.pre = nullptr; out.act = WQ_ACT_NONE;
-        out.wide = a.cols % 4 == 0;
-    }
     const int shift = a.gated ? __builtin_ctz(2 * NA) : __builtin_ctz(4 * NA), quads = 1 << shift;
     const int c = (lane & (quads - 1)) * 4, o = (pa * WA + wa) * quads * 4 + c;
     const int row_step = 64 >> shift;
     v4f bias = {}, bias_up = {};
     if (o < a.outs) {
-        bias = fp8_bias(out, o);
-        if (a.gated) bias_up = fp8_bias(out, a.outs + o);
+        bias = fp8_bias(a, o);
+        if (a.gated) bias_up = fp8_bias(a, a.outs + o);
     }
     __syncthreads();   // the last stage has been read by all
 #pragma unroll
@@ -280,7 +269,7 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
             for (int row = (team * 64 + lane) >> shift; row < 16; row += row_step * KS) {   // (the teams share the rows)
                 const int p = b0 + (wb * NB + f) * 16 + row;
                 if (p >= a.rows) break;
-                const v4f res[1] = {fp8_residual(out, p, o)};
+                const v4f res[1] = {fp8_residual(a, p, o)};
                 const float *sums = (const float *)lds + wave * PART + row * RS + c;
                 v4f z[1] = {bias + *(const v4f *)sums}, up[1] = {};
                 if (a.gated) up[0] = bias_up + *(const v4f *)(sums + 8 * NA);
@@ -289,7 +278,7 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
                     z[0] += *(const v4f *)(sums + k * (BYTES / 4));
                     if (a.gated) up[0] += *(const v4f *)(sums + k * (BYTES / 4) + 8 * NA);
                 }
-                fp8_finish<1>(out, p, 0, o, z, up, res);
+                fp8_finish<1>(a, p, 0, o, z, up, res);
             }
         }
         __builtin_amdgcn_wave_barrier();
@@ -297,29 +286,26 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
 }
 
 template <int MODE, int NA, int NB, int WA, int WB, int KS, int U, int NST>
-hipError_t launch_fp8_tile(const wq_fp8_product &a, int slices, float *partial, hipStream_t s) {
+hipError_t launch_fp8_tile(const wq_fp8_product &a, hipStream_t s) {
     wq_fp8_grid t;
     const int across = a.gated ? 8 * NA * WA : 16 * NA * WA;   // columns of y in a tile
     t.nA = (a.outs + across - 1) / across;
     t.nB = (a.rows + 16 * NB * WB - 1) / (16 * NB * WB);
-    t.tiles = t.nA * t.nB;
-    t.total = t.tiles * slices;
+    t.total = t.nA * t.nB;
     t.per_xcd = (t.total + 7) / 8;
-    t.partial = partial;
-    t.slices = slices;
     hipLaunchKernelGGL((k_fp8_tile<MODE, NA, NB, WA, WB, KS, U, NST>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * WA * WB * KS), 0, s, a, t);
     return hipGetLastError();
 }
 
 template <int MODE>
-hipError_t launch_fp8_form(const wq_fp8_product &a, int form, int slices, float *partial, hipStream_t s) {
+hipError_t launch_fp8_form(const wq_fp8_product &a, int form, hipStream_t s) {
     switch (form) {
-        case WQ_FP8_TILE_256: return launch_fp8_tile<MODE, 8, 4, 2, 4, 1, 2, 2>(a, slices, partial, s);
-        case WQ_FP8_TILE_128: return launch_fp8_tile<MODE, 4, 4, 2, 2, 1, 2, 2>(a, slices, partial, s);
-        case WQ_FP8_TILE_128x64: return launch_fp8_tile<MODE, 4, 2, 2, 2, 1, 2, 2>(a, slices, partial, s);
-        case WQ_FP8_TILE_64: return launch_fp8_tile<MODE, 2, 2, 2, 2, 1, 2, 2>(a, slices, partial, s);
-        case WQ_FP8_TILE_64_2: return launch_fp8_tile<MODE, 2, 2, 2, 2, 2, 2, 2>(a, slices, partial, s);
-        default: return launch_fp8_tile<MODE, 2, 2, 2, 2, 4, 2, 2>(a, slices, partial, s);
+        case WQ_FP8_TILE_256: return launch_fp8_tile<MODE, 8, 4, 2, 4, 1, 2, 2>(a, s);
+        case WQ_FP8_TILE_128: return launch_fp8_tile<MODE, 4, 4, 2, 2, 1, 2, 2>(a, s);
+        case WQ_FP8_TILE_128x64: return launch_fp8_tile<MODE, 4, 2, 2, 2, 1, 2, 2>(a, s);
+        case WQ_FP8_TILE_64: return launch_fp8_tile<MODE, 2, 2, 2, 2, 1, 2, 2>(a, s);
+        case WQ_FP8_TILE_64_2: return launch_fp8_tile<MODE, 2, 2, 2, 2, 2, 2, 2>(a, s);
+        default: return launch_fp8_tile<MODE, 2, 2, 2, 2, 4, 2, 2>(a, s);
     }
 }
 

@@ -60,7 +60,7 @@ class Fp8Layout(ctypes.Structure):
                 [(k, ctypes.c_uint64) for k in
                  ("blob_bytes", "blob_codes_off", "blob_scales_off", "blob_bias_off", "blob_codes_t_off", "blob_scales_t_off",
                   "ws_bytes", "ws_codes_off", "ws_scales_off", "ws_dz_codes_off", "ws_dz_scales_off", "ws_xt_off", "ws_xt_scales_off",
-                  "ws_dzt_off", "ws_dzt_scales_off", "ws_db_off", "ws_part_off")])
+                  "ws_dzt_off", "ws_dzt_scales_off", "ws_db_off")])
 
 
 # wq_k2_variant_t (include/wq.h): the kernel instance of stages 2+3
