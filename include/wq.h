@@ -494,7 +494,8 @@ wq_status_t wq_fp8_layer_norm_quantize(const wq_fp8_plan_t *plan, void *stream, 
 /* The product with its epilogue, of the codes in the workspace:
  *   z = bias + x W^T;   gated 0: y = act(z) + residual;   gated 1: y[o] = act(z[o]) z[Cout/2 + o] + residual[o]
  * as wq_linear_matmul, in fp32 and rounded once to `type`.  Gated: Cout a multiple of 64, else UNSUPPORTED.  pre_dev (NULL: not wanted): z [rows][Cout] rounded to the type, for the backward pass.
- * y_dev may be residual_dev itself with the same stride. */
+ * y_dev may be residual_dev itself with the same stride; any other overlap of the tensors is the caller's error.  The workspace has to hold at
+ * least as many rows as the call multiplies. */
 wq_status_t wq_fp8_matmul(const wq_fp8_plan_t *plan, void *stream, int rows, const void *workspace_dev, size_t workspace_bytes,
                           const void *weight_blob_dev, size_t blob_bytes, int activation, int gated, int type,
                           const void *residual_dev, int64_t residual_stride, void *pre_dev, int64_t pre_stride, void *y_dev,
@@ -525,8 +526,8 @@ wq_status_t wq_fp8_backward(const wq_fp8_plan_t *plan, void *stream, int rows, i
                             int64_t dw_stride, float *db_dev, int accumulate);
 
 /* ---------------------------------------------------------------------------
- * Layer norm of rows of any float type and any length C >= 1 (strides, alignment and errors as above; more than 2^25 rows or 2^30
- * columns -> UNSUPPORTED):
+ * Layer norm of rows of any float type and any length C >= 1 (strides, alignment and errors as above; more than 2^25 pieces of 512
+ * columns, a row counted as eight at most, or 2^30 columns -> UNSUPPORTED):
  *   h = x + residual in fp32, y = (h - mean) / sqrt(var + eps) gamma + beta, rounded as wq_fp8_layer_norm_quantize's v and then
  *   once to the type.  sum_dev as there.  y_dev may be x_dev or residual_dev itself with the same stride; sum_dev and y_dev are
  *   two tensors. */

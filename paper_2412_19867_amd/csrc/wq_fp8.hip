@@ -135,7 +135,7 @@ wq_status_t wq_fp8_plan_create(wq_fp8_plan_t **out, int rows, int Cin, int Cout,
     const uint64_t B = ((uint64_t)Cin + 127) / 128, O = ((uint64_t)Cout + 127) / 128, TB = (R + 127) / 128;
     const uint64_t Cin16 = ((uint64_t)Cin + 15) / 16 * 16, Cout16 = ((uint64_t)Cout + 15) / 16 * 16;
     if (B * 128 * R > most || B * 128 * Cout16 > most || O * B * 4 > most) return WQ_ERR_UNSUPPORTED;
-    if (backward && (O * 128 * R > most || O * 128 * Cin16 > most || TB * 256 * Cin16 > most || TB * 256 * Cout16 > most || Cin16 * Cout16 > most / 4))
+    if (backward && (O * 128 * R > most || O * 128 * Cin16 > most || TB * 256 * Cin16 > most || TB * 256 * Cout16 > most))
         return WQ_ERR_UNSUPPORTED;
     wq_fp8_plan *p = new (std::nothrow) wq_fp8_plan();
     if (!p) return WQ_ERR_DEVICE;
