@@ -433,7 +433,8 @@ wq_status_t wq_linear_forward(const wq_direct_plan_t *plan, void *stream, int ro
  *   codes: the e4m3 number nearest to v / s (exact but for that one rounding), ties to even; NaN and infinity give NaN.
  * Weights of a checkpoint may have any fp32 scales instead (a plan made with fp32_scales), at a multiply-add per group and value.
  * Precision: a code times a power of two is a bf16 number, products of those are exact and the matrix core adds them with 24 bits:
- * z is within (Cin + 16) 2^-24 of |bias| + the sum of the terms' magnitudes.  Gradients that are stored as bf16 or fp16 (dx, dw) are formed from the
+ * z is within (Cin + 16) 2^-24 of |bias| + the sum of the terms' magnitudes, as long as codes times scales are normal bf16 numbers (2^-126
+ * and up).  Gradients that are stored as bf16 or fp16 (dx, dw) are formed from the
  * codes directly at up to twice the rate: of eight neighbouring products the matrix core then drops what lies 2^-13 below the largest,
  * some 1.5e-5 of the result in the root mean square, where the type's own rounding is 1e-4 or more.
  * Formats (sizes and offsets from wq_fp8_plan_layout; B = in_blocks, O = out_blocks, a piece is 16 codes of a row):
@@ -471,8 +472,8 @@ wq_status_t wq_fp8_weight_prepare(wq_fp8_plan_t *plan, void *stream, int type, c
                                   const float *bias_dev, void *weight_blob_dev, size_t blob_bytes);
 
 /* Weights as a checkpoint holds them: e4m3 codes [Cout][Cin] (row stride in bytes) and scales [out_blocks][in_blocks], contiguous,
- * either fp32 (any finite numbers; a plan without fp32_scales -> UNSUPPORTED) or e8m0 bytes (2^(byte - 127); 0 counts as 2^-126,
- * 255, which is NaN, as 2^127).  Codes that are NaN stay NaN. */
+ * either fp32 (any numbers; a plan without fp32_scales -> UNSUPPORTED) or e8m0 bytes (2^(byte - 127); 0 counts as 2^-126, 255, which is
+ * NaN, makes its block NaN).  Codes that are NaN stay NaN. */
 typedef enum { WQ_SCALE_FP32 = 0, WQ_SCALE_E8M0 = 1 } wq_scale_type_t;
 wq_status_t wq_fp8_weight_load(wq_fp8_plan_t *plan, void *stream, const void *codes_dev, int64_t codes_stride, int scale_type,
                                const void *scales_dev, const float *bias_dev, void *weight_blob_dev, size_t blob_bytes);
@@ -493,9 +494,10 @@ wq_status_t wq_fp8_layer_norm_quantize(const wq_fp8_plan_t *plan, void *stream, 
 
 /* The product with its epilogue, of the codes in the workspace:
  *   z = bias + x W^T;   gated 0: y = act(z) + residual;   gated 1: y[o] = act(z[o]) z[Cout/2 + o] + residual[o]
- * as wq_linear_matmul, in fp32 and rounded once to `type`.  Gated: Cout a multiple of 64, else UNSUPPORTED.  pre_dev (NULL: not wanted): z [rows][Cout] rounded to the type, for the backward pass.
- * y_dev may be residual_dev itself with the same stride; any other overlap of the tensors is the caller's error.  The workspace has to hold at
- * least as many rows as the call multiplies. */
+ * as wq_linear_matmul, in fp32 and rounded once to `type`.  Gated: Cout a multiple of 64, else UNSUPPORTED.
+ * pre_dev (NULL: not wanted): z [rows][Cout] rounded to the type, for the backward pass.
+ * y_dev may be residual_dev itself with the same stride; other tensors that overlap race.  The workspace has to hold at least as many rows
+ * as the call multiplies. */
 wq_status_t wq_fp8_matmul(const wq_fp8_plan_t *plan, void *stream, int rows, const void *workspace_dev, size_t workspace_bytes,
                           const void *weight_blob_dev, size_t blob_bytes, int activation, int gated, int type,
                           const void *residual_dev, int64_t residual_stride, void *pre_dev, int64_t pre_stride, void *y_dev,
@@ -517,7 +519,7 @@ wq_status_t wq_fp8_forward(const wq_fp8_plan_t *plan, void *stream, int rows, in
  *   db = sum of dz over the rows, in fp32
  * dx_dev [rows][Cin] of `type` (x's, dy's and pre's too), dw_dev [Cout][Cin] of `type` or fp32, db_dev fp32 [Cout]; each may be
  * NULL and is then not computed (x_dev is looked at for dw alone, the blob for dx alone).  accumulate 1: dw and db are added to what
- * is there, in fp32 and rounded once.  dx_dev may be x_dev or dy_dev itself (with their strides).  rows = 0: dw and db become zero unless they
+ * is there, in fp32 and rounded once.  dx_dev may be x_dev, dy_dev or pre_dev itself (with their strides).  rows = 0: dw and db become zero unless they
  * accumulate.  The results have the same bits in every call with the same arguments. */
 wq_status_t wq_fp8_backward(const wq_fp8_plan_t *plan, void *stream, int rows, int type, const void *x_dev, int64_t x_stride,
                             const void *dy_dev, int64_t dy_stride, const void *pre_dev, int64_t pre_stride,

@@ -35,6 +35,7 @@ __device__ __forceinline__ uint32_t neighbour(uint32_t v) { return (uint32_t)__b
 
 // A wave takes 16 rows x 128 columns: four lanes to a row, each with four runs of eight elements 32 apart.  Two lanes' runs make a
 // piece of 16 codes; they exchange halves so that each stores whole pieces, 16 rows of a plane side by side.
+//   bound: memory: 4096x4096 bf16 9 to 10 us (50 MB, 5.2 TB/s).
 template <int TYPE, bool WHOLE>
 __global__ __launch_bounds__(256) void k_fp8_quantize(const wq_fp8_rows_args a) {
     using T = typename Elem<TYPE>::type;
@@ -135,7 +136,7 @@ __device__ __forceinline__ void activation_slope(const float (&z)[N], int act, f
 //   ALONG: 0 no codes along the rows, 1 codes, 2 values in bf16.
 //   Two tensors in one launch: the first `blocks` workgroups take the first.
 //   bound: memory: x and dy of 4096 x 4096 bf16 into values and codes 33 us (150 MB).  Eight rows a lane and half the lanes: 35, and with
-//   a gate, whose three tensors then do not fit the registers, 42 in place of 22 (1000x1280, 2x5120 columns).
+//   a gate, whose three tensors then do not fit the registers, 42 in place of 26 (1000x1280, 2x5120 columns).
 template <int TYPE, int ALONG, bool WHOLE>
 __global__ __launch_bounds__(512, 4) void k_fp8_both(const wq_fp8_both_args first, const wq_fp8_both_args second, unsigned blocks) {
     using T = typename Elem<TYPE>::type;
@@ -286,7 +287,8 @@ __global__ __launch_bounds__(256) void k_fp8_zero(T *dw, int rows, int cols, lon
 
 // ------------------------------------------------------------ weights
 // A workgroup takes a block of 128 x 128: lanes as in k_fp8_both, the block's scale over all of them.  Codes in both orders leave
-// through LDS: 16-row blocks of eight pieces.  LOAD: w are codes already.
+// through LDS: 16-row blocks of eight pieces.  LOAD: w are codes already; a scale that is NaN makes them NaN.
+//   bound: memory: 4096x4096 bf16 with the transpose 17 us (67 MB); it runs once.
 template <int TYPE, bool LOAD>
 __global__ __launch_bounds__(256) void k_fp8_weights(const wq_fp8_weight_args a) {
     using T = typename Elem<TYPE>::type;
@@ -299,13 +301,14 @@ __global__ __launch_bounds__(256) void k_fp8_weights(const wq_fp8_weight_args a)
     uint2 codes[8];   // of a row's eight columns
     float v[8][8];
     if constexpr (LOAD) {
+        const bool nan = a.scale_type == WQ_SCALE_E8M0 && ((const uint8_t *)a.given)[blockIdx.x] == 255;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             uint32_t t[2] = {0, 0};
             const uint8_t *row = (const uint8_t *)a.w + (long)(o0 + i) * a.ws + c;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (o0 + i < a.Cout && c + j < a.Cin) t[j >> 2] |= (uint32_t)row[j] << (8 * (j & 3));
+                if (o0 + i < a.Cout && c + j < a.Cin) t[j >> 2] |= (nan ? 0x7fu : (uint32_t)row[j]) << (8 * (j & 3));
             codes[i] = make_uint2(t[0], t[1]);
         }
         if (tid == 0) {

@@ -15,6 +15,9 @@ constexpr int kSlices = 4;   // waves that share a tile's reduction (others only
 // alone.  Codes are multiplied as bf16 numbers, x's with their power of two; a multiply-add applies the weights' scale, any fp32 number.
 // FUSED: the workgroup quantizes the rows of x itself, into LDS, while its first weights are on their way: a launch less, with the
 // bits of two.
+//   bound: the latency of a wave's one round of loads below some 30 MB of weights, the memory above: 1x8192->4096 (34 MB) 9.3 us, 3.6 TB/s;
+//   16x4096->2x8192 gated (67 MB) 13.2 and 2.7 to quantize, 5.1 TB/s.  D of 6 and 8 in place of 4: 1x4096->2x8192 gated 18.2 and 20.4 us, so
+//   15.1 (their registers leave a workgroup less on a CU); 1x8192->4096 9.5, 9.4.
 template <bool GATED, int NB, bool FUSED>
 __global__ __launch_bounds__(FUSED ? 512 : 256) void k_fp8_rows(const wq_fp8_product a, const wq_fp8_rows_grid t) {
     constexpr int NE = GATED ? 2 : 1, D = 4;
@@ -178,16 +181,16 @@ __global__ __launch_bounds__(FUSED ? 512 : 256) void k_fp8_rows(const wq_fp8_pro
         const int row = tid >> 2, c = (tid & 3) * 4, p = p0 + 16 * f + row, o = ob * 16 + c;
         if (tid >= 64 || p >= a.rows || o >= a.outs) continue;
         const float *s = part_s + row * RS + c;
-        const v4f res[1] = {fp8_residual(a, p, o)};
-        v4f z[1] = {*(const v4f *)s + fp8_bias(a, o)}, up[1] = {};
-        if constexpr (GATED) up[0] = *(const v4f *)(s + 16) + fp8_bias(a, a.outs + o);
+        const v4f res = fp8_residual(a, p, o);
+        v4f z = *(const v4f *)s + fp8_bias(a, o), up = {};
+        if constexpr (GATED) up = *(const v4f *)(s + 16) + fp8_bias(a, a.outs + o);
 #pragma unroll
         for (int k = 1; k < kSlices; ++k) {
             s += 16 * RS;
-            z[0] += *(const v4f *)s;
-            if constexpr (GATED) up[0] += *(const v4f *)(s + 16);
+            z += *(const v4f *)s;
+            if constexpr (GATED) up += *(const v4f *)(s + 16);
         }
-        fp8_finish<1>(a, p, 0, o, z, up, res);
+        fp8_finish(a, p, o, z, up, res);
     }
 }
 

@@ -13,64 +13,54 @@ __device__ __forceinline__ void lds_load4(__amdgpu_buffer_rsrc_t r, char *lds, u
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, WQ_LDS_PTR(lds), 4, voff, soff, 0, 0);
 }
 
-// Until at most VM of the wave's loads are outstanding (they complete in order) and its LDS reads are done, then the
-// workgroup's barrier.
-template <int VM>
-__device__ __forceinline__ void wait_and_barrier() {
-    static_assert(VM >= 0 && VM < 64, "vmcnt is a 6-bit counter");
-    asm volatile("s_waitcnt %0\n\ts_barrier" ::"n"(0x0070 | (VM & 0xf) | ((VM >> 4) << 14)) : "memory");
-}
+// Until the wave's loads and LDS reads are done, then the workgroup's barrier.
+__device__ __forceinline__ void wait_and_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 struct wq_fp8_grid {
     int nA, nB, total, per_xcd;   // tiles along a and b, their number, the share of each XCD
 };
 
-// The epilogue of columns o .. o + 3 of rows p, p + step, .. (R of them) from their sums with the bias (gated: up, those of the other
-// half), and the residual's values.
-template <int R>
-__device__ __forceinline__ void fp8_finish(const wq_fp8_product &a, long p, int step, int o, const v4f (&zs)[R], const v4f (&up)[R],
-                                           const v4f (&res)[R]) {
+// The epilogue of columns o .. o + 3 of row p, which exists, from their sums with the bias (gated: up, those of the other half), and the
+// residual's values.
+__device__ __forceinline__ void fp8_finish(const wq_fp8_product &a, long p, int o, v4f zs, v4f up, v4f res) {
     const int n = a.outs - o;
-    float z[4 * R];
-#pragma unroll
-    for (int i = 0; i < 4 * R; ++i) z[i] = zs[i / 4][i % 4];
     if (a.pre) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            if (p + r * step >= a.rows) break;
-            store_elems(a.pre, (p + r * step) * a.ps + o, a.type, a.wide && n >= 4, n, zs[r]);
-            if (a.gated) store_elems(a.pre, (p + r * step) * a.ps + a.outs + o, a.type, a.wide && n >= 4, n, up[r]);
-        }
+        store_elems(a.pre, p * a.ps + o, a.type, a.wide && n >= 4, n, zs);
+        if (a.gated) store_elems(a.pre, p * a.ps + a.outs + o, a.type, a.wide && n >= 4, n, up);
     }
+    float z[4] = {zs.x, zs.y, zs.z, zs.w};
     activate(z, a.act);
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        v4f y = {z[4 * r], z[4 * r + 1], z[4 * r + 2], z[4 * r + 3]};
-        if (a.gated) y *= up[r];
-        if (a.res) y += res[r];
-        if (p + r * step < a.rows) store_elems(a.y, (p + r * step) * a.ys + o, a.type, a.wide && n >= 4, n, y);
-    }
+    v4f y = {z[0], z[1], z[2], z[3]};
+    if (a.gated) y *= up;
+    if (a.res) y += res;
+    store_elems(a.y, p * a.ys + o, a.type, a.wide && n >= 4, n, y);
 }
 __device__ __forceinline__ v4f fp8_residual(const wq_fp8_product &a, long p, int o) {
     const int n = a.outs - o;
-    return a.res && p < a.rows ? load_elems(a.res, p * a.rs + o, a.type, a.wide && n >= 4, n) : v4f{};
+    return a.res ? load_elems(a.res, p * a.rs + o, a.type, a.wide && n >= 4, n) : v4f{};
 }
 // (the bias is padded to whole blocks, a column's own four always lie in it)
 __device__ __forceinline__ v4f fp8_bias(const wq_fp8_product &a, int o) { return a.bias ? *(const v4f *)(a.bias + o) : v4f{}; }
 
 // WA x WB waves, each with NA x NB blocks of 16 x 16 (a's rows x b's); KS such teams share a tile's reduction, each a contiguous part of K.
-// A stage has U KiB of each 16-row block, a group's eight pieces or four of them: they go straight into LDS with the scales of the rows, in the
-// order in which lanes read them, into a ring of NST stages per team, NST - 1 of them in flight.
-template <int MODE, int NA, int NB, int WA, int WB, int KS, int U, int NST>
+// A stage has a group's 2 KiB of each 16-row block, 128 codes or 64 values of K: they go straight into LDS with the scales of the rows, in the
+// order in which lanes read them, one of a team's two stages while the other is multiplied.  A product of a group is P = sum of a b; exact
+// modes convert the codes, with their powers of two, to bf16 on the way from LDS to the matrix core (a's each by one wave column, b's once a
+// stage); any fp32 scale of a's is applied to P in a multiply-add.
+//   bound: the matrix core, at the clock that its power leaves; converting takes turns with it on a SIMD.  4096x4096->2x8192 bf16 exact 393
+//   us, 1.40 PFLOP/s (the library's bf16 product of as many numbers 1.50; the same instructions on registers alone 2.03, from LDS with the
+//   conversions 1.78); values 4096x4096->4096, of 4096 rows, 119 us (1.16); codes directly 66 us (2.08; the library's with one scale for all 2.84).
+//   tried at 4096x4096->2x8192: 8 x 8 blocks a wave and four waves 441; half stages in a ring of three or four 402, 409; a wave's priority
+//   raised around its products 395; products of 32 x 32 2 % less on registers alone.
+template <int MODE, int NA, int NB, int WA, int WB, int KS>
 __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_product a, const wq_fp8_grid t) {
     constexpr int W = WA * WB, OA = NA * WA, OB = NB * WB;   // blocks of the workgroup tile
     constexpr bool EXACT = MODE == WQ_FP8_EXACT || MODE == WQ_FP8_EXACT_FP32, ROWS = MODE == WQ_FP8_DIRECT_ROWS, VALUES = MODE == WQ_FP8_VALUES;
     constexpr bool DIRECT = !EXACT && !VALUES, MADD = MODE == WQ_FP8_EXACT_FP32 || MODE == WQ_FP8_DIRECT_FP32;
-    static_assert(U == 2 || (U == 1 && !DIRECT), "the direct product takes a whole group");
     constexpr int QB = VALUES ? 0 : (OB + 3) / 4, QA = ROWS ? (OA + 3) / 4 : VALUES ? 0 : 1;   // loads of scales, 64 of one group each
-    constexpr int BOFF = OA * U * 1024, SBOFF = BOFF + OB * U * 1024, SAOFF = SBOFF + QB * 256, STAGE = SAOFF + QA * 256;
+    constexpr int BOFF = OA * 2048, SBOFF = BOFF + OB * 2048, SAOFF = SBOFF + QB * 256, STAGE = SAOFF + QA * 256;
     constexpr int RS = 16 * NA + 4, PART = 16 * RS;   // epilogue: floats of a row and of a wave's 16 rows
-    constexpr int BYTES = NST * STAGE > W * PART * 4 ? NST * STAGE : W * PART * 4;
+    constexpr int BYTES = 2 * STAGE > W * PART * 4 ? 2 * STAGE : W * PART * 4;
     __shared__ __attribute__((aligned(16))) char lds[KS * BYTES];
 
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, q = lane >> 4;
@@ -82,7 +72,7 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
     const int band = logical / (8 * t.nA), in_band = logical - band * 8 * t.nA, high = min(8, t.nB - band * 8);
     const int pa = in_band / high, pb = band * 8 + in_band % high;
     // the team's stages; all teams make the same number of turns
-    constexpr int PER = VALUES ? 4 / U : 2 / U;   // stages of 128 of K
+    constexpr int PER = VALUES ? 2 : 1;   // stages of 128 of K
     const int s_beg = team * a.groups / KS * PER, s_end = (team + 1) * a.groups / KS * PER, turns = (a.groups + KS - 1) / KS * PER;
     char *const stages = lds + team * BYTES;
 
@@ -98,25 +88,23 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
     const __amdgpu_buffer_rsrc_t rB = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.b.data), 0, (int)a.b.bytes, kBufFlags);
 
     // ---- the loader ---- (rows past the end read the last one again, whose sums are not stored)
-    constexpr int LA = OA * U / W, LB = OB * U / W;   // loads of 1 KiB of a wave: half a group of a block each
-    static_assert(LA * W == OA * U && LB * W == OB * U, "the waves share the loads evenly");
+    constexpr int LA = OA * 2 / W, LB = OB * 2 / W;   // loads of 1 KiB of a wave: half a group of a block each
+    static_assert(LA * W == OA * 2 && LB * W == OB * 2, "the waves share the loads evenly");
     unsigned vA[LA], vB[LB];
     auto place = [&](const wq_fp8_operand &o, int row, int u) {
         const int r = min(row + l16, o.rows - 1);
         return (unsigned)(r >> 4) * o.block + ((unsigned)u * 4u + q) * o.piece + (unsigned)(r & 15) * 16u;
     };
 #pragma unroll
-    for (int u = 0; u < LA; ++u) vA[u] = place(a.a, row_of((wave * LA + u) / U), (wave * LA + u) % U);
+    for (int u = 0; u < LA; ++u) vA[u] = place(a.a, row_of((wave * LA + u) / 2), (wave * LA + u) % 2);
 #pragma unroll
-    for (int u = 0; u < LB; ++u) vB[u] = place(a.b, b0 + (wave * LB + u) / U * 16, (wave * LB + u) % U);
+    for (int u = 0; u < LB; ++u) vB[u] = place(a.b, b0 + (wave * LB + u) / 2 * 16, (wave * LB + u) % 2);
     // loads of scales, b's and then a's, are dealt to the waves in turn (a wave without one of its own repeats another's)
     const unsigned vSA = (unsigned)(min(row_of(min(lane, OA - 1)), a.a.rows - 1) >> 7) * (unsigned)a.a.scale_step * 4u;
-    constexpr int NS = QA + QB, LS = (NS + W - 1) / W, LPS = LA + LB + LS;
-    auto issue = [&](int s, int slot) {
+    constexpr int NS = QA + QB, LS = (NS + W - 1) / W;
+    auto issue = [&](int g, int slot) {   // the g-th group, of 128 codes or 64 values
         char *const to = stages + slot * STAGE;
-        const int g = U == 2 ? s : s >> 1;   // the group, of 128 codes or 64 values
-        const unsigned half = U == 1 ? (unsigned)(s & 1) * 4u : 0u;
-        const unsigned oA = (unsigned)g * a.a.group + half * a.a.piece, oB = (unsigned)g * a.b.group + half * a.b.piece;
+        const unsigned oA = (unsigned)g * a.a.group, oB = (unsigned)g * a.b.group;
 #pragma unroll
         for (int u = 0; u < LA; ++u) lds_load16(rA, to + (wave * LA + u) * 1024, vA[u], oA);
 #pragma unroll
@@ -148,9 +136,9 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
 #pragma unroll
         for (int f = 0; f < NB; ++f) M[e][f] = v4f{0.f, 0.f, 0.f, 0.f};
 
-    const char *const atA = stages + wa * NA * U * 1024 + lane * 16, *const atB = stages + BOFF + wb * NB * U * 1024 + lane * 16;
+    const char *const atA = stages + wa * NA * 2048 + lane * 16, *const atB = stages + BOFF + wb * NB * 2048 + lane * 16;
     const char *const atSB = stages + SBOFF + wb * NB * 64 + l16 * 4, *const atSA = stages + SAOFF + (ROWS ? wa * NA * 64 + l16 * 4 : wa * NA * 4);
-    auto compute = [&](int s, int slot) {
+    auto compute = [&](int slot) {
         const char *const pA = atA + slot * STAGE, *const pB = atB + slot * STAGE;
         float sa[NA];
         if constexpr (!VALUES) {
@@ -190,10 +178,10 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
 #pragma unroll
                 for (int f = 0; f < NB; ++f) sb[f] = *(const float *)(atSB + slot * STAGE + f * 64);
             }
-            constexpr int NK = VALUES ? U : 2 * U;   // products of 32 of K
+            constexpr int NK = VALUES ? 2 : 4;   // products of 32 of K
             auto read = [&](const char *p, float scale, v8bf (&v)[NK]) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
+                for (int u = 0; u < 2; ++u) {
                     const v4i c = *(const v4i *)(p + u * 1024);
                     if constexpr (VALUES) {
                         v[u] = __builtin_bit_cast(v8bf, c);
@@ -205,11 +193,11 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
             };
             v8bf bv[NB][NK];
 #pragma unroll
-            for (int f = 0; f < NB; ++f) read(pB + f * U * 1024, sb[f], bv[f]);
+            for (int f = 0; f < NB; ++f) read(pB + f * 2048, sb[f], bv[f]);
 #pragma unroll
             for (int e = 0; e < NA; ++e) {
                 v8bf av[NK];
-                read(pA + e * U * 1024, MADD || VALUES ? 1.0f : sa[e], av);
+                read(pA + e * 2048, MADD || VALUES ? 1.0f : sa[e], av);
                 v4f P[NB];
 #pragma unroll
                 for (int f = 0; f < NB; ++f) P[f] = MADD ? v4f{0.f, 0.f, 0.f, 0.f} : M[e][f];
@@ -230,19 +218,16 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
         }
     };
 
+    if (s_beg < s_end) issue(s_beg, 0);
+    for (int i = 0; i < turns; i += 2) {
 #pragma unroll
-    for (int d = 0; d < NST - 1; ++d)
-        if (s_beg + d < s_end) issue(s_beg + d, d);
-    for (int i = 0; i < turns; i += NST) {
-#pragma unroll
-        for (int slot = 0; slot < NST; ++slot) {   // (a constant: so are the addresses in LDS)
+        for (int slot = 0; slot < 2; ++slot) {   // (a constant: so are the addresses in LDS)
             if (i + slot >= turns) break;
             const int s = s_beg + i + slot;
             // the stage's loads have landed, every wave's, and the slot of the stage before has been read by all
-            if (NST > 2 && s + NST - 1 <= s_end) wait_and_barrier<(NST - 2) * LPS>();
-            else wait_and_barrier<0>();
-            if (s + NST - 1 < s_end) issue(s + NST - 1, (slot + NST - 1) % NST);
-            if (s < s_end) compute(s, slot);
+            wait_and_barrier();
+            if (s + 1 < s_end) issue(s + 1, slot ^ 1);
+            if (s < s_end) compute(slot);
         }
     }
 
@@ -269,23 +254,23 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
             for (int row = (team * 64 + lane) >> shift; row < 16; row += row_step * KS) {   // (the teams share the rows)
                 const int p = b0 + (wb * NB + f) * 16 + row;
                 if (p >= a.rows) break;
-                const v4f res[1] = {fp8_residual(a, p, o)};
+                const v4f res = fp8_residual(a, p, o);
                 const float *sums = (const float *)lds + wave * PART + row * RS + c;
-                v4f z[1] = {bias + *(const v4f *)sums}, up[1] = {};
-                if (a.gated) up[0] = bias_up + *(const v4f *)(sums + 8 * NA);
+                v4f z = bias + *(const v4f *)sums, up = {};
+                if (a.gated) up = bias_up + *(const v4f *)(sums + 8 * NA);
 #pragma unroll
                 for (int k = 1; k < KS; ++k) {
-                    z[0] += *(const v4f *)(sums + k * (BYTES / 4));
-                    if (a.gated) up[0] += *(const v4f *)(sums + k * (BYTES / 4) + 8 * NA);
+                    z += *(const v4f *)(sums + k * (BYTES / 4));
+                    if (a.gated) up += *(const v4f *)(sums + k * (BYTES / 4) + 8 * NA);
                 }
-                fp8_finish<1>(a, p, 0, o, z, up, res);
+                fp8_finish(a, p, o, z, up, res);
             }
         }
         __builtin_amdgcn_wave_barrier();
     }
 }
 
-template <int MODE, int NA, int NB, int WA, int WB, int KS, int U, int NST>
+template <int MODE, int NA, int NB, int WA, int WB, int KS>
 hipError_t launch_fp8_tile(const wq_fp8_product &a, hipStream_t s) {
     wq_fp8_grid t;
     const int across = a.gated ? 8 * NA * WA : 16 * NA * WA;   // columns of y in a tile
@@ -293,19 +278,19 @@ hipError_t launch_fp8_tile(const wq_fp8_product &a, hipStream_t s) {
     t.nB = (a.rows + 16 * NB * WB - 1) / (16 * NB * WB);
     t.total = t.nA * t.nB;
     t.per_xcd = (t.total + 7) / 8;
-    hipLaunchKernelGGL((k_fp8_tile<MODE, NA, NB, WA, WB, KS, U, NST>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * WA * WB * KS), 0, s, a, t);
+    hipLaunchKernelGGL((k_fp8_tile<MODE, NA, NB, WA, WB, KS>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * WA * WB * KS), 0, s, a, t);
     return hipGetLastError();
 }
 
 template <int MODE>
 hipError_t launch_fp8_form(const wq_fp8_product &a, int form, hipStream_t s) {
     switch (form) {
-        case WQ_FP8_TILE_256: return launch_fp8_tile<MODE, 8, 4, 2, 4, 1, 2, 2>(a, s);
-        case WQ_FP8_TILE_128: return launch_fp8_tile<MODE, 4, 4, 2, 2, 1, 2, 2>(a, s);
-        case WQ_FP8_TILE_128x64: return launch_fp8_tile<MODE, 4, 2, 2, 2, 1, 2, 2>(a, s);
-        case WQ_FP8_TILE_64: return launch_fp8_tile<MODE, 2, 2, 2, 2, 1, 2, 2>(a, s);
-        case WQ_FP8_TILE_64_2: return launch_fp8_tile<MODE, 2, 2, 2, 2, 2, 2, 2>(a, s);
-        default: return launch_fp8_tile<MODE, 2, 2, 2, 2, 4, 2, 2>(a, s);
+        case WQ_FP8_TILE_256: return launch_fp8_tile<MODE, 8, 4, 2, 4, 1>(a, s);
+        case WQ_FP8_TILE_128: return launch_fp8_tile<MODE, 4, 4, 2, 2, 1>(a, s);
+        case WQ_FP8_TILE_128x64: return launch_fp8_tile<MODE, 4, 2, 2, 2, 1>(a, s);
+        case WQ_FP8_TILE_64: return launch_fp8_tile<MODE, 2, 2, 2, 2, 1>(a, s);
+        case WQ_FP8_TILE_64_2: return launch_fp8_tile<MODE, 2, 2, 2, 2, 2>(a, s);
+        default: return launch_fp8_tile<MODE, 2, 2, 2, 2, 4>(a, s);
     }
 }
 

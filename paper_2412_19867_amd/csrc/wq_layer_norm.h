@@ -34,7 +34,7 @@ __device__ __forceinline__ norm_stats stats_of(double sum, double squares, int C
 
 // Elements c .. c + 7 of a row of `cols`, zero behind its end and (live false) everywhere; rows lie anywhere, elements are aligned to
 // themselves.  Nothing branches on a lane: registers that one branch loads and another one fills would make each load wait for the
-// one before (the gradient's two readings of 4096 rows of 8192 fp32 102 us so, 89 without).  A lane at the end reads the row's last eight
+// one before (the gradient of 4096 rows of 8192 fp32 102 us so, 98 without).  A lane at the end reads the row's last eight
 // and shifts them.  WHOLE: rows of whole eights.
 template <typename T, bool WHOLE>
 __device__ __forceinline__ void load8_row(const T *row, int c, int cols, bool live, float (&v)[8]) {

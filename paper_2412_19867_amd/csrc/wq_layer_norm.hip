@@ -13,6 +13,8 @@ namespace {
 
 // Rows in pieces of eight elements a lane, held in registers: one pass over the data.  `wpr` waves share a row of up to 512 V wpr
 // elements.
+//   bound: the memory for many rows, below some 30 MB the launch and one round of loads: 777x5120 fp16 with a residual into codes and the sum
+//   9.3 to 10.4 us (28 MB, 2.9 TB/s); 1x4096 bf16 4 us.
 template <int TYPE, bool CODES, int V, bool WHOLE>
 __global__ __launch_bounds__(512) void k_layer_norm(const wq_layer_norm_args a, int wpr, unsigned run) {
     using T = typename Elem<TYPE>::type;
@@ -69,7 +71,7 @@ __global__ __launch_bounds__(512) void k_layer_norm(const wq_layer_norm_args a, 
         const int c = c0 + k * step, n = a.C - c;
         if (a.sum && live && n > 0) store8_some<T>((T *)a.sum + p * a.ss + c, n, v[k]);
         // (gamma and beta come from the L2, which all rows ask for the same lines: asked for with x, ahead of the sums, they hold up x
-        // itself, 777x5120 fp16 13.5 us in place of 9.3)
+        // itself, 777x5120 fp16 13.5 us in place of 10.4)
         float y[8], gm[8], bt[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) gm[j] = 1.0f, bt[j] = 0.0f;
@@ -152,7 +154,7 @@ __global__ __launch_bounds__(256) void k_layer_norm_long(const wq_layer_norm_arg
 }
 
 // Pieces of 512 elements of a row over waves: as few pieces a lane as eight waves allow, and no more waves than hold them
-// (5120 columns: five waves with two pieces; eight, some with one, 12.0 us in place of 9.9 at 777 rows).
+// (5120 columns: five waves with two pieces; eight, some with one, 12.2 us in place of 9.3 at 777 rows).
 struct row_form {
     int V, wpr, upw;   // pieces a lane, waves to a row, rows of a workgroup
 };
@@ -190,6 +192,8 @@ void launch_norm(const wq_layer_norm_args &a, hipStream_t s) {
 // ------------------------------------------------------------ gradient
 // A workgroup's units of `wpr` waves take every units-th row; the weight's and bias's gradients of a unit's rows add up in its lanes'
 // registers and leave as one row of partial sums.
+//   bound: memory and the loads in flight: 4096x8192 fp32 98 us (403 MB, 4.1 TB/s; a large copy's 5.06 would be 80), 6.9 more for the columns.
+//   What the registers hold leaves two workgroups a CU; while one adds up a row's sums the other loads.
 template <int TYPE, int V, bool WHOLE>
 __global__ __launch_bounds__(512, V <= 2 ? 4 : 2) void k_layer_norm_grad(const wq_layer_norm_grad_args a, int wpr, int units) {
     using T = typename Elem<TYPE>::type;

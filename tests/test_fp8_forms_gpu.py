@@ -246,3 +246,25 @@ def test_calls_of_other_numbers_of_rows(wq):
         assert bool(part[rows - 5:].isnan().all())
         X = quantized(x[:rows - 5].float(), 1)
         check(part[:rows - 5], X @ w.t() + bias, X.abs() @ w.abs().t() + bias.abs(), 500, False)
+
+
+def test_a_nan_scale_makes_its_block_nan(wq):
+    """e8m0 byte 255, in a plan of either kind, forward and backward; the other blocks' columns are what they were."""
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    codes = torch.randn((300, 200), generator=gen, device="cuda").to(torch.float8_e4m3fn)
+    e = torch.full((3, 2), 127, dtype=torch.uint8, device="cuda")
+    x, dy = rows_of(gen, 5, 200).bfloat16(), rows_of(gen, 5, 300).bfloat16()
+    for any_scales in (False, True):
+        plan = wq.Fp8LinearPlan(5, 200, 300, backward=True, fp32_scales=any_scales)
+        blob, ws = plan.alloc_blob(), plan.alloc_workspace()
+        got = []
+        for byte in (127, 255):
+            e[1, 0] = byte
+            plan.weight_load(codes, e.view(torch.float8_e8m0fnu), None, blob)
+            y, dx = torch.empty((5, 300), device="cuda", dtype=x.dtype), torch.empty_like(x)
+            plan.linear(x, blob, ws, y)
+            plan.backward(None, dy, blob, ws, dx=dx)
+            got.append((y, dx))
+        (y, dx), (yn, dxn) = got
+        assert bool(yn[:, 128:256].isnan().all()) and torch.equal(yn[:, :128], y[:, :128]) and torch.equal(yn[:, 256:], y[:, 256:])
+        assert bool(dxn[:, :128].isnan().all()) and torch.equal(dxn[:, 128:], dx[:, 128:])
