@@ -13,8 +13,8 @@ namespace {
 
 // Rows in pieces of eight elements a lane, held in registers: one pass over the data.  `wpr` waves share a row of up to 512 V wpr
 // elements.
-//   bound: the memory for many rows, below some 30 MB the launch and one round of loads: 777x5120 fp16 with a residual into codes and the sum
-//   9.3 to 10.4 us (28 MB, 2.9 TB/s); 1x4096 bf16 4 us.
+//   bound: the memory for many rows, below some 30 MB the launch and one round of loads: 777x5120 fp16 into codes 9.3 to 10.4 us (12 MB), 1x4096
+//   bf16 4.
 template <int TYPE, bool CODES, int V, bool WHOLE>
 __global__ __launch_bounds__(512) void k_layer_norm(const wq_layer_norm_args a, int wpr, unsigned run) {
     using T = typename Elem<TYPE>::type;
