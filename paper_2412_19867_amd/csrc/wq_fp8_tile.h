@@ -51,7 +51,7 @@ __device__ __forceinline__ v4f fp8_bias(const wq_fp8_product &a, int o) { return
 //   us, 1.40 PFLOP/s (the library's bf16 product of as many numbers 1.50; the same instructions on registers alone 2.03, from LDS with the
 //   conversions 1.78); values 4096x4096->4096, of 4096 rows, 119 us (1.16); codes directly 66 us (2.08; the library's with one scale for all 2.84).
 //   tried at 4096x4096->2x8192: 8 x 8 blocks a wave and four waves 441; half stages in a ring of three or four 402, 409; a wave's priority
-//   raised around its products 395; products of 32 x 32 2 % less on registers alone.
+//   raised around its products 395; products of 32 x 32, on registers alone 12 % slower.
 template <int MODE, int NA, int NB, int WA, int WB, int KS>
 __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_product a, const wq_fp8_grid t) {
     constexpr int W = WA * WB, OA = NA * WA, OB = NB * WB;   // blocks of the workgroup tile
