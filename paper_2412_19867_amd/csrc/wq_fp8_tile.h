@@ -13,8 +13,13 @@ __device__ __forceinline__ void lds_load4(__amdgpu_buffer_rsrc_t r, char *lds, u
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, WQ_LDS_PTR(lds), 4, voff, soff, 0, 0);
 }
 
-// Until the wave's loads and LDS reads are done, then the workgroup's barrier.
-__device__ __forceinline__ void wait_and_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// Until at most VM of the wave's loads are outstanding (they complete in order) and its LDS reads are done, then the workgroup's
+// barrier.
+template <int VM>
+__device__ __forceinline__ void wait_and_barrier() {
+    static_assert(VM >= 0 && VM < 64, "vmcnt is a 6-bit counter");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(VM) : "memory");
+}
 
 struct wq_fp8_grid {
     int nA, nB, total, per_xcd;   // tiles along a and b, their number, the share of each XCD
@@ -44,7 +49,7 @@ __device__ __forceinline__ v4f fp8_bias(const wq_fp8_product &a, int o) { return
 
 // WA x WB waves, each with NA x NB blocks of 16 x 16 (a's rows x b's); KS such teams share a tile's reduction, each a contiguous part of K.
 // A stage has a group's 2 KiB of each 16-row block, 128 codes or 64 values of K: they go straight into LDS with the scales of the rows, in the
-// order in which lanes read them, one of a team's two stages while the other is multiplied.  A product of a group is P = sum of a b; exact
+// order in which lanes read them, all but one of a team's NST stages while that is multiplied.  A product of a group is P = sum of a b; exact
 // modes convert the codes, with their powers of two, to bf16 on the way from LDS to the matrix core (a's each by one wave column, b's once a
 // stage); any fp32 scale of a's is applied to P in a multiply-add.
 //   bound: the matrix core, at the clock that its power leaves; converting takes turns with it on a SIMD.  4096x4096->2x8192 bf16 exact 393
@@ -52,7 +57,7 @@ __device__ __forceinline__ v4f fp8_bias(const wq_fp8_product &a, int o) { return
 //   conversions 1.78); values 4096x4096->4096, of 4096 rows, 119 us (1.16); codes directly 66 us (2.08; the library's with one scale for all 2.84).
 //   tried at 4096x4096->2x8192: 8 x 8 blocks a wave and four waves 441; half stages in a ring of three or four 402, 409; a wave's priority
 //   raised around its products 395; products of 32 x 32, on registers alone 12 % slower.
-template <int MODE, int NA, int NB, int WA, int WB, int KS>
+template <int MODE, int NA, int NB, int WA, int WB, int KS, int NST>
 __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_product a, const wq_fp8_grid t) {
     constexpr int W = WA * WB, OA = NA * WA, OB = NB * WB;   // blocks of the workgroup tile
     constexpr bool EXACT = MODE == WQ_FP8_EXACT || MODE == WQ_FP8_EXACT_FP32, ROWS = MODE == WQ_FP8_DIRECT_ROWS, VALUES = MODE == WQ_FP8_VALUES;
@@ -60,7 +65,7 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
     constexpr int QB = VALUES ? 0 : (OB + 3) / 4, QA = ROWS ? (OA + 3) / 4 : VALUES ? 0 : 1;   // loads of scales, 64 of one group each
     constexpr int BOFF = OA * 2048, SBOFF = BOFF + OB * 2048, SAOFF = SBOFF + QB * 256, STAGE = SAOFF + QA * 256;
     constexpr int RS = 16 * NA + 4, PART = 16 * RS;   // epilogue: floats of a row and of a wave's 16 rows
-    constexpr int BYTES = 2 * STAGE > W * PART * 4 ? 2 * STAGE : W * PART * 4;
+    constexpr int BYTES = NST * STAGE > W * PART * 4 ? NST * STAGE : W * PART * 4;
     __shared__ __attribute__((aligned(16))) char lds[KS * BYTES];
 
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, q = lane >> 4;
@@ -101,7 +106,7 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
     for (int u = 0; u < LB; ++u) vB[u] = place(a.b, b0 + (wave * LB + u) / 2 * 16, (wave * LB + u) % 2);
     // loads of scales, b's and then a's, are dealt to the waves in turn (a wave without one of its own repeats another's)
     const unsigned vSA = (unsigned)(min(row_of(min(lane, OA - 1)), a.a.rows - 1) >> 7) * (unsigned)a.a.scale_step * 4u;
-    constexpr int NS = QA + QB, LS = (NS + W - 1) / W;
+    constexpr int NS = QA + QB, LS = (NS + W - 1) / W, LPS = LA + LB + LS;
     auto issue = [&](int g, int slot) {   // the g-th group, of 128 codes or 64 values
         char *const to = stages + slot * STAGE;
         const unsigned oA = (unsigned)g * a.a.group, oB = (unsigned)g * a.b.group;
@@ -218,15 +223,18 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
         }
     };
 
-    if (s_beg < s_end) issue(s_beg, 0);
-    for (int i = 0; i < turns; i += 2) {
 #pragma unroll
-        for (int slot = 0; slot < 2; ++slot) {   // (a constant: so are the addresses in LDS)
+    for (int d = 0; d < NST - 1; ++d)
+        if (s_beg + d < s_end) issue(s_beg + d, d);
+    for (int i = 0; i < turns; i += NST) {
+#pragma unroll
+        for (int slot = 0; slot < NST; ++slot) {   // (a constant: so are the addresses in LDS)
             if (i + slot >= turns) break;
             const int s = s_beg + i + slot;
             // the stage's loads have landed, every wave's, and the slot of the stage before has been read by all
-            wait_and_barrier();
-            if (s + 1 < s_end) issue(s + 1, slot ^ 1);
+            if (NST > 2 && s + NST - 1 <= s_end) wait_and_barrier<(NST - 2) * LPS>();
+            else wait_and_barrier<0>();
+            if (s + NST - 1 < s_end) issue(s + NST - 1, (slot + NST - 1) % NST);
             if (s < s_end) compute(slot);
         }
     }
@@ -270,7 +278,7 @@ __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_
     }
 }
 
-template <int MODE, int NA, int NB, int WA, int WB, int KS>
+template <int MODE, int NA, int NB, int WA, int WB, int KS, int NST>
 hipError_t launch_fp8_tile(const wq_fp8_product &a, hipStream_t s) {
     wq_fp8_grid t;
     const int across = a.gated ? 8 * NA * WA : 16 * NA * WA;   // columns of y in a tile
@@ -278,19 +286,22 @@ hipError_t launch_fp8_tile(const wq_fp8_product &a, hipStream_t s) {
     t.nB = (a.rows + 16 * NB * WB - 1) / (16 * NB * WB);
     t.total = t.nA * t.nB;
     t.per_xcd = (t.total + 7) / 8;
-    hipLaunchKernelGGL((k_fp8_tile<MODE, NA, NB, WA, WB, KS>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * WA * WB * KS), 0, s, a, t);
+    hipLaunchKernelGGL((k_fp8_tile<MODE, NA, NB, WA, WB, KS, NST>), dim3((unsigned)t.per_xcd * 8u), dim3(64 * WA * WB * KS), 0, s, a, t);
     return hipGetLastError();
 }
 
 template <int MODE>
 hipError_t launch_fp8_form(const wq_fp8_product &a, int form, hipStream_t s) {
     switch (form) {
-        case WQ_FP8_TILE_256: return launch_fp8_tile<MODE, 8, 4, 2, 4, 1>(a, s);
-        case WQ_FP8_TILE_128: return launch_fp8_tile<MODE, 4, 4, 2, 2, 1>(a, s);
-        case WQ_FP8_TILE_128x64: return launch_fp8_tile<MODE, 4, 2, 2, 2, 1>(a, s);
-        case WQ_FP8_TILE_64: return launch_fp8_tile<MODE, 2, 2, 2, 2, 1>(a, s);
-        case WQ_FP8_TILE_64_2: return launch_fp8_tile<MODE, 2, 2, 2, 2, 2>(a, s);
-        default: return launch_fp8_tile<MODE, 2, 2, 2, 2, 4>(a, s);
+        case WQ_FP8_TILE_256: return launch_fp8_tile<MODE, 8, 4, 2, 4, 1, 2>(a, s);
+        case WQ_FP8_TILE_128: return launch_fp8_tile<MODE, 4, 4, 2, 2, 1, 2>(a, s);
+        case WQ_FP8_TILE_128x64: return launch_fp8_tile<MODE, 4, 2, 2, 2, 1, 2>(a, s);
+        case WQ_FP8_TILE_64: return launch_fp8_tile<MODE, 2, 2, 2, 2, 1, 2>(a, s);
+        case WQ_FP8_TILE_64_2: return launch_fp8_tile<MODE, 2, 2, 2, 2, 2, 2>(a, s);
+        case WQ_FP8_TILE_64_2_3: return launch_fp8_tile<MODE, 2, 2, 2, 2, 2, 3>(a, s);
+        default:
+            if constexpr (MODE == WQ_FP8_EXACT || MODE == WQ_FP8_EXACT_FP32) return launch_fp8_tile<MODE, 2, 2, 2, 2, 4, 2>(a, s);
+            return hipErrorInvalidValue;   // (the rules give it to no other)
     }
 }
 
