@@ -10,7 +10,8 @@ enum wq_fp8_tile_form {
     WQ_FP8_TILE_64 = 3,
     WQ_FP8_TILE_64_2 = 4,   // two teams
     WQ_FP8_TILE_64_4 = 5,   // four (exact sums only)
-    WQ_FP8_TILE_64_2_3 = 6  // two teams whose stages are a ring of three, a workgroup a CU
+    WQ_FP8_TILE_64_2_3 = 6, // two teams whose stages are a ring of three, a workgroup a CU
+    WQ_FP8_TILE_128_2 = 7   // 128, two teams, a workgroup a CU
 };
 
 struct wq_fp8_form {
@@ -21,19 +22,24 @@ struct wq_fp8_form {
 inline long wq_fp8_tiles(int outs, int rows, int across, int down) {
     return (long)((outs + across - 1) / across) * ((rows + down - 1) / down);
 }
+// Whether tiles of 128 x 128, two to a CU, fill their last round of 512 well.
+inline bool wq_fp8_full(long n128) { return (n128 + 511) / 512 * 512 <= 1.32 * n128; }
 
 // y [rows][outs] from K in `groups` groups of 128; gated: outs columns from twice as many weight rows, so tiles are half as wide.
-// exact: bf16 sums, else codes (half the time in the matrix core).  Fitted on 282 layers of 33 to 8192 rows; us on either side of each line, rows
-// x K -> columns:
+// exact: bf16 sums, else codes (half the time in the matrix core).  Over 239 drawn layers of 33 to 8192 rows 0.6 %
+// (geometric mean) above the best form, 23 % at most; us on either side of each line, rows x K -> columns, or the number of tiles:
 //   rows: up to 128 of them while there are at most 900 blocks of 16 x 16 (64x6592->1728 7.4, tiles 18.0; 80x1792->2048 6.5, 8.7;
 //     52x7744->9152, 2288 blocks: 27.8, 20.7); one block of rows a workgroup up to 16 rows or 256 blocks, else two
 //   256: reductions from 2048 on where the last round of 256 of them wastes less than they gain over 128 (a fifth):
 //     4096x4096->2x8192 393, 443; 2472x4608->2x2912 104, 121; 1000x1280->2x5120 38.5, 35
-//   128: the same from 448 of them (512x4096->2x8192, 512: 59, of 128x64 66; 772x3904->2x3616, 399: 58, 49)
-//   128x64 from 384, 64 x 64 from 512, two teams above 256 tiles of 64, one to a CU and more (374, K 7296: 34.2, with a ring of three 41.5).  One
-//   to a CU or less: a CU has no more of the memory's latency to hide than its own teams ask for, so they ask for two stages ahead (75 tiles, K
-//   10240, not exact: 24.9, two stages 30.5, four teams 26.9); four teams for exact sums of K from 2048 on, whose conversions they share (120, K
-//   7808: 20.2, the ring 23.3; 145, K 2176: 9.7, 9.5)
+//   128: where the card holds 512 of them and the last round is full (450 tiles, K 5632: 84, 128x64 94; 576, K 3328: 101, 91), not exact
+//     also above 256 of long reductions (344, K 10240: 77, 82); one to a CU of long reductions with two teams (1024x8192->4096 58, 128x64 69;
+//     220, K 1536: 17.2, 64 x 64 14.9)
+//   128x64 from 384, short reductions of few tiles excepted (287 of 128, K 1536: 25.0, 64 x 64 22.9; 365, K 5376: 65, 70)
+//   64 x 64 above 512 and for the shortest (336, K 640: 7.3, two teams 7.6), two teams above 256, two to a CU (374, K 7296: 34.2, with a ring of
+//   three 41.5).  One to a CU or less: a CU has no more of the memory's latency to hide than its own teams ask for, so they ask for two
+//   stages ahead (75 tiles, K 10240, not exact: 24.9, two stages 30.5, four teams 26.9); four teams for exact sums of K from 2048 on, whose
+//   conversions they share (120, K 7808: 20.2, the ring 23.3; 145, K 2176: 9.7, 9.5)
 // (K in slices of several workgroups and a kernel that joins them was better for 7 of 90 layers, narrow ones of few rows: 139x10240->320
 // 27 us, so 18.)
 inline wq_fp8_form wq_fp8_choose_form(int rows, int outs, bool gated, int groups, bool exact) {
@@ -43,22 +49,25 @@ inline wq_fp8_form wq_fp8_choose_form(int rows, int outs, bool gated, int groups
     const long n256 = wq_fp8_tiles(outs, rows, 256 / half, 256), n128 = wq_fp8_tiles(outs, rows, 128 / half, 128);
     const long n64 = wq_fp8_tiles(outs, rows, 64 / half, 64);
     if (groups >= 16 && (n256 + 255) / 256 * 256 <= 0.3 * n128) return {0, WQ_FP8_TILE_256};
-    if (groups >= 16 && n128 >= 448) return {0, WQ_FP8_TILE_128};
-    if (wq_fp8_tiles(outs, rows, 128 / half, 64) >= 384) return {0, WQ_FP8_TILE_128x64};
-    if (n64 > 256) return {0, n64 >= 512 ? WQ_FP8_TILE_64 : WQ_FP8_TILE_64_2};
+    if (groups >= 9 && wq_fp8_full(n128)) return {0, WQ_FP8_TILE_128};
+    if (!exact && groups >= 28 && n128 > 256 && n128 <= 512) return {0, WQ_FP8_TILE_128};
+    if (n128 > 200 && n128 <= 256 && groups >= (exact ? 16 : 40)) return {0, WQ_FP8_TILE_128_2};
+    if (wq_fp8_tiles(outs, rows, 128 / half, 64) >= 384 && (n128 > 640 || groups >= (exact ? 18 : 10))) return {0, WQ_FP8_TILE_128x64};
+    if (n64 > 256) return {0, n64 > 512 || groups < 7 ? WQ_FP8_TILE_64 : WQ_FP8_TILE_64_2};
     return {0, exact && groups >= 16 ? WQ_FP8_TILE_64_4 : WQ_FP8_TILE_64_2_3};
 }
 
-// dw [Cout][Cin] from groups of 128 rows.  Fitted on 145 layers; us on either side of each line, rows x Cin -> Cout, with the quantization (20
-// to 40 of it): 256: 4096x4096->4096 136, of 128 150; 941x1728->8192 64, 69;  128x64 over 128 below 512 of the latter: 3033x2624->1792
-// fp32 59, 63;  64 from 512 tiles: 1716x2944->1024 23.6, two teams 27.1;  two teams: 3280x640->2688 25.7, one 28.2;  a ring of three up to 256 tiles: 196,
-// of 3700 rows, fp32 27.3, two stages 34.6, four teams 31.2.
+// dw [Cout][Cin] from groups of 128 rows.  Over 120 drawn layers 0.7 % above the best form, 18 % at most; us on either side of each line, rows x
+// Cin -> Cout or the number of tiles, with the quantization (20 to 40 of it):
+//   256: 4096x4096->4096 136, of 128 150; 941x1728->8192 64, 69;  128 where it fills its rounds: 408 tiles, of 3045 rows, 66.9, 128x64 80.6;
+//   128x64 above 220 of 128: 342, of 1135 rows, 25.9, 128 28.6, 64 x 64 26.8;  64 x 64 above 512: 1716x2944->1024 23.6, two teams 27.1;  two teams
+//   above 256: 3280x640->2688 25.7, one 28.2;  a ring of three below: 196, of 3700 rows, fp32 27.3, two stages 34.6, four teams 31.2.
 inline wq_fp8_form wq_fp8_choose_grad_form(int Cout, int Cin, int groups) {
     const long n256 = wq_fp8_tiles(Cin, Cout, 256, 256), n128 = wq_fp8_tiles(Cin, Cout, 128, 128), n64 = wq_fp8_tiles(Cin, Cout, 64, 64);
     if (groups >= 7 && (n256 + 255) / 256 * 256 <= 0.3 * n128) return {0, WQ_FP8_TILE_256};
-    if (groups >= 7 && n128 >= 512) return {0, WQ_FP8_TILE_128};
-    if (wq_fp8_tiles(Cin, Cout, 128, 64) >= 440) return {0, WQ_FP8_TILE_128x64};
-    return {0, n64 >= 512 ? WQ_FP8_TILE_64 : n64 > 256 ? WQ_FP8_TILE_64_2 : WQ_FP8_TILE_64_2_3};
+    if (groups >= 9 && wq_fp8_full(n128)) return {0, WQ_FP8_TILE_128};
+    if (wq_fp8_tiles(Cin, Cout, 128, 64) >= 440 && !(groups < 9 && n128 <= 512 && wq_fp8_full(n128))) return {0, WQ_FP8_TILE_128x64};
+    return {0, n64 > 512 ? WQ_FP8_TILE_64 : n64 > 256 ? WQ_FP8_TILE_64_2 : WQ_FP8_TILE_64_2_3};
 }
 
 // Whether the product for few rows may take rows of x as they are, as far as sizes go: up to 16384 elements of a workgroup's 16 rows,

@@ -299,9 +299,12 @@ hipError_t launch_fp8_form(const wq_fp8_product &a, int form, hipStream_t s) {
         case WQ_FP8_TILE_64: return launch_fp8_tile<MODE, 2, 2, 2, 2, 1, 2>(a, s);
         case WQ_FP8_TILE_64_2: return launch_fp8_tile<MODE, 2, 2, 2, 2, 2, 2>(a, s);
         case WQ_FP8_TILE_64_2_3: return launch_fp8_tile<MODE, 2, 2, 2, 2, 2, 3>(a, s);
-        default:
+        case WQ_FP8_TILE_128_2:   // (not for the weights' gradient)
+            if constexpr (MODE != WQ_FP8_DIRECT_ROWS && MODE != WQ_FP8_VALUES) return launch_fp8_tile<MODE, 4, 4, 2, 2, 2, 2>(a, s);
+            return hipErrorInvalidValue;
+        default:   // (exact sums only)
             if constexpr (MODE == WQ_FP8_EXACT || MODE == WQ_FP8_EXACT_FP32) return launch_fp8_tile<MODE, 2, 2, 2, 2, 4, 2>(a, s);
-            return hipErrorInvalidValue;   // (the rules give it to no other)
+            return hipErrorInvalidValue;
     }
 }
 

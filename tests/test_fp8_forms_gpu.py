@@ -8,25 +8,26 @@ import torch
 pytestmark = pytest.mark.gpu
 
 U = 2.0 ** -24
-TILES = {"t256": 0, "t128": 1, "t128x64": 2, "t64": 3, "t64two": 4, "t64four": 5, "t64ring": 6}
+TILES = {"t256": 0, "t128": 1, "t128x64": 2, "t64": 3, "t64two": 4, "t64four": 5, "t64ring": 6, "t128two": 7}
 # rows, Cin, Cout, gated
 FORWARD = {
     "t256": (4090, 2100, 4090, False), "t256-gated": (4090, 2048, 8128, True),
     "t128": (1020, 2050, 8180, False), "t128-gated": (1020, 2048, 8128, True),
-    "t128x64": (1000, 500, 3190, False), "t128x64-gated": (1000, 640, 3136, True),
+    "t128x64": (1000, 2310, 4600, False), "t128x64-gated": (1000, 2304, 4608, True),
     "t64": (1000, 700, 2555, False), "t64-gated": (1000, 640, 2560, True),
     "t64two": (1300, 1100, 1010, False), "t64two-gated": (1300, 1150, 1024, True),
     "t64four": (200, 2100, 500, False), "t64four-gated": (200, 2050, 448, True),
     "t64ring": (200, 900, 500, False), "t64ring-gated": (300, 1152, 1024, True),
+    "t128two": (1000, 2100, 3450, False), "t128two-gated": (1000, 2050, 3456, True),
 }
 # rows, Cin, Cout: the gradient of x
 INPUT_GRADS = {
-    "t256": (4090, 4090, 2100), "t128": (1020, 8180, 2050), "t128x64": (1000, 3190, 700), "t64": (1000, 2555, 640),
+    "t256": (4090, 4090, 2100), "t128": (1020, 8180, 2050), "t128x64": (1000, 4600, 1400), "t128two": (1000, 3450, 5130), "t64": (1000, 2555, 640),
     "t64two": (1100, 1250, 1100), "t64ring": (300, 1010, 1000),
 }
 # the gradient of the weights
 WEIGHT_GRADS = {
-    "t256": (1000, 4090, 4090), "t128": (1000, 2040, 4090), "t128x64": (300, 1280, 2870), "t64": (200, 1000, 2555),
+    "t256": (1000, 4090, 4090), "t128": (1200, 2040, 4090), "t128x64": (300, 1280, 2870), "t64": (200, 1000, 2555),
     "t64two": (600, 1060, 1090), "t64ring": (1700, 500, 630),
 }
 # few rows: rows, Cin, Cout, gated
