@@ -532,7 +532,7 @@ wq_status_t wq_fp8_backward(const wq_fp8_plan_t *plan, void *stream, int rows, i
  * columns, a row counted as eight at most, or 2^30 columns -> UNSUPPORTED):
  *   h = x + residual in fp32, y = (h - mean) / sqrt(var + eps) gamma + beta, rounded as wq_fp8_layer_norm_quantize's v and then
  *   once to the type.  sum_dev as there.  y_dev may be x_dev or residual_dev itself with the same stride; sum_dev and y_dev are
- *   two tensors. */
+ *   two tensors (else INVALID_ARG). */
 wq_status_t wq_layer_norm(void *stream, int rows, int C, int type, const void *x_dev, int64_t x_stride,
                           const void *residual_dev, int64_t residual_stride, const float *gamma_dev, const float *beta_dev,
                           double eps, void *sum_dev, int64_t sum_stride, void *y_dev, int64_t y_stride);

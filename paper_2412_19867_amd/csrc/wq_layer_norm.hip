@@ -471,7 +471,7 @@ wq_status_t wq_layer_norm(void *stream, int rows, int C, int type, const void *x
     a.x = x_dev; a.res = residual_dev; a.sum = sum_dev; a.y = y_dev; a.gamma = gamma_dev; a.beta = beta_dev;
     a.xs = x_stride; a.rs = residual_stride; a.ss = sum_stride; a.ys = y_stride;
     a.rows = rows; a.C = C; a.eps = eps;
-    if (!wq_good_layer_norm(a, type) || (rows != 0 && !y_dev)) return WQ_ERR_INVALID_ARG;
+    if (!wq_good_layer_norm(a, type) || (rows != 0 && (!y_dev || y_dev == sum_dev))) return WQ_ERR_INVALID_ARG;
     if (!good_size(rows, C)) return WQ_ERR_UNSUPPORTED;
     if (rows == 0) return WQ_OK;
     return wq_launch_layer_norm(a, type, (hipStream_t)stream) == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;

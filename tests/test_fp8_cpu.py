@@ -218,10 +218,10 @@ NORM = "stream rows C type x xs res rs gamma beta eps sum ss y ys"
     (dict(rows=-1), INVALID), (dict(C=0), INVALID), (dict(type=3), INVALID), (dict(x=None), INVALID), (dict(y=None), INVALID), (dict(xs=63), INVALID),
     (dict(rs=63), INVALID), (dict(ss=63), INVALID), (dict(ys=63), INVALID), (dict(x=PTR + 1), INVALID), (dict(y=PTR + 1), INVALID),
     (dict(gamma=PTR + 2), INVALID), (dict(beta=PTR + 2), INVALID), (dict(eps=0.0), INVALID), (dict(eps=math.inf), INVALID),
-    (dict(rows=0, x=None, y=None), OK), (dict(rows=1 << 26), UNSUPPORTED),
+    (dict(sum=PTR), INVALID), (dict(rows=0, x=None, y=None), OK), (dict(rows=1 << 26), UNSUPPORTED),
     (dict(rows=1 << 24, C=4096, xs=4096, rs=4096, ss=4096, ys=4096), UNSUPPORTED)])
 def test_layer_norm_refusals(wq, change, status):
-    d = dict(stream=None, rows=4, C=64, type=1, x=PTR, xs=64, res=PTR, rs=64, gamma=PTR, beta=PTR, eps=1e-5, sum=PTR, ss=64, y=PTR, ys=64)
+    d = dict(stream=None, rows=4, C=64, type=1, x=PTR, xs=64, res=PTR, rs=64, gamma=PTR, beta=PTR, eps=1e-5, sum=PTR + 4096, ss=64, y=PTR, ys=64)
     assert call(wq.lib().wq_layer_norm, NORM, d, **change) == status
 
 
