@@ -289,10 +289,11 @@ __global__ __launch_bounds__(512, 4) void k_fp8_both(const wq_fp8_both_args firs
 }
 
 // db of partial sums [blocks][cols].
-__global__ __launch_bounds__(1024) void k_fp8_db(const float *part, int blocks, int cols, float *db, int accumulate) {
-    const long c = (long)blockIdx.x * 64 + (threadIdx.x & 63);
-    const double s = column_sum(part, blocks, cols, c, c < cols);
-    if (threadIdx.x < 64 && c < cols) db[c] = (float)(accumulate ? (double)db[c] + s : s);
+constexpr int kDbColumns = 16;
+__global__ __launch_bounds__(256) void k_fp8_db(const float *part, int blocks, int cols, float *db, int accumulate) {
+    const long c = (long)blockIdx.x * kDbColumns + threadIdx.x % kDbColumns;
+    const double s = column_sum<kDbColumns, 256>(part, blocks, cols, c, c < cols);
+    if (threadIdx.x < kDbColumns && c < cols) db[c] = (float)(accumulate ? (double)db[c] + s : s);
 }
 
 template <typename T>
@@ -432,7 +433,7 @@ hipError_t wq_launch_fp8_both(const wq_fp8_both_args &x, const wq_fp8_both_args 
 }
 
 hipError_t wq_launch_fp8_db(const float *part, int blocks, int cols, float *db, int accumulate, hipStream_t s) {
-    hipLaunchKernelGGL(k_fp8_db, dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, s, part, blocks, cols, db, accumulate);
+    hipLaunchKernelGGL(k_fp8_db, dim3((unsigned)((cols + kDbColumns - 1) / kDbColumns)), dim3(256), 0, s, part, blocks, cols, db, accumulate);
     return hipGetLastError();
 }
 

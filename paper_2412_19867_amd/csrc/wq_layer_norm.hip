@@ -192,7 +192,8 @@ void launch_norm(const wq_layer_norm_args &a, hipStream_t s) {
 // ------------------------------------------------------------ gradient
 // A workgroup's units of `wpr` waves take every units-th row; the weight's and bias's gradients of a unit's rows add up in its lanes'
 // registers and leave as one row of partial sums.
-//   bound: memory and the loads in flight: 4096x8192 fp32 98 us (403 MB, 4.1 TB/s; a large copy's 5.06 would be 80), 6.9 more for the columns.
+//   bound: memory and the 64-bit sums, which no other workgroup's loads hide in full: 4096x8192 fp32 98 us (403 MB, 4.1 TB/s; a large copy's 5.06
+//   would be 80), bf16 70; 6.9 more for the columns.  The row ahead on its way into LDS: 101 us, 8192x4096 less by as much.
 //   What the registers hold leaves two workgroups a CU; while one adds up a row's sums the other loads.
 template <int TYPE, int V, bool WHOLE>
 __global__ __launch_bounds__(512, V <= 2 ? 4 : 2) void k_layer_norm_grad(const wq_layer_norm_grad_args a, int wpr, int units) {
@@ -309,10 +310,11 @@ __global__ __launch_bounds__(512, V <= 2 ? 4 : 2) void k_layer_norm_grad(const w
 }
 
 // dgamma and dbeta of partial rows [units][2][C].
+template <int COLUMNS>
 __global__ __launch_bounds__(1024) void k_layer_norm_columns(const wq_layer_norm_grad_args a, int units) {
-    const long c = (long)blockIdx.x * 64 + (threadIdx.x & 63), n = 2L * a.C;
-    const double s = column_sum(a.part, units, n, c, c < n);
-    if (threadIdx.x >= 64 || c >= n) return;
+    const long c = (long)blockIdx.x * COLUMNS + threadIdx.x % COLUMNS, n = 2L * a.C;
+    const double s = column_sum<COLUMNS, 1024>(a.part, units, n, c, c < n);
+    if (threadIdx.x >= COLUMNS || c >= n) return;
     float *out = c < a.C ? a.dgamma : a.dbeta;
     const long i = c < a.C ? c : c - a.C;
     if (out) out[i] = (float)(a.accumulate ? (double)out[i] + s : s);
@@ -397,23 +399,31 @@ grad_form choose_grad_form(int rows, int C) {
     if (chunks > 32) return {4, 0, 4, 0, rows < 64 ? rows : 64};
     const row_form r = choose_rows(chunks);
     grad_form f = {r.wpr, r.V, r.wpr * r.upw, 0, 0};
-    // as many workgroups as the card holds at once
-    const int upw = r.upw, most = (f.V == 1 ? 1280 : f.V == 2 ? 1024 : 512) * 4 / f.waves;
-    f.blocks = (rows + upw - 1) / upw < most ? (rows + upw - 1) / upw : most;
+    // as many workgroups on each CU as it holds at once, all CUs alike, but four rows to a unit from 256 of them on, whose partial sums are
+    // written and read again: 8192x4096 fp32 89 us with two workgroups of eight waves a CU, 105 with two and a half;  2048x5120 bf16 two with four
+    // rows to a unit 34, three 43, four 55;  3000x640 bf16 one 18, five 25
+    const int upw = r.upw, all = (rows + upw - 1) / upw, resident = (f.V == 1 ? 20 : f.V == 2 ? 16 : 8) / f.waves;
+    const int four = all / 1024 < 1 ? 1 : all / 1024, most = 256 * (four < resident ? four : resident);
+    f.blocks = all < most ? all : most;
     f.units = f.blocks * upw;
     return f;
 }
 
 template <int TYPE>
 void launch_grad(const wq_layer_norm_grad_args &a, const grad_form &f, hipStream_t s) {
-    const unsigned columns = (unsigned)((2L * a.C + 63) / 64);
+    // (few columns in more workgroups, whose lanes then have fewer rows: 4096x1280 fp32 25.4 us in all, of 64 columns each 28.6; 2048x5120 36.8, 33.9)
+    auto add_columns = [&] {
+        const long n = 2L * a.C;
+        if (n >= 8192) hipLaunchKernelGGL(k_layer_norm_columns<64>, dim3((unsigned)((n + 63) / 64)), dim3(1024), 0, s, a, f.units);
+        else hipLaunchKernelGGL(k_layer_norm_columns<16>, dim3((unsigned)((n + 15) / 16)), dim3(1024), 0, s, a, f.units);
+    };
     if (f.V == 0) {
         if (a.part) {   // the rows' statistics, then the columns, before dx may take their place
             wq_layer_norm_grad_args first = a;
             first.dx = nullptr;
             hipLaunchKernelGGL((k_layer_norm_grad_long<TYPE>), dim3((unsigned)a.rows), dim3(256), 0, s, first);
             hipLaunchKernelGGL((k_layer_norm_columns_long<TYPE>), dim3((unsigned)((a.C + 63) / 64), (unsigned)f.units), dim3(256), 0, s, a, f.units);
-            hipLaunchKernelGGL(k_layer_norm_columns, dim3(columns), dim3(1024), 0, s, a, f.units);
+            add_columns();
         }
         if (a.dx) {
             wq_layer_norm_grad_args last = a;
@@ -431,7 +441,7 @@ void launch_grad(const wq_layer_norm_grad_args &a, const grad_form &f, hipStream
     };
     if (a.C % 8 == 0) launch(std::true_type{});
     else launch(std::false_type{});
-    if (a.part) hipLaunchKernelGGL(k_layer_norm_columns, dim3(columns), dim3(1024), 0, s, a, f.units);
+    if (a.part) add_columns();
 }
 
 bool good_type(int type) { return type == WQ_FP32 || type == WQ_BF16 || type == WQ_FP16; }
