@@ -191,7 +191,7 @@ void launch_norm(const wq_layer_norm_args &a, hipStream_t s) {
 
 // ------------------------------------------------------------ gradient
 // A workgroup's units of `wpr` waves take every units-th row; the weight's and bias's gradients of a unit's rows add up in its lanes'
-// registers and leave as one row of partial sums.
+// registers and leave as one row of partial sums of the workgroup.
 //   bound: memory and the 64-bit sums, which no other workgroup's loads hide in full: 4096x8192 fp32 98 us (403 MB, 4.1 TB/s; a large copy's 5.06
 //   would be 80), bf16 70; 6.9 more for the columns.  The row ahead on its way into LDS: 101 us, 8192x4096 less by as much.
 //   What the registers hold leaves two workgroups a CU; while one adds up a row's sums the other loads.
@@ -299,7 +299,25 @@ __global__ __launch_bounds__(512, V <= 2 ? 4 : 2) void k_layer_norm_grad(const w
         }
     }
     if (!a.part) return;
-    float *out = a.part + (size_t)unit * 2 * a.C;
+    if constexpr (V == 1) {
+        if (upw > 1) {   // the workgroup's units (rows of 1024 elements and less) leave one row of partial sums
+            __shared__ __attribute__((aligned(16))) float others[3 * 2 * 512];
+            const int u = w / wpr, at = (w % wpr) * 512 + lane * 8;
+            if (u > 0) {
+                float *mine = others + (u - 1) * 2 * 512 * wpr + at;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) mine[j] = dgamma[0][j], mine[512 * wpr + j] = dbeta[0][j];
+            }
+            __syncthreads();
+            if (u > 0) return;
+            for (int k = 0; k < upw - 1; ++k) {
+                const float *theirs = others + k * 2 * 512 * wpr + at;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) dgamma[0][j] += theirs[j], dbeta[0][j] += theirs[512 * wpr + j];
+            }
+        }
+    }
+    float *out = a.part + (size_t)blockIdx.x * 2 * a.C;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         const int c = c0 + k * step, n = a.C - c;
@@ -309,11 +327,11 @@ __global__ __launch_bounds__(512, V <= 2 ? 4 : 2) void k_layer_norm_grad(const w
     }
 }
 
-// dgamma and dbeta of partial rows [units][2][C].
+// dgamma and dbeta of partial rows [parts][2][C].
 template <int COLUMNS>
-__global__ __launch_bounds__(1024) void k_layer_norm_columns(const wq_layer_norm_grad_args a, int units) {
+__global__ __launch_bounds__(1024) void k_layer_norm_columns(const wq_layer_norm_grad_args a, int parts) {
     const long c = (long)blockIdx.x * COLUMNS + threadIdx.x % COLUMNS, n = 2L * a.C;
-    const double s = column_sum<COLUMNS, 1024>(a.part, units, n, c, c < n);
+    const double s = column_sum<COLUMNS, 1024>(a.part, parts, n, c, c < n);
     if (threadIdx.x >= COLUMNS || c >= n) return;
     float *out = c < a.C ? a.dgamma : a.dbeta;
     const long i = c < a.C ? c : c - a.C;
@@ -391,14 +409,14 @@ __global__ __launch_bounds__(256) void k_zero_columns(float *dgamma, float *dbet
 }
 
 struct grad_form {
-    int wpr, V, waves, blocks, units;   // V = 0: rows of any length
+    int wpr, V, waves, blocks, units, parts;   // parts: rows of partial sums.  V = 0: rows of any length
 };
 // Sizes alone decide: the workspace is as large as the most units that so many rows or fewer make.
 grad_form choose_grad_form(int rows, int C) {
     const int chunks = (C + 511) / 512;
-    if (chunks > 32) return {4, 0, 4, 0, rows < 64 ? rows : 64};
+    if (chunks > 32) return {4, 0, 4, 0, rows < 64 ? rows : 64, rows < 64 ? rows : 64};
     const row_form r = choose_rows(chunks);
-    grad_form f = {r.wpr, r.V, r.wpr * r.upw, 0, 0};
+    grad_form f = {r.wpr, r.V, r.wpr * r.upw, 0, 0, 0};
     // as many workgroups on each CU as it holds at once, all CUs alike, but four rows to a unit from 256 of them on, whose partial sums are
     // written and read again: 8192x4096 fp32 89 us with two workgroups of eight waves a CU, 105 with two and a half;  2048x5120 bf16 two with four
     // rows to a unit 34, three 43, four 55;  3000x640 bf16 one 18, five 25
@@ -406,6 +424,7 @@ grad_form choose_grad_form(int rows, int C) {
     const int four = all / 1024 < 1 ? 1 : all / 1024, most = 256 * (four < resident ? four : resident);
     f.blocks = all < most ? all : most;
     f.units = f.blocks * upw;
+    f.parts = f.blocks;
     return f;
 }
 
@@ -414,8 +433,8 @@ void launch_grad(const wq_layer_norm_grad_args &a, const grad_form &f, hipStream
     // (few columns in more workgroups, whose lanes then have fewer rows: 4096x1280 fp32 25.4 us in all, of 64 columns each 28.6; 2048x5120 36.8, 33.9)
     auto add_columns = [&] {
         const long n = 2L * a.C;
-        if (n >= 8192) hipLaunchKernelGGL(k_layer_norm_columns<64>, dim3((unsigned)((n + 63) / 64)), dim3(1024), 0, s, a, f.units);
-        else hipLaunchKernelGGL(k_layer_norm_columns<16>, dim3((unsigned)((n + 15) / 16)), dim3(1024), 0, s, a, f.units);
+        if (n >= 8192) hipLaunchKernelGGL(k_layer_norm_columns<64>, dim3((unsigned)((n + 63) / 64)), dim3(1024), 0, s, a, f.parts);
+        else hipLaunchKernelGGL(k_layer_norm_columns<16>, dim3((unsigned)((n + 15) / 16)), dim3(1024), 0, s, a, f.parts);
     };
     if (f.V == 0) {
         if (a.part) {   // the rows' statistics, then the columns, before dx may take their place
@@ -491,7 +510,7 @@ wq_status_t wq_layer_norm_workspace(int rows, int C, uint64_t *bytes) {
     if (rows < 0 || C < 1 || !bytes) return WQ_ERR_INVALID_ARG;
     if (!good_size(rows, C)) return WQ_ERR_UNSUPPORTED;
     const grad_form f = choose_grad_form(rows, C);
-    *bytes = ((uint64_t)f.units * 2 * (uint64_t)C * 4 + 255) / 256 * 256 + (f.V == 0 ? (uint64_t)rows * 16 : 0);
+    *bytes = ((uint64_t)f.parts * 2 * (uint64_t)C * 4 + 255) / 256 * 256 + (f.V == 0 ? (uint64_t)rows * 16 : 0);
     return WQ_OK;
 }
 
@@ -523,7 +542,7 @@ wq_status_t wq_layer_norm_grad(void *stream, int rows, int C, int type, const vo
     a.dys = dy_stride; a.hs = h_stride; a.rs = residual_grad_stride; a.dxs = dx_stride;
     a.rows = rows; a.C = C; a.accumulate = accumulate; a.eps = eps;
     a.part = columns ? (float *)workspace_dev : nullptr;
-    a.stats = (double *)((char *)workspace_dev + ((uint64_t)f.units * 2 * (uint64_t)C * 4 + 255) / 256 * 256);
+    a.stats = (double *)((char *)workspace_dev + ((uint64_t)f.parts * 2 * (uint64_t)C * 4 + 255) / 256 * 256);
     if (type == WQ_FP32) launch_grad<WQ_FP32>(a, f, s);
     else if (type == WQ_BF16) launch_grad<WQ_BF16>(a, f, s);
     else launch_grad<WQ_FP16>(a, f, s);
