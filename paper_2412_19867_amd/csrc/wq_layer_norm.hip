@@ -417,11 +417,11 @@ grad_form choose_grad_form(int rows, int C) {
     if (chunks > 32) return {4, 0, 4, 0, rows < 64 ? rows : 64, rows < 64 ? rows : 64};
     const row_form r = choose_rows(chunks);
     grad_form f = {r.wpr, r.V, r.wpr * r.upw, 0, 0, 0};
-    // as many workgroups on each CU as it holds at once, all CUs alike, but four rows to a unit from 256 of them on, whose partial sums are
-    // written and read again: 8192x4096 fp32 89 us with two workgroups of eight waves a CU, 105 with two and a half;  2048x5120 bf16 two with four
-    // rows to a unit 34, three 43, four 55;  3000x640 bf16 one 18, five 25
+    // as many workgroups on each CU as it holds at once, all CUs alike, but no more than one for each 1024 rows, since their partial sums are
+    // written and read again: 8192x4096 fp32 89 us with two workgroups of eight waves a CU, 105 with two and a half;  2048x5120 bf16 two 34,
+    // three 43, four 55;  4096x1280 fp32 two 26.6, four 25.4, six 27.5
     const int upw = r.upw, all = (rows + upw - 1) / upw, resident = (f.V == 1 ? 20 : f.V == 2 ? 16 : 8) / f.waves;
-    const int four = all / 1024 < 1 ? 1 : all / 1024, most = 256 * (four < resident ? four : resident);
+    const int each = rows < 2048 ? 1 : rows / 1024, most = 256 * (each < resident ? each : resident);
     f.blocks = all < most ? all : most;
     f.units = f.blocks * upw;
     f.parts = f.blocks;
