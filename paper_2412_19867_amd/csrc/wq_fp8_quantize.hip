@@ -135,7 +135,7 @@ __device__ __forceinline__ void activation_slope(const float (&z)[N], int act, f
 // leave through LDS, where they lie as in memory.
 //   ALONG: 0 no codes along the rows, 1 codes, 2 values in bf16.
 //   Two tensors in one launch: the first `blocks` workgroups take the first.
-//   bound: memory: x and dy of 4096 x 4096 bf16 into values and codes 33 us (150 MB).  Eight rows a lane and half the lanes: 35, and with
+//   bound: memory: x and dy of 4096 x 4096 bf16 into values and codes 31 us (150 MB).  Eight rows a lane and half the lanes: 35, and with
 //   a gate, whose three tensors then do not fit the registers, 42 in place of 26 (1000x1280, 2x5120 columns).
 template <int TYPE, int ALONG, bool WHOLE>
 __global__ __launch_bounds__(512, 4) void k_fp8_both(const wq_fp8_both_args first, const wq_fp8_both_args second, unsigned blocks) {
