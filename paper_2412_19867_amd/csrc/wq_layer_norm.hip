@@ -14,11 +14,11 @@ namespace {
 // Rows in pieces of eight elements a lane, held in registers: one pass over the data.  `wpr` waves share a row of up to 512 V wpr
 // elements.
 //   bound: the memory for many rows, below some 30 MB the launch and one round of loads: 777x5120 fp16 into codes 9.3 to 10.4 us (12 MB), 1x4096
-//   bf16 4.
+//   bf16 3.7; 4096x8192 fp32 67 (268 MB, 4.0 TB/s).
 template <int TYPE, bool CODES, int V, bool WHOLE>
-__global__ __launch_bounds__(512) void k_layer_norm(const wq_layer_norm_args a, int wpr, unsigned run) {
+__global__ __launch_bounds__(1024) void k_layer_norm(const wq_layer_norm_args a, int wpr, unsigned run) {
     using T = typename Elem<TYPE>::type;
-    __shared__ double part[8][2];
+    __shared__ double part[16][2];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int upw = (int)(blockDim.x >> 6) / wpr;   // rows of a workgroup
     // an XCD takes `run` workgroups in a row: neighbouring rows' codes share lines, which its L2 puts together
@@ -51,15 +51,32 @@ __global__ __launch_bounds__(512) void k_layer_norm(const wq_layer_norm_args a, 
             sums[0] += d;
             sums[1] = __builtin_fma(d, d, sums[1]);
         }
+    // gamma and beta come from the L2, which all rows ask for the same lines: with one piece a lane they are on their way while the sums are added up
+    // (1x4096 bf16 3.7 us, so 4.1; 512x4096 into codes 6.8, 7.3), with two their registers would cost a wave a SIMD (777x5120 fp16 12.4, so 9.3)
+    constexpr bool EARLY = V == 1;
+    float gms[EARLY ? V : 1][8], bts[EARLY ? V : 1][8];
+    auto load_weights = [&](int c, float (&gm)[8], float (&bt)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) gm[j] = 1.0f, bt[j] = 0.0f;
+        if (a.gamma) load8_row<float, WHOLE>(a.gamma, c, a.C, true, gm);
+        if (a.beta) load8_row<float, WHOLE>(a.beta, c, a.C, true, bt);
+    };
+    if constexpr (EARLY) {
+        asm volatile("" : "+v"(sums[0]), "+v"(sums[1]));
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < V; ++k) load_weights(c0 + k * step, gms[k], bts[k]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
     wave_sums(sums);
     if (wpr > 1) {
         if (lane == 0) part[w][0] = sums[0], part[w][1] = sums[1];
         __syncthreads();
         // a lane takes one wave's share of one sum
-        const int k = (lane >> 1) & 7;
+        const int k = (lane >> 1) & 15;
         double t = k < wpr ? part[w / wpr * wpr + k][lane & 1] : 0.0;
 #pragma unroll
-        for (int m = 2; m < 16; m <<= 1) t += __shfl_xor(t, m);
+        for (int m = 2; m < 32; m <<= 1) t += __shfl_xor(t, m);
         sums[0] = __shfl(t, 0);
         sums[1] = __shfl(t, 1);
     }
@@ -70,13 +87,13 @@ __global__ __launch_bounds__(512) void k_layer_norm(const wq_layer_norm_args a, 
     for (int k = 0; k < V; ++k) {
         const int c = c0 + k * step, n = a.C - c;
         if (a.sum && live && n > 0) store8_some<T>((T *)a.sum + p * a.ss + c, n, v[k]);
-        // (gamma and beta come from the L2, which all rows ask for the same lines: asked for with x, ahead of the sums, they hold up x
-        // itself, 777x5120 fp16 13.5 us in place of 10.4)
         float y[8], gm[8], bt[8];
+        if constexpr (EARLY) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) gm[j] = 1.0f, bt[j] = 0.0f;
-        if (a.gamma) load8_row<float, WHOLE>(a.gamma, c, a.C, true, gm);
-        if (a.beta) load8_row<float, WHOLE>(a.beta, c, a.C, true, bt);
+            for (int j = 0; j < 8; ++j) gm[j] = gms[k][j], bt[j] = bts[k][j];
+        } else {
+            load_weights(c, gm, bt);
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] = (float)((double)v[k][j] - mean) * r * gm[j] + bt[j];
         if constexpr (!CODES) {
@@ -153,14 +170,17 @@ __global__ __launch_bounds__(256) void k_layer_norm_long(const wq_layer_norm_arg
     }
 }
 
-// Pieces of 512 elements of a row over waves: as few pieces a lane as eight waves allow, and no more waves than hold them
-// (5120 columns: five waves with two pieces; eight, some with one, 12.2 us in place of 9.3 at 777 rows).
+// Pieces of 512 elements of a row over waves: up to 8 waves with two pieces a lane, longer rows over up to 16, with as few pieces a lane as they
+// allow, and no more waves than hold them (5120 columns: five waves with two pieces; eight, some with one, 12.2 us in place of 9.3 at 777
+// rows, ten with one 10.5; 8192 fp32 at 4096 rows: eight 67.7, sixteen with one piece 77.4; 12288 bf16 at 2000: twelve with two 32.6, six with
+// four 47.2).
 struct row_form {
     int V, wpr, upw;   // pieces a lane, waves to a row, rows of a workgroup
 };
 row_form choose_rows(int chunks) {
+    const int waves = chunks > 16 ? 16 : 8;
     row_form f = {1, 1, 1};
-    while (8 * f.V < chunks) f.V *= 2;
+    while (waves * f.V < chunks) f.V *= 2;
     f.wpr = (chunks + f.V - 1) / f.V;
     f.upw = f.wpr < 4 ? 4 / f.wpr : 1;
     return f;
@@ -182,8 +202,7 @@ void launch_norm(const wq_layer_norm_args &a, hipStream_t s) {
         constexpr bool W = decltype(whole)::value;
         if (V == 1) hipLaunchKernelGGL((k_layer_norm<TYPE, CODES, 1, W>), grid, block, 0, s, a, wpr, run);
         else if (V == 2) hipLaunchKernelGGL((k_layer_norm<TYPE, CODES, 2, W>), grid, block, 0, s, a, wpr, run);
-        else if (V == 4) hipLaunchKernelGGL((k_layer_norm<TYPE, CODES, 4, W>), grid, block, 0, s, a, wpr, run);
-        else hipLaunchKernelGGL((k_layer_norm<TYPE, CODES, 8, W>), grid, block, 0, s, a, wpr, run);
+        else hipLaunchKernelGGL((k_layer_norm<TYPE, CODES, 4, W>), grid, block, 0, s, a, wpr, run);
     };
     if (a.C % 8 == 0) launch(std::true_type{});
     else launch(std::false_type{});
@@ -196,9 +215,9 @@ void launch_norm(const wq_layer_norm_args &a, hipStream_t s) {
 //   would be 80), bf16 70; 6.9 more for the columns.  The row ahead on its way into LDS: 101 us, 8192x4096 less by as much.
 //   What the registers hold leaves two workgroups a CU; while one adds up a row's sums the other loads.
 template <int TYPE, int V, bool WHOLE>
-__global__ __launch_bounds__(512, V <= 2 ? 4 : 2) void k_layer_norm_grad(const wq_layer_norm_grad_args a, int wpr, int units) {
+__global__ __launch_bounds__(V == 1 ? 512 : 1024, 4) void k_layer_norm_grad(const wq_layer_norm_grad_args a, int wpr, int units) {
     using T = typename Elem<TYPE>::type;
-    __shared__ double part[2][8][4];
+    __shared__ double part[2][16][4];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int upw = (int)(blockDim.x >> 6) / wpr;
     const int unit = (int)blockIdx.x * upw + w / wpr;
@@ -256,11 +275,11 @@ __global__ __launch_bounds__(512, V <= 2 ? 4 : 2) void k_layer_norm_grad(const w
             double(*mine)[4] = part[i & 1];
             if (lane < 4) mine[w][lane] = lane == 0 ? sums[0] : lane == 1 ? sums[1] : lane == 2 ? sums[2] : sums[3];
             __syncthreads();
-            // a lane takes one wave's share of one sum (all 32 in each lane's registers would cost a workgroup a CU)
-            const int k = (lane >> 2) & 7;
+            // a lane takes one wave's share of one sum (all of them in each lane's registers would cost a workgroup a CU)
+            const int k = lane >> 2;
             double v = k < wpr ? mine[w / wpr * wpr + k][lane & 3] : 0.0;
 #pragma unroll
-            for (int m = 4; m < 32; m <<= 1) v += __shfl_xor(v, m);
+            for (int m = 4; m < 64; m <<= 1) v += __shfl_xor(v, m);
 #pragma unroll
             for (int j = 0; j < 4; ++j) sums[j] = __shfl(v, j);
         }
@@ -420,7 +439,7 @@ grad_form choose_grad_form(int rows, int C) {
     // as many workgroups on each CU as it holds at once, all CUs alike, but no more than one for each 1024 rows, since their partial sums are
     // written and read again: 8192x4096 fp32 89 us with two workgroups of eight waves a CU, 105 with two and a half;  2048x5120 bf16 two 34,
     // three 43, four 55;  4096x1280 fp32 two 26.6, four 25.4, six 27.5
-    const int upw = r.upw, all = (rows + upw - 1) / upw, resident = (f.V == 1 ? 20 : f.V == 2 ? 16 : 8) / f.waves;
+    const int upw = r.upw, all = (rows + upw - 1) / upw, resident = (f.V == 1 ? 20 : 16) / f.waves;
     const int each = rows < 2048 ? 1 : rows / 1024, most = 256 * (each < resident ? each : resident);
     f.blocks = all < most ? all : most;
     f.units = f.blocks * upw;
@@ -455,8 +474,7 @@ void launch_grad(const wq_layer_norm_grad_args &a, const grad_form &f, hipStream
     auto launch = [&](auto whole) {
         constexpr bool W = decltype(whole)::value;
         if (f.V == 1) hipLaunchKernelGGL((k_layer_norm_grad<TYPE, 1, W>), grid, block, 0, s, a, f.wpr, f.units);
-        else if (f.V == 2) hipLaunchKernelGGL((k_layer_norm_grad<TYPE, 2, W>), grid, block, 0, s, a, f.wpr, f.units);
-        else hipLaunchKernelGGL((k_layer_norm_grad<TYPE, 4, W>), grid, block, 0, s, a, f.wpr, f.units);
+        else hipLaunchKernelGGL((k_layer_norm_grad<TYPE, 2, W>), grid, block, 0, s, a, f.wpr, f.units);
     };
     if (a.C % 8 == 0) launch(std::true_type{});
     else launch(std::false_type{});

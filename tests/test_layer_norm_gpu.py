@@ -10,7 +10,8 @@ pytestmark = pytest.mark.gpu
 
 # rows, rows of the plan, C
 NORMS = [(1, 1, 1), (1, 3, 7), (1, 1, 4096), (3, 3, 513), (5, 8, 96), (7, 7, 640), (16, 16, 4096), (9, 33, 1281), (130, 130, 320), (2, 2, 8192),
-         (17, 17, 5120), (3, 3, 16385), (2, 4, 33280), (1, 1, 70001), (65, 65, 2047), (777, 777, 130), (1300, 1300, 24)]
+         (17, 17, 5120), (3, 3, 16385), (2, 4, 33280), (1, 1, 70001), (65, 65, 2047), (777, 777, 130), (1300, 1300, 24),
+         (5, 5, 8200), (4, 4, 12001), (3, 3, 16384), (3, 3, 24000), (2, 2, 32767)]   # over 16 waves, with two pieces a lane and with four
 
 
 def vectors(rng, C):
