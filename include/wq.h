@@ -529,7 +529,7 @@ wq_status_t wq_fp8_backward(const wq_fp8_plan_t *plan, void *stream, int rows, i
 
 /* ---------------------------------------------------------------------------
  * Layer norm of rows of any float type and any length C >= 1 (strides, alignment and errors as above; more than 2^25 pieces of 512
- * columns, a row counted as eight at most, or 2^30 columns -> UNSUPPORTED):
+ * columns, a row counted as 16 at most, or 2^30 columns -> UNSUPPORTED):
  *   h = x + residual in fp32, y = (h - mean) / sqrt(var + eps) gamma + beta, rounded as wq_fp8_layer_norm_quantize's v and then
  *   once to the type.  sum_dev as there.  y_dev may be x_dev or residual_dev itself with the same stride; sum_dev and y_dev are
  *   two tensors (else INVALID_ARG). */

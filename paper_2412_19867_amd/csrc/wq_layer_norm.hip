@@ -488,8 +488,8 @@ bool good_rows(const void *t, int64_t stride, int rows, int cols, int type) {
     return ((uintptr_t)t % (type == WQ_FP32 ? 4 : 2)) == 0 && (rows <= 1 || (stride >= cols && stride <= INT64_MAX / 16 / rows));
 }
 
-// (offsets of columns are 32 bits wide; a launch has less than 2^32 lanes, up to 512 of them to a row)
-bool good_size(int rows, int C) { return C <= 1 << 30 && (long)rows * (C <= 4096 ? (C + 511) / 512 : 8) <= 1 << 25; }
+// (offsets of columns are 32 bits wide; a launch has less than 2^32 lanes, up to 1024 of them to a row)
+bool good_size(int rows, int C) { return C <= 1 << 30 && (long)rows * (C <= 4096 ? (C + 511) / 512 : C <= 8192 ? 8 : 16) <= 1 << 25; }
 
 bool good_eps(double eps) { return eps >= FLT_MIN && eps <= DBL_MAX; }
 

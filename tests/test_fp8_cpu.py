@@ -243,6 +243,7 @@ def test_layer_norm_workspace(wq):
     import ctypes
     size, f = ctypes.c_uint64(), wq.lib().wq_layer_norm_workspace
     assert f(-1, 8, ctypes.byref(size)) == INVALID and f(1, 0, ctypes.byref(size)) == INVALID and f(1, 8, None) == INVALID
+    assert f(1 << 22, 9000, ctypes.byref(size)) == UNSUPPORTED and f(1 << 21, 9000, ctypes.byref(size)) == OK
     assert f(1 << 26, 8, ctypes.byref(size)) == UNSUPPORTED and f(8, (1 << 30) + 1, ctypes.byref(size)) == UNSUPPORTED
     for C in (1, 512, 8192, 16384, 20000):   # more rows need as much or more
         last = 0
