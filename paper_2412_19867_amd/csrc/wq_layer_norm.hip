@@ -2,6 +2,7 @@
 // scale for each 128 columns; and its gradient.
 #include <float.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "wq_column_sums.h"
@@ -346,15 +347,24 @@ __global__ __launch_bounds__(V == 1 ? 512 : 1024, 4) void k_layer_norm_grad(cons
     }
 }
 
+// Workgroups along the columns of a launch; each takes every so many blocks of columns (a launch has less than 2^32 lanes, and a row of 2^27
+// columns or more would ask for as many).
+constexpr long kMostColumnBlocks = 1 << 16;
+
 // dgamma and dbeta of partial rows [parts][2][C].
 template <int COLUMNS>
 __global__ __launch_bounds__(1024) void k_layer_norm_columns(const wq_layer_norm_grad_args a, int parts) {
-    const long c = (long)blockIdx.x * COLUMNS + threadIdx.x % COLUMNS, n = 2L * a.C;
-    const double s = column_sum<COLUMNS, 1024>(a.part, parts, n, c, c < n);
-    if (threadIdx.x >= COLUMNS || c >= n) return;
-    float *out = c < a.C ? a.dgamma : a.dbeta;
-    const long i = c < a.C ? c : c - a.C;
-    if (out) out[i] = (float)(a.accumulate ? (double)out[i] + s : s);
+    const long n = 2L * a.C;
+    for (long first = (long)blockIdx.x * COLUMNS; first < n; first += (long)gridDim.x * COLUMNS) {
+        const long c = first + threadIdx.x % COLUMNS;
+        const double s = column_sum<COLUMNS, 1024>(a.part, parts, n, c, c < n);
+        if (threadIdx.x < COLUMNS && c < n) {
+            float *out = c < a.C ? a.dgamma : a.dbeta;
+            const long i = c < a.C ? c : c - a.C;
+            if (out) out[i] = (float)(a.accumulate ? (double)out[i] + s : s);
+        }
+        __syncthreads();   // the shares have been read
+    }
 }
 
 // Rows of any length: a workgroup to a row, which it reads twice; the rows' mean and factor stay in the workspace for the columns' sums.
@@ -402,22 +412,26 @@ __global__ __launch_bounds__(256) void k_layer_norm_columns_long(const wq_layer_
     using T = typename Elem<TYPE>::type;
     __shared__ float part[2][4][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, unit = blockIdx.y;
-    const long c = (long)blockIdx.x * 64 + lane;
-    float dgamma = 0.0f, dbeta = 0.0f;
-    if (c < a.C)
-        for (long p = (long)unit + (long)w * units; p < a.rows; p += 4L * units) {
-            const float n = (float)((double)(float)((const T *)a.h)[p * a.hs + c] - a.stats[2 * p]) * (float)a.stats[2 * p + 1];
-            const float d = (float)((const T *)a.dy)[p * a.dys + c];
-            dgamma = __builtin_fmaf(d, n, dgamma);
-            dbeta += d;
+    for (long first = (long)blockIdx.x * 64; first < a.C; first += (long)gridDim.x * 64) {
+        const long c = first + lane;
+        float dgamma = 0.0f, dbeta = 0.0f;
+        if (c < a.C)
+            for (long p = (long)unit + (long)w * units; p < a.rows; p += 4L * units) {
+                const float n = (float)((double)(float)((const T *)a.h)[p * a.hs + c] - a.stats[2 * p]) * (float)a.stats[2 * p + 1];
+                const float d = (float)((const T *)a.dy)[p * a.dys + c];
+                dgamma = __builtin_fmaf(d, n, dgamma);
+                dbeta += d;
+            }
+        part[0][w][lane] = dgamma;
+        part[1][w][lane] = dbeta;
+        __syncthreads();
+        if (w == 0 && c < a.C) {
+            float *out = a.part + (size_t)unit * 2 * a.C + c;
+            out[0] = part[0][0][lane] + part[0][1][lane] + part[0][2][lane] + part[0][3][lane];
+            out[a.C] = part[1][0][lane] + part[1][1][lane] + part[1][2][lane] + part[1][3][lane];
         }
-    part[0][w][lane] = dgamma;
-    part[1][w][lane] = dbeta;
-    __syncthreads();
-    if (w || c >= a.C) return;
-    float *out = a.part + (size_t)unit * 2 * a.C + c;
-    out[0] = part[0][0][lane] + part[0][1][lane] + part[0][2][lane] + part[0][3][lane];
-    out[a.C] = part[1][0][lane] + part[1][1][lane] + part[1][2][lane] + part[1][3][lane];
+        __syncthreads();   // the sums have been read
+    }
 }
 
 __global__ __launch_bounds__(256) void k_zero_columns(float *dgamma, float *dbeta, int C) {
@@ -448,27 +462,30 @@ grad_form choose_grad_form(int rows, int C) {
 }
 
 template <int TYPE>
-void launch_grad(const wq_layer_norm_grad_args &a, const grad_form &f, hipStream_t s) {
+hipError_t launch_grad(const wq_layer_norm_grad_args &a, const grad_form &f, hipStream_t s) {
+    const auto column_blocks = [](long n, int columns) { return (unsigned)std::min((n + columns - 1) / columns, kMostColumnBlocks); };
     // (few columns in more workgroups, whose lanes then have fewer rows: 4096x1280 fp32 25.4 us in all, of 64 columns each 28.6; 2048x5120 36.8, 33.9)
     auto add_columns = [&] {
         const long n = 2L * a.C;
-        if (n >= 8192) hipLaunchKernelGGL(k_layer_norm_columns<64>, dim3((unsigned)((n + 63) / 64)), dim3(1024), 0, s, a, f.parts);
-        else hipLaunchKernelGGL(k_layer_norm_columns<16>, dim3((unsigned)((n + 15) / 16)), dim3(1024), 0, s, a, f.parts);
+        if (n >= 8192) hipLaunchKernelGGL(k_layer_norm_columns<64>, dim3(column_blocks(n, 64)), dim3(1024), 0, s, a, f.parts);
+        else hipLaunchKernelGGL(k_layer_norm_columns<16>, dim3(column_blocks(n, 16)), dim3(1024), 0, s, a, f.parts);
     };
     if (f.V == 0) {
         if (a.part) {   // the rows' statistics, then the columns, before dx may take their place
             wq_layer_norm_grad_args first = a;
             first.dx = nullptr;
             hipLaunchKernelGGL((k_layer_norm_grad_long<TYPE>), dim3((unsigned)a.rows), dim3(256), 0, s, first);
-            hipLaunchKernelGGL((k_layer_norm_columns_long<TYPE>), dim3((unsigned)((a.C + 63) / 64), (unsigned)f.units), dim3(256), 0, s, a, f.units);
+            hipLaunchKernelGGL((k_layer_norm_columns_long<TYPE>), dim3(column_blocks(a.C, 64), (unsigned)f.units), dim3(256), 0, s, a, f.units);
             add_columns();
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;   // (before anything is written over h or dy)
         }
         if (a.dx) {
             wq_layer_norm_grad_args last = a;
             last.stats = nullptr;
             hipLaunchKernelGGL((k_layer_norm_grad_long<TYPE>), dim3((unsigned)a.rows), dim3(256), 0, s, last);
         }
-        return;
+        return hipGetLastError();
     }
     const dim3 grid((unsigned)f.blocks), block(64 * f.waves);
     auto launch = [&](auto whole) {
@@ -479,6 +496,7 @@ void launch_grad(const wq_layer_norm_grad_args &a, const grad_form &f, hipStream
     if (a.C % 8 == 0) launch(std::true_type{});
     else launch(std::false_type{});
     if (a.part) add_columns();
+    return hipGetLastError();
 }
 
 bool good_type(int type) { return type == WQ_FP32 || type == WQ_BF16 || type == WQ_FP16; }
@@ -561,10 +579,8 @@ wq_status_t wq_layer_norm_grad(void *stream, int rows, int C, int type, const vo
     a.rows = rows; a.C = C; a.accumulate = accumulate; a.eps = eps;
     a.part = columns ? (float *)workspace_dev : nullptr;
     a.stats = (double *)((char *)workspace_dev + ((uint64_t)f.parts * 2 * (uint64_t)C * 4 + 255) / 256 * 256);
-    if (type == WQ_FP32) launch_grad<WQ_FP32>(a, f, s);
-    else if (type == WQ_BF16) launch_grad<WQ_BF16>(a, f, s);
-    else launch_grad<WQ_FP16>(a, f, s);
-    return hipGetLastError() == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;
+    const hipError_t e = type == WQ_FP32 ? launch_grad<WQ_FP32>(a, f, s) : type == WQ_BF16 ? launch_grad<WQ_BF16>(a, f, s) : launch_grad<WQ_FP16>(a, f, s);
+    return e == hipSuccess ? WQ_OK : WQ_ERR_DEVICE;
 }
 
 }  // extern "C"
