@@ -90,3 +90,10 @@ def test_the_longest_row(wq):
         check(dx[0, s], r * (d - mg - n * mgn), 10 * U * r * (d.abs() + abs(mg) + (n * mgn).abs()))
         check(dgamma[s], d * n, 30 * U * (d * n).abs())
         assert torch.equal(dbeta[s], dy[0, s].float())
+
+
+# nine to sixteen waves to a row and several rows to each (8193 to 16384 columns); longer rows, whose columns are added up by 64 units of four waves
+@pytest.mark.parametrize("dtype", NAMES)
+@pytest.mark.parametrize("n,C,over", [(600, 8200, "dy"), (520, 12001, None), (700, 16384, "h"), (70, 16392, None), (300, 16400, "h")])
+def test_several_rows_to_each_wave(wq, n, C, over, dtype):
+    run(wq, n, C, NAMES[dtype], over)
