@@ -434,9 +434,11 @@ wq_status_t wq_linear_forward(const wq_direct_plan_t *plan, void *stream, int ro
  * Weights of a checkpoint may have any fp32 scales instead (a plan made with fp32_scales), at a multiply-add per group and value.
  * Precision: a code times a power of two is a bf16 number, products of those are exact and the matrix core adds them with 24 bits:
  * z is within (Cin + 16) 2^-24 of |bias| + the sum of the terms' magnitudes, as long as codes times scales are normal bf16 numbers (2^-126
- * and up).  Gradients that are stored as bf16 or fp16 (dx, dw) are formed from the
- * codes directly at up to twice the rate: of eight neighbouring products the matrix core then drops what lies 2^-13 below the largest,
- * some 1.5e-5 of the result in the root mean square, where the type's own rounding is 1e-4 or more.
+ * and up).  Gradients that are stored as bf16 or fp16 (dx of more than a few rows, dw) are formed from the
+ * codes directly at up to twice the rate: the matrix core then cuts the products of each eight neighbours along the reduction, towards zero, to
+ * multiples of 2^-13 of the largest one's power of two.  The sum is within 7 2^-13 of the terms' magnitudes (a quarter of that at worst where it was
+ * measured), and in the root mean square off by 1.5e-5 of the results where values are of like size, by up to 9e-5 where some channels are twenty times
+ * as loud or tokens of very unlike size; the type's own rounding is 2e-4 (fp16) or 1.7e-3 (bf16).  Gradients in fp32 keep 24 bits.
  * Formats (sizes and offsets from wq_fp8_plan_layout; B = in_blocks, O = out_blocks, a piece is 16 codes of a row):
  *   weight blob : codes [ceil(Cout/16)][B][8 pieces][16 rows][16]          at blob_codes_off
  *                 scales fp32 [O][B], bias fp32 [ceil(Cout/16) 16]         at blob_scales_off, blob_bias_off
