@@ -539,7 +539,8 @@ wq_status_t wq_layer_norm(void *stream, int rows, int C, int type, const void *x
                           const void *residual_dev, int64_t residual_stride, const float *gamma_dev, const float *beta_dev,
                           double eps, void *sum_dev, int64_t sum_stride, void *y_dev, int64_t y_stride);
 
-/* Its gradient.  h_dev: what was normalized (sum_dev of the forward call, or x), whose mean and variance are formed again;
+/* Its gradient at the rows of h_dev (sum_dev of the forward call, or x), whose mean and variance are formed again.  With a residual the forward call
+ * normalizes the fp32 sum, and sum_dev is that rounded to the type: in 16 bits the gradient is that of rows a half step of the type away.
  *   n = (h - mean) r, g = dy gamma:  dx = r (g - mean(g) - n mean(g n)) + residual_grad, rounded once to the type
  *   dgamma = sum of dy n over the rows, dbeta = sum of dy, fp32 [C]; accumulate 1: added to what is there.
  * residual_grad_dev (NULL: none): the gradient that reached h on its other way (the residual stream's).  dx_dev, dgamma_dev and

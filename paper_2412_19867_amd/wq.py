@@ -849,8 +849,8 @@ class LayerNormPlan(_RowCalls):
 
     def backward(self, dy, h, ws, dx=None, gamma=None, eps=1e-5, residual_grad=None, dgamma=None, dbeta=None, accumulate=False,
                  stream=None):
-        """Gradients of forward() from dy, the gradient of y, and h, what was normalized: dx (the gradient of h, and so of x and of
-        the residual; may be dy or h itself) with `residual_grad` added, dgamma and dbeta, those that are given (the latter added
+        """Gradients of forward() from dy, the gradient of y, at the rows of h: x, or with a residual what `out` got (their sum rounded
+        to the type, of which forward() normalizes the fp32 sum): dx (the gradient of h, and so of x and of the residual; may be dy or h itself) with `residual_grad` added, dgamma and dbeta, those that are given (the latter added
         to what they hold with `accumulate`)."""
         C = self._cols
         n, dtype, code, dev, yp, ys = self._first(dy, C, "dy")
