@@ -1,6 +1,4 @@
 // The linear layer in 8-bit floating point: plans, checks and the calls of include/wq.h.
-#include <float.h>
-
 #include <new>
 
 #include "wq_fp8_form.h"

@@ -29,7 +29,11 @@ inline bool wq_fp8_full(long n128) { return (n128 + 511) / 512 * 512 <= 1.32 * n
 // exact: bf16 sums, else codes (half the time in the matrix core).  Over 239 drawn layers of 33 to 8192 rows 0.6 %
 // (geometric mean) above the best form, 23 % at most; us on either side of each line, rows x K -> columns, or the number of tiles:
 //   rows: up to 128 of them while there are at most 900 blocks of 16 x 16 (64x6592->1728 7.4, tiles 18.0; 80x1792->2048 6.5, 8.7;
-//     52x7744->9152, 2288 blocks: 27.8, 20.7); one block of rows a workgroup up to 16 rows or 256 blocks, else two
+//     52x7744->9152, 2288 blocks: 27.8, 20.7); one block of rows a workgroup up to 16 rows or 256 blocks, else two.
+//     The line was fitted on layers of 33 rows and more.  On 35 layers of 904 to 4000 blocks (K 1024 to 16384, gated or not, whole calls) the kernel
+//     for few rows is the better one beyond it too for one row, by 7 to 57 % (8192->28672 41, tiles 64; 1024->14464 6.8, 9.7), and for four rows in 31
+//     layers (8192->28672 43, 64; 4096->40960 38.7, 35.7); at 16 rows it depends on K (8192->28672 51, 65; 1024->28672 18.2, 11.5); 32 rows
+//     are better on tiles in 27 layers (8192->28672 65, 66; 4096->28672 39.8, 36.7), 128 in all (8192->28672 179, 71)
 //   256: reductions from 2048 on where the last round of 256 of them wastes less than they gain over 128 (a fifth):
 //     4096x4096->2x8192 393, 443; 2472x4608->2x2912 104, 121; 1000x1280->2x5120 38.5, 35
 //   128: where the card holds 512 of them and the last round is full (450 tiles, K 5632: 84, 128x64 94; 576, K 3328: 101, 91), not exact

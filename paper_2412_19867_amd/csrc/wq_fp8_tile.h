@@ -52,11 +52,12 @@ __device__ __forceinline__ v4f fp8_bias(const wq_fp8_product &a, int o) { return
 // order in which lanes read them, all but one of a team's NST stages while that is multiplied.  A product of a group is P = sum of a b; exact
 // modes convert the codes, with their powers of two, to bf16 on the way from LDS to the matrix core (a's each by one wave column, b's once a
 // stage); any fp32 scale of a's is applied to P in a multiply-add.
-//   bound: the matrix core, at the clock that its power leaves; converting takes turns with it on a SIMD.  4096x4096->2x8192 bf16 exact 393
-//   us, 1.40 PFLOP/s (the library's bf16 product of as many numbers 1.50; the same instructions on registers alone 2.03, from LDS with the
-//   conversions 1.78); values 4096x4096->4096, of 4096 rows, 119 us (1.16); codes directly 66 us (2.08; the library's with one scale for all 2.84).
-//   tried at 4096x4096->2x8192: 8 x 8 blocks a wave and four waves 441; half stages in a ring of three or four 402, 409; a wave's priority
-//   raised around its products 395; products of 32 x 32, on registers alone 12 % slower.
+//   bound: the matrix core, at the clock that its power leaves; converting takes turns with it on a SIMD.  4096x4096->2x8192 bf16 exact 405 to 415
+//   us, 1.33 to 1.36 PFLOP/s, and 415 to 515 in the first fifty launches after a pause, while the clock settles (the library's bf16 product of as many
+//   numbers 1.50; the same instructions on registers alone 2.03, from LDS with the conversions 1.78); values 4096x4096->4096, of 4096 rows, 107 us
+//   (1.28; 118 to 123 at first); codes directly 67 us (2.04; 72 to 77 at first; the library's with one scale for all 2.84).
+//   tried at 4096x4096->2x8192, the best of some runs each (this kernel's: 393): 8 x 8 blocks a wave and four waves 441; half stages in a ring of
+//   three or four 402, 409; a wave's priority raised around its products 395; products of 32 x 32, on registers alone 12 % slower.
 template <int MODE, int NA, int NB, int WA, int WB, int KS, int NST>
 __global__ __launch_bounds__(64 * WA * WB * KS, 2) void k_fp8_tile(const wq_fp8_product a, const wq_fp8_grid t) {
     constexpr int W = WA * WB, OA = NA * WA, OB = NB * WB;   // blocks of the workgroup tile

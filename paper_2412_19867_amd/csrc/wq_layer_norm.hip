@@ -15,7 +15,8 @@ namespace {
 // Rows in pieces of eight elements a lane, held in registers: one pass over the data.  `wpr` waves share a row of up to 512 V wpr
 // elements.
 //   bound: the memory for many rows, below some 30 MB the launch and one round of loads: 777x5120 fp16 into codes 9.3 to 10.4 us (12 MB), 1x4096
-//   bf16 3.7; 4096x8192 fp32 67 (268 MB, 4.0 TB/s).
+//   bf16 3.7; 4096x8192 fp32 68 (268 MB, 4.0 TB/s).  In 16 bits the loads, the 64-bit sums and the stores of a row take turns, and half the bytes hide
+//   less of the sums: 4096x8192 bf16 38 (134 MB, 3.5 TB/s), 2000x12288 32 (98 MB, 3.1), 2048x5120 15 (42 MB, 2.8).
 template <int TYPE, bool CODES, int V, bool WHOLE>
 __global__ __launch_bounds__(1024) void k_layer_norm(const wq_layer_norm_args a, int wpr, unsigned run) {
     using T = typename Elem<TYPE>::type;
@@ -121,7 +122,8 @@ __global__ __launch_bounds__(1024) void k_layer_norm(const wq_layer_norm_args a,
     }
 }
 
-// Rows of any length, read three times: a workgroup of four waves to a row, a wave to a group of 128 columns at a time.
+// Rows of any length, read twice: a workgroup of four waves to a row, a wave to a group of 128 columns at a time, element by element.
+//   bound: one row's loads wait for each other: 64x40000 bf16 82 us; 1000x40000 167 (160 MB, 1.0 TB/s), fp32 187.
 template <int TYPE, bool CODES>
 __global__ __launch_bounds__(256) void k_layer_norm_long(const wq_layer_norm_args a) {
     using T = typename Elem<TYPE>::type;
@@ -212,8 +214,9 @@ void launch_norm(const wq_layer_norm_args &a, hipStream_t s) {
 // ------------------------------------------------------------ gradient
 // A workgroup's units of `wpr` waves take every units-th row; the weight's and bias's gradients of a unit's rows add up in its lanes'
 // registers and leave as one row of partial sums of the workgroup.
-//   bound: memory and the 64-bit sums, which no other workgroup's loads hide in full: 4096x8192 fp32 98 us (403 MB, 4.1 TB/s; a large copy's 5.06
-//   would be 80), bf16 70; 6.9 more for the columns.  The row ahead on its way into LDS: 101 us, 8192x4096 less by as much.
+//   bound: memory and the 64-bit sums, which no other workgroup's loads hide in full: 4096x8192 fp32 96 to 105 us (403 MB, 3.8 to 4.2 TB/s; a large
+//   copy's 5.06 would be 80), 7 more for the columns.  In 16 bits the sums are what is left: with the columns 4096x8192 bf16 77 us (201 MB, 2.6 TB/s),
+//   2048x5120 34 (63 MB, 1.9), 2000x12288 67 (147 MB, 2.2).  The row ahead on its way into LDS: 101 us, 8192x4096 less by as much.
 //   What the registers hold leaves two workgroups a CU; while one adds up a row's sums the other loads.
 template <int TYPE, int V, bool WHOLE>
 __global__ __launch_bounds__(V == 1 ? 512 : 1024, 4) void k_layer_norm_grad(const wq_layer_norm_grad_args a, int wpr, int units) {
@@ -368,6 +371,8 @@ __global__ __launch_bounds__(1024) void k_layer_norm_columns(const wq_layer_norm
 }
 
 // Rows of any length: a workgroup to a row, which it reads twice; the rows' mean and factor stay in the workspace for the columns' sums.
+//   bound: one row's loads wait for each other, and h and dy are read four times in all: 1000x40000 bf16 with the weight's and bias's gradients 272 us
+//   (240 MB read and written once, 0.9 TB/s), fp32 393; 64x40000 bf16 171.
 template <int TYPE>
 __global__ __launch_bounds__(256) void k_layer_norm_grad_long(const wq_layer_norm_grad_args a) {
     using T = typename Elem<TYPE>::type;
